@@ -160,6 +160,35 @@ int32_t qrnnt_act_pitch(int32_t cols);
 qrnnt_status qrnnt_quantize_act_rows(const float *x, int64_t rows, int32_t cols, float inv_scale, int32_t bits,
                                      int8_t *q, int32_t ld_out, void *stream);
 
+/* ---- 8-bit activations with a range for each row ("token") ----
+ *
+ * The MAX range picker of Sec. 3.1 on activations: the step of a row follows from the row itself, so no range has to
+ * be known beforehand and one loud row does not cost the others their resolution.  A row that holds a value that is
+ * not finite gets scale NaN and codes 0, a row of zeros scale 1 and codes 0.  Codes lie in [-127, 127]; which of two
+ * codes a value next to their border gets is decided by the exact quotient (ties to even), not by its fp32 rounding.
+ *
+ * Element types of the floating arrays of these and the following calls.  Pitches (ld_*) are in elements and at least
+ * cols; rows may start at any element, 16-byte aligned ones are fastest. */
+enum { QRNNT_F32 = 0, QRNNT_F16 = 1, QRNNT_BF16 = 2 };
+
+/* scale[r] = max_k |x[r,k]| / 127, q[r,k] = rne(127 x[r,k] / max_k |x[r,k]|).  x [device] [rows, cols] of `dtype` with
+ * row pitch ld_x; q [device] int8, 16-byte aligned, row pitch ld_q bytes (>= cols, a multiple of 16, normally
+ * qrnnt_act_pitch(cols)), the bytes from column cols to qrnnt_act_pitch(cols) written as zero and those behind left as
+ * they are; scale [device] fp32 [rows].  No output may overlap an input.  rows = 0 does nothing. */
+qrnnt_status qrnnt_quantize_tokens(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t ld_x, int8_t *q,
+                                   int32_t ld_q, float *scale, void *stream);
+
+/* Residual sum, root-mean-square norm and quantizer in one pass:
+ *   h = x + residual, rounded to `dtype` and stored in sum_out (residual NULL: h = x, sum_out not written);
+ *   y = h / sqrt(mean_k h^2 + eps) * weight;   scale[r] = max|y| / 127;   q = rne(127 y / max|y|).
+ * The root divides all of a row alike, so the codes are those of h * weight and only the scale carries it.  weight
+ * [device] [cols] of `dtype`, or NULL for 1.  All matrices are [rows, cols] of `dtype` with pitches of their own;
+ * sum_out may be x or residual itself (same pitch), and may not overlap them otherwise.  eps >= 0.  q, scale and the
+ * rows that are zero or not finite as in qrnnt_quantize_tokens. */
+qrnnt_status qrnnt_rms_norm_quant(const void *x, const void *residual, const void *weight, int32_t dtype, int64_t rows,
+                                  int32_t cols, int64_t ld_x, int64_t ld_residual, float eps, void *sum_out,
+                                  int64_t ld_sum, int8_t *q, int32_t ld_q, float *scale, void *stream);
+
 /* ---- quantized linear layer (Sec. 3.2: weights and inputs quantized) ---- */
 
 /* y[n,r] = a_scale * row_scale[r] * sum_k w[r,k]*a[n,k] + bias[r]; with
@@ -179,6 +208,19 @@ qrnnt_status qrnnt_linear(const qrnnt_qmat *w, const float *bias, float a_scale,
  * external LM (Sec. 2). */
 qrnnt_status qrnnt_linear_quant(const qrnnt_qmat *w, const float *bias, float a_scale, const int8_t *a, int32_t N,
                                 float inv_scale, int32_t bits, int8_t *q, void *stream);
+
+/* y[m,r] = a_scale[m] * row_scale[r] * sum_k w[r,k]*a[m,k] + bias[r] for codes with a scale for each row of a (as
+ * qrnnt_quantize_tokens and qrnnt_rms_norm_quant write them): w 8-bit, TILED, cols <= 131071 (the sums are exact
+ * in int32 for any codes).  a [device] int8 [M, cols] with row pitch ld_a bytes (>= qrnnt_act_pitch(cols), a multiple
+ * of 16), 16-byte aligned; the bytes behind column cols may hold anything.  a_scale [device] fp32 [M].  bias [device]
+ * fp32 [rows] or NULL.  y [device] [M, rows] of y_dtype (QRNNT_F32, _F16, _BF16; rounded once from fp32) with row
+ * pitch ld_y elements >= rows.  workspace [device]: qrnnt_linear_tokens_workspace bytes, 256-byte aligned, or NULL
+ * where that is 0: products of few rows and a long sum are cut along the sum.  Calls that may run at the same time
+ * need workspaces of their own.  M = 0 does nothing. */
+size_t qrnnt_linear_tokens_workspace(const qrnnt_qmat *w, int32_t M);
+qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const int8_t *a, int32_t ld_a,
+                                 const float *a_scale, int32_t M, void *y, int32_t y_dtype, int64_t ld_y,
+                                 void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- LSTM: one step for a set of hypotheses (Sec. 3.2, Sec. 3.4) ---- */
 
@@ -350,6 +392,43 @@ qrnnt_status qrnnt_joint_fuse(const float *enc_proj, int32_t n_enc_rows, const i
 qrnnt_status qrnnt_beam_step(const float *score, const float *fused, int32_t B, int32_t W, int32_t V,
                              int32_t blank, int32_t force_blank, int32_t *parent_out, int32_t *token_out,
                              float *score_out, void *stream);
+
+/* Selection over large vocabularies, from logits.  Per utterance b the candidates of hypothesis w are (w,k) for all
+ * tokens k, valued
+ *   v = score[b,w] + (logits[b*W+w,k] - lse),   lse = log sum_k exp(logits[b*W+w,k])     (log_softmax != 0)
+ *   v = score[b,w] + logits[b*W+w,k]                                                     (log_softmax == 0),
+ * or, where finished[b,w] != 0, the single candidate (w, end_token) valued score[b,w] (its logits are not read).  The
+ * n_out best go best first to parent_out (w), token_out (k) and score_out [B,n_out]: by v, compared in fp64 and rounded
+ * to fp32 once, equal ones by w, then by logit, then by k (lowest w and k first).  Candidates valued -inf or NaN are
+ * never taken, so a hypothesis with score -inf, with all its logits -inf, or (log_softmax != 0) with a logit that is NaN
+ * or +inf has none.  Unfilled ranks get parent = token = -1, score = -inf.
+ * score [device] fp32 [B,W]; logits [device] [B*W, V] of `dtype` with row pitch ld elements; finished [device] [B,W] or
+ * NULL; finished_out [device] uint8 [B,n_out] or NULL: 1 where the parent was finished or the token is end_token (no
+ * token: -1), 0 elsewhere and for unfilled ranks.  W <= 64, n_out <= 64, W*V < 2^31.  No output may overlap an input.
+ * workspace [device]: qrnnt_beam_select_workspace bytes (0 on bad sizes), 256-byte aligned; calls that may run at the
+ * same time need workspaces of their own.  B = 0 does nothing. */
+size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, int32_t n_out);
+qrnnt_status qrnnt_beam_select(const float *score, const void *logits, int32_t dtype, int64_t ld, int32_t log_softmax,
+                               const uint8_t *finished, int32_t end_token, int32_t B, int32_t W, int32_t V,
+                               int32_t n_out, int32_t *parent_out, int32_t *token_out, float *score_out,
+                               uint8_t *finished_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Reordering of the states that belong to hypotheses (codes, cells, histories, caches) after a selection, all of them in
+ * one launch: for every array, row b*W_out + j of dst becomes row b*W + parent[b,j] of src, byte for byte.  Rows with
+ * a negative parent are left as they were; parents are clamped to W - 1.
+ * parent [device] int32 [B, W_out]; W, W_out <= 64; 1 to QRNNT_MAX_STATES arrays.  src may be dst (same pitch,
+ * W == W_out): then rows that stay are not touched.  No other overlap of a dst with any src or dst of the call.  Any
+ * alignment and row length; rows that start on 16-byte boundaries are fastest.  states [host] is read during the call
+ * only.  B = 0 does nothing. */
+#define QRNNT_MAX_STATES 32
+typedef struct {
+    const void *src;            /* [device] [B*W] rows */
+    void *dst;                  /* [device] [B*W_out] rows */
+    int64_t row_bytes;          /* bytes of a row that move, > 0 */
+    int64_t src_pitch, dst_pitch; /* bytes from row to row, >= row_bytes */
+} qrnnt_state_rows;
+qrnnt_status qrnnt_reorder_states(const qrnnt_state_rows *states, int32_t n_states, const int32_t *parent, int32_t B,
+                                  int32_t W, int32_t W_out, void *stream);
 
 /* ---- the whole decoding loop on the device (Sec. 2; Eq. 1) ---- */
 

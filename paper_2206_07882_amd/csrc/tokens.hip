@@ -1,0 +1,316 @@
+// 8-bit activations with a range for each row: the MAX range picker of Sec. 3.1 on activations, by itself
+// (qrnnt_quantize_tokens) and behind a residual sum and a root-mean-square norm (qrnnt_rms_norm_quant).
+//
+// q = rne(127 u / max|u|) with u = h * weight: the root mean square of the row divides u and its range alike, so the codes
+// need the largest |u| only and the root enters the scale.  One pass over memory: a row's u stay in registers between
+// the reduction and the codes.
+#include "elem.h"
+#include "kernels.h"
+
+namespace {
+
+struct QrTokenArgs {
+    const void *x, *residual, *weight;
+    void *sum;
+    int64_t rows, ld_x, ld_res, ld_sum;
+    int cols, ld_q;
+    float eps;
+    int8_t *q;
+    float *scale;
+};
+
+// What a row reduces to.  key: largest |u| as bits (NaN above infinity above numbers).  peak: the largest |u| where fp32
+// does not hold the products exactly.
+template <bool WIDE>
+struct QrRowSums {
+    float ss;
+    unsigned key;
+    double peak;
+
+    __device__ __forceinline__ void add(const QrRowSums &o)
+    {
+        ss += o.ss;
+        key = o.key > key ? o.key : key;
+        if (WIDE) peak = fmax(peak, o.peak);
+    }
+    __device__ __forceinline__ void reduce_wave(bool sums)
+    {
+        if (sums)
+            for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
+        key = qr_wave_reduce_u32<true>(key);
+        if (WIDE)
+            for (int off = 32; off > 0; off >>= 1) peak = fmax(peak, __shfl_xor(peak, off));
+    }
+};
+
+// Sum, largest value and "all finite" over the threads of a row, in fp64 (rows out of fp32's comfort only).
+template <int TPR>
+__device__ __forceinline__ void reduce_row64(double &sum, double &peak, bool &bad, double *lds)
+{
+    for (int off = 32; off > 0; off >>= 1) {
+        sum += __shfl_xor(sum, off);
+        peak = fmax(peak, __shfl_xor(peak, off));
+    }
+    bad = __any(bad);
+    if (TPR > 64) {
+        constexpr int NW = TPR / 64;
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            lds[wave] = sum;
+            lds[NW + wave] = peak;
+            lds[2 * NW + wave] = bad ? 1.0 : 0.0;
+        }
+        __syncthreads();
+        sum = 0.0, peak = 0.0;
+        double any = 0.0;
+        for (int w = 0; w < NW; ++w) {
+            sum += lds[w];
+            peak = fmax(peak, lds[NW + w]);
+            any += lds[2 * NW + w];
+        }
+        bad = any != 0.0;
+    }
+}
+
+// A row whose values fp32 does not carry well: all zero, not finite, squares or products that overflow or vanish.  All
+// of it in fp64, from the stored h.
+template <class T, bool NORM, int TPR>
+__device__ __forceinline__ void odd_row(const T *h, const T *weight, int cols, float eps, int t, int8_t *q, float *scale, double *lds)
+{
+    constexpr int V = QrVec<T>::N;
+    double sum = 0.0, peak = 0.0;
+    bool bad = false;
+    auto value = [&](int c) { return (double)(float)h[c] * (NORM && weight ? (double)(float)weight[c] : 1.0); };
+    for (int c0 = t * V; c0 < cols; c0 += TPR * V)
+        for (int i = 0; i < V && c0 + i < cols; ++i) {
+            const double u = value(c0 + i), hd = (double)(float)h[c0 + i];
+            bad |= !(fabs(u) < INFINITY) || !(fabs(hd) < INFINITY);
+            peak = fmax(peak, fabs(u));
+            sum += hd * hd;
+        }
+    reduce_row64<TPR>(sum, peak, bad, lds);
+    const bool none = bad || peak == 0.0;
+    for (int c0 = t * V; c0 < cols; c0 += TPR * V)
+        for (int i = 0; i < V && c0 + i < cols; ++i) q[c0 + i] = none ? 0 : (int8_t)(int)rint(127.0 * value(c0 + i) / peak);
+    if (t == 0) {
+        const double root = NORM ? sqrt(sum / cols + (double)eps) : 1.0;
+        *scale = bad ? NAN : (peak == 0.0 ? 1.0f : (float)(peak / root / 127.0));
+    }
+}
+
+// TPR threads to a row (64: four rows to a workgroup), PER vectors of 16 bytes to a thread; PER = 0: rows of any length, read
+// a second time for the codes.
+template <class T, bool NORM, int TPR, int PER>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void tokens_kernel(const QrTokenArgs a)
+{
+    constexpr int V = QrVec<T>::N, RPB = TPR < 256 ? 256 / TPR : 1, NW = TPR / 64;
+    constexpr bool WIDE = NORM && sizeof(T) == 4;   // products of two fp32 values do not fit fp32
+    __shared__ QrRowSums<WIDE> red[NW > 1 ? NW : 1];
+    __shared__ double red64[3 * NW];
+    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (row >= a.rows) return;   // (whole waves; where rows share a workgroup nothing waits for others)
+    const int t = threadIdx.x % TPR, cols = a.cols;
+    const T *x = (const T *)a.x + row * a.ld_x, *res = (const T *)a.residual, *weight = (const T *)a.weight;
+    T *sum = (T *)a.sum;
+    if (NORM && res) {
+        res += row * a.ld_res;
+        sum += row * a.ld_sum;
+    }
+    const T *h_at = NORM && res ? sum : x;   // where h can be read again
+    int8_t *q = a.q + row * a.ld_q;
+
+    QrRowSums<WIDE> s = {0.0f, 0u, 0.0};
+    // h of the vector at column c from its inputs; stores the sum
+    auto form = [&](int c, float (&v)[V], const float (&r)[V]) {
+        if (NORM && res) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = (float)(T)(v[i] + r[i]);
+            qr_store_vec(sum + c, cols - c, v);
+        }
+    };
+    // v: h on entry, u on return
+    auto take = [&](float (&v)[V], const float (&w)[V]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (NORM) s.ss = fmaf(v[i], v[i], s.ss);
+            if (WIDE) s.peak = fmax(s.peak, fabs((double)v[i] * (double)w[i]));
+            if (NORM) v[i] *= w[i];
+            const unsigned k = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+            s.key = k > s.key ? k : s.key;
+        }
+    };
+    auto ones = [](float (&w)[V]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = 1.0f;
+    };
+
+    constexpr int P = PER ? PER : 1;
+    float u[P][V];
+    if (PER) {
+        // all loads of the row first: a vector that lies inside the row as it is, what hangs over its end element by element
+        float r[P][V], w[P][V];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (p * TPR + t) * V, n = cols - c;
+            const bool whole = n >= V;
+            if (cols >= V) {   // uniform
+                const int at = whole ? c : 0;
+                qr_load_vec(x + at, u[p]);
+                if (NORM && res) qr_load_vec(res + at, r[p]);
+                if (NORM && weight) qr_load_vec(weight + at, w[p]);
+            }
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    u[p][i] = i < n ? (float)x[c + i] : 0.0f;
+                    if (NORM && res) r[p][i] = i < n ? (float)res[c + i] : 0.0f;
+                    if (NORM && weight) w[p][i] = i < n ? (float)weight[c + i] : 0.0f;
+                }
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (p * TPR + t) * V;
+            if (!(NORM && weight)) ones(w[p]);
+            form(c, u[p], r[p]);
+            take(u[p], w[p]);
+        }
+    } else {
+        for (int c = t * V; c < cols; c += TPR * V) {
+            float r[V], w[V];
+            qr_load_vec(x + c, cols - c, 0.0f, u[0]);
+            if (NORM && res) qr_load_vec(res + c, cols - c, 0.0f, r);
+            if (NORM && weight) qr_load_vec(weight + c, cols - c, 0.0f, w);
+            else ones(w);
+            form(c, u[0], r);
+            take(u[0], w);
+        }
+    }
+    s.reduce_wave(NORM);
+    if (NW > 1) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+        __syncthreads();
+        s = red[0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) s.add(red[w]);
+    }
+    const float peak = WIDE ? (float)s.peak : __uint_as_float(s.key);
+    // padding behind the last vector: up to 15 bytes, in words
+    if (t < 3 && qr_round_up(cols, V) + 4 * t < qr_act_pitch(cols)) *(unsigned *)(q + qr_round_up(cols, V) + 4 * t) = 0u;
+    if (!(peak >= 0x1p-60f && peak <= 0x1p100f && s.key < 0x7F800000u && (!NORM || (s.ss >= 0x1p-80f && s.ss < INFINITY)))) {   // uniform over the row
+        if (t < V && cols + t < qr_round_up(cols, V)) q[cols + t] = 0;
+        odd_row<T, NORM, TPR>(h_at, weight, cols, a.eps, t, q, a.scale + row, red64);
+        return;
+    }
+    const float inv = 127.0f / peak;
+    // u * inv is off by at most 3 roundings of 127 (2.3e-5): where it is nearer than 2^-14 to the border of two codes the
+    // quotient itself decides
+    auto codes = [&](int c, const float (&v)[V]) {
+        int k[V];
+        bool near = false;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float p = v[i] * inv, r = __builtin_rintf(p);
+            near |= fabsf(p - r) > 0.5f - 0x1p-14f;
+            k[i] = (int)r;
+        }
+        if (near) {
+            const double pk = WIDE ? s.peak : (double)peak;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                double e = (double)v[i];
+                if (WIDE && c + i < cols) e = (double)(float)h_at[c + i] * (weight ? (double)(float)weight[c + i] : 1.0);
+                k[i] = (int)rint(127.0 * e / pk);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V; i += 4)
+            *(unsigned *)(q + c + i) = (unsigned)(k[i] & 0xFF) | (unsigned)(k[i + 1] & 0xFF) << 8 | (unsigned)(k[i + 2] & 0xFF) << 16 | (unsigned)k[i + 3] << 24;
+    };
+    if (PER) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (p * TPR + t) * V;
+            if (c < cols) codes(c, u[p]);
+        }
+    } else {
+        for (int c = t * V; c < cols; c += TPR * V) {
+            float w[V];
+            qr_load_vec(h_at + c, cols - c, 0.0f, u[0]);
+            if (NORM && weight) {
+                qr_load_vec(weight + c, cols - c, 0.0f, w);
+#pragma unroll
+                for (int i = 0; i < V; ++i) u[0][i] *= w[i];
+            }
+            codes(c, u[0]);
+        }
+    }
+    if (t == 0) a.scale[row] = NORM ? (peak * (1.0f / sqrtf(s.ss / (float)cols + a.eps))) / 127.0f : peak / 127.0f;
+}
+
+template <class T, bool NORM>
+void launch_tokens(const QrTokenArgs &a, hipStream_t st)
+{
+    constexpr int V = QrVec<T>::N;
+    const int nv = (a.cols + V - 1) / V;
+#define QR_TOKENS(tpr, per) \
+    tokens_kernel<T, NORM, tpr, per><<<(unsigned)((a.rows + (tpr < 256 ? 256 / tpr : 1) - 1) / (tpr < 256 ? 256 / tpr : 1)), tpr < 256 ? 256 : tpr, 0, st>>>(a)
+    if (nv <= 64) QR_TOKENS(64, 1);
+    else if (nv <= 128) QR_TOKENS(64, 2);
+    else if (nv <= 256) QR_TOKENS(256, 1);
+    else if (nv <= 512) QR_TOKENS(256, 2);
+    else if (nv <= 1024) QR_TOKENS(256, 4);
+    else if (nv <= 2048) QR_TOKENS(1024, 2);
+    else if (nv <= 4096) QR_TOKENS(1024, 4);
+    else QR_TOKENS(1024, 0);
+#undef QR_TOKENS
+}
+
+template <bool NORM>
+qrnnt_status launch_tokens(int dtype, const QrTokenArgs &a, hipStream_t st)
+{
+    if (dtype == QRNNT_F32) launch_tokens<float, NORM>(a, st);
+    else if (dtype == QRNNT_F16) launch_tokens<_Float16, NORM>(a, st);
+    else launch_tokens<__bf16, NORM>(a, st);
+    return qr_launch_status();
+}
+
+}  // namespace
+
+extern "C" qrnnt_status qrnnt_quantize_tokens(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t ld_x, int8_t *q,
+                                              int32_t ld_q, float *scale, void *stream)
+{
+    QR_REQUIRE(qr_is_dtype(dtype), QRNNT_ERR_RANGE);
+    QR_REQUIRE(rows >= 0 && rows <= INT32_MAX && cols > 0 && ld_x >= cols && ld_q >= cols && ld_q % 16 == 0, QRNNT_ERR_SHAPE);
+    if (rows == 0) return QRNNT_OK;
+    QR_REQUIRE(x != nullptr && q != nullptr && scale != nullptr, QRNNT_ERR_NULL);
+    QR_REQUIRE(qr_aligned(x, qr_dtype_size(dtype)) && qr_aligned(q, 16) && qr_aligned(scale, 4), QRNNT_ERR_ALIGN);
+    QrTokenArgs a = {};
+    a.x = x;  a.rows = rows;  a.cols = cols;  a.ld_x = ld_x;  a.q = q;  a.ld_q = ld_q;  a.scale = scale;
+    return launch_tokens<false>(dtype, a, (hipStream_t)stream);
+}
+
+extern "C" qrnnt_status qrnnt_rms_norm_quant(const void *x, const void *residual, const void *weight, int32_t dtype, int64_t rows,
+                                             int32_t cols, int64_t ld_x, int64_t ld_residual, float eps, void *sum_out,
+                                             int64_t ld_sum, int8_t *q, int32_t ld_q, float *scale, void *stream)
+{
+    QR_REQUIRE(qr_is_dtype(dtype) && eps >= 0.0f && eps < INFINITY, QRNNT_ERR_RANGE);
+    QR_REQUIRE(rows >= 0 && rows <= INT32_MAX && cols > 0 && ld_x >= cols && ld_q >= cols && ld_q % 16 == 0, QRNNT_ERR_SHAPE);
+    QR_REQUIRE(residual == nullptr || (ld_residual >= cols && ld_sum >= cols), QRNNT_ERR_SHAPE);
+    if (rows == 0) return QRNNT_OK;
+    QR_REQUIRE(x != nullptr && q != nullptr && scale != nullptr && (residual == nullptr || sum_out != nullptr), QRNNT_ERR_NULL);
+    const size_t e = qr_dtype_size(dtype);
+    QR_REQUIRE(qr_aligned(x, e) && qr_aligned(residual, e) && qr_aligned(weight, e) && qr_aligned(sum_out, e) && qr_aligned(q, 16) && qr_aligned(scale, 4),
+               QRNNT_ERR_ALIGN);
+    if (residual != nullptr) {
+        const size_t bytes = qr_matrix_bytes(rows, cols, ld_sum, e);
+        QR_REQUIRE((sum_out == x && ld_sum == ld_x) || !qr_overlap(sum_out, bytes, x, qr_matrix_bytes(rows, cols, ld_x, e)), QRNNT_ERR_RANGE);
+        QR_REQUIRE((sum_out == residual && ld_sum == ld_residual) ||
+                       !qr_overlap(sum_out, bytes, residual, qr_matrix_bytes(rows, cols, ld_residual, e)), QRNNT_ERR_RANGE);
+    }
+    QrTokenArgs a = {};
+    a.x = x;  a.residual = residual;  a.weight = weight;  a.sum = sum_out;  a.rows = rows;  a.cols = cols;
+    a.ld_x = ld_x;  a.ld_res = ld_residual;  a.ld_sum = ld_sum;  a.eps = eps;  a.q = q;  a.ld_q = ld_q;  a.scale = scale;
+    return launch_tokens<true>(dtype, a, (hipStream_t)stream);
+}

@@ -59,10 +59,12 @@ class CModel(C.Structure):
 
 EXPORTS = ["qrnnt_status_str", "qrnnt_abi_version", "qrnnt_pack_int4_bytes", "qrnnt_pack_int4", "qrnnt_unpack_int4",
            "qrnnt_pack_int8_bytes", "qrnnt_pack_int8", "qrnnt_quantize_act8", "qrnnt_act_pitch", "qrnnt_quantize_act_rows",
-           "qrnnt_quantize_act", "qrnnt_linear", "qrnnt_linear_quant", "qrnnt_lstm_step", "qrnnt_lstm_layer_workspace", "qrnnt_lstm_layer",
+           "qrnnt_quantize_act", "qrnnt_quantize_tokens", "qrnnt_rms_norm_quant", "qrnnt_linear", "qrnnt_linear_quant",
+           "qrnnt_linear_tokens_workspace", "qrnnt_linear_tokens", "qrnnt_lstm_step", "qrnnt_lstm_layer_workspace", "qrnnt_lstm_layer",
            "qrnnt_input_projection", "qrnnt_input_table", "qrnnt_lstm_step_group", "qrnnt_lstm_step_group_listed",
            "qrnnt_bilstm_layer_workspace", "qrnnt_bilstm_layer", "qrnnt_lstm_layer_static",
-           "qrnnt_joint_fuse", "qrnnt_beam_step", "qrnnt_decode_workspace", "qrnnt_decode", "qrnnt_decode_ex",
+           "qrnnt_joint_fuse", "qrnnt_beam_step", "qrnnt_beam_select_workspace", "qrnnt_beam_select", "qrnnt_reorder_states",
+           "qrnnt_decode_workspace", "qrnnt_decode", "qrnnt_decode_ex",
            "qrnnt_decode_alsd_workspace", "qrnnt_decode_alsd", "qrnnt_decode_alsd_ex",
            "qrnnt_diag_mfma_forms", "qrnnt_diag_mfma_form_name", "qrnnt_diag_mfma_rate", "qrnnt_diag_lstm_layer", "qrnnt_diag_decode",
            "qrnnt_diag_decode_shared"]
@@ -102,6 +104,16 @@ def load():
         lib.qrnnt_linear_quant.argtypes = [vp, vp, f32, vp, i32, f32, i32, vp, vp]
         lib.qrnnt_joint_fuse.argtypes = [vp, i32, vp, vp, vp, vp, f32, f32, vp, vp, f32, f32, f32, i32, i32, vp, vp, vp, vp]
         lib.qrnnt_beam_step.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+        i64, size = C.c_int64, C.c_size_t
+        lib.qrnnt_quantize_tokens.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, vp]
+        lib.qrnnt_rms_norm_quant.argtypes = [vp, vp, vp, i32, i64, i32, i64, i64, f32, vp, i64, vp, i32, vp, vp]
+        lib.qrnnt_linear_tokens_workspace.restype = size
+        lib.qrnnt_linear_tokens_workspace.argtypes = [vp, i32]
+        lib.qrnnt_linear_tokens.argtypes = [vp, vp, vp, i32, vp, i32, vp, i32, i64, vp, size, vp]
+        lib.qrnnt_beam_select_workspace.restype = size
+        lib.qrnnt_beam_select_workspace.argtypes = [i32, i32, i32, i32]
+        lib.qrnnt_beam_select.argtypes = [vp, vp, i32, i64, i32, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, size, vp]
+        lib.qrnnt_reorder_states.argtypes = [vp, i32, vp, i32, i32, i32, vp]
         lib.qrnnt_lstm_step_group.argtypes = [vp, i32, vp]
         lib.qrnnt_lstm_step_group_listed.argtypes = [vp, i32, vp, vp, vp]
         _lib = lib
@@ -252,6 +264,123 @@ def linear_quant(w: QMat, bias: Optional[torch.Tensor], a_scale: float, a: torch
     _call("qrnnt_linear_quant", C.byref(cw), _addr(bias, torch.float32), a_scale, _addr(a, torch.int8), N, inv_scale,
           bits, q.data_ptr(), _stream_handle())
     return q
+
+
+F32, F16, BF16 = 0, 1, 2
+_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
+def _dtype(t: torch.dtype) -> int:
+    if t not in _DTYPES:
+        raise TypeError(f"expected float32, float16 or bfloat16, got {t}")
+    return _DTYPES[t]
+
+
+def _here(*tensors):
+    """The tensors a call works on have to be on the current device, on whose current stream it runs."""
+    current = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else -1
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"expected a tensor on the current GPU, got one on {t.device}")
+        if t is not None and t.get_device() < 0:
+            raise ValueError("expected a tensor on the GPU")
+
+
+def _matrix(t: torch.Tensor, dtype, rows: int, cols: int):
+    """(address, pitch) of a [rows, cols] matrix whose rows may lie apart."""
+    if t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"expected a matrix of {rows} x {cols}, got {tuple(t.shape)}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the elements of a row must be contiguous")
+    pitch = t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    if pitch < cols:
+        raise ValueError("rows must not overlap")
+    return t.data_ptr(), pitch
+
+
+def _vector(t: Optional[torch.Tensor], dtype, n: int):
+    if t is None:
+        return None
+    if t.numel() != n:
+        raise ValueError(f"expected {n} elements, got {t.numel()}")
+    return _addr(t, dtype)
+
+
+def _code_outputs(rows: int, cols: int, codes, scale, device):
+    ld = (cols + 15) // 16 * 16   # qrnnt_act_pitch
+    if codes is None:
+        codes = torch.empty((rows, ld), dtype=torch.int8, device=device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=device)
+    _here(codes, scale)
+    addr, ld = _matrix(codes, torch.int8, rows, codes.shape[1] if codes.dim() == 2 else ld)
+    if codes.shape[1] < (cols + 15) // 16 * 16:
+        raise ValueError(f"codes have {codes.shape[1]} columns, rows of {cols} take {(cols + 15) // 16 * 16}")
+    return codes, scale, addr, ld
+
+
+def quantize_tokens(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """[rows, cols] of float32, float16 or bfloat16 (rows may lie apart) -> int8 codes [rows, act_pitch(cols)] with zeros behind
+    the columns, and the scale of each row: 8 bits over the row's own range (qrnnt_quantize_tokens)."""
+    _here(x)
+    rows, cols = x.shape
+    px, ld = _matrix(x, x.dtype, rows, cols)
+    codes, scale, pq, ld_q = _code_outputs(rows, cols, codes, scale, x.device)
+    _call("qrnnt_quantize_tokens", px, _dtype(x.dtype), rows, cols, ld, pq, ld_q, _vector(scale, torch.float32, rows), _stream_handle())
+    return codes, scale
+
+
+def rms_norm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                   residual: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+                   codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """Residual sum, root-mean-square norm and 8-bit quantizer with a scale for each row (qrnnt_rms_norm_quant): returns
+    (codes, scale, x + residual, or x itself without a residual).  sum_out may be x or residual."""
+    _here(x, weight, residual, sum_out)
+    rows, cols = x.shape
+    px, ld = _matrix(x, x.dtype, rows, cols)
+    pr = ps = None
+    ld_r = ld_s = cols
+    if residual is not None:
+        pr, ld_r = _matrix(residual, x.dtype, rows, cols)
+        if sum_out is None:
+            sum_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        ps, ld_s = _matrix(sum_out, x.dtype, rows, cols)
+    elif sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    codes, scale, pq, ld_q = _code_outputs(rows, cols, codes, scale, x.device)
+    _call("qrnnt_rms_norm_quant", px, pr, _vector(weight, x.dtype, cols), _dtype(x.dtype), rows, cols, ld, ld_r, eps, ps, ld_s,
+          pq, ld_q, _vector(scale, torch.float32, rows), _stream_handle())
+    return codes, scale, x if residual is None else sum_out
+
+
+def linear_tokens_workspace(w: QMat, M: int) -> int:
+    cw = w.c()
+    return int(load().qrnnt_linear_tokens_workspace(C.byref(cw), M))
+
+
+def linear_tokens(w: QMat, codes: torch.Tensor, scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                  dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """8-bit linear layer of rows with a scale each, as quantize_tokens and rms_norm_quant return them: w from
+    pack_int8(..., LAYOUT_TILED), codes [M, act_pitch(cols)] (qrnnt_linear_tokens).  out may be a matrix whose rows lie apart."""
+    _here(codes, scale, bias, out, workspace, w.packed)
+    M = codes.shape[0]
+    pa, ld_a = _matrix(codes, torch.int8, M, codes.shape[1])
+    if codes.shape[1] < act_pitch(w.cols):
+        raise ValueError(f"codes have {codes.shape[1]} columns, a layer of {w.cols} reads {act_pitch(w.cols)}")
+    if out is None:
+        out = torch.empty((M, w.rows), dtype=dtype, device=codes.device)
+    py, ld_y = _matrix(out, out.dtype, M, w.rows)
+    cw = w.c()
+    if workspace is None:
+        need = int(load().qrnnt_linear_tokens_workspace(C.byref(cw), M))
+        workspace = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
+    n_ws = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("qrnnt_linear_tokens", C.byref(cw), _vector(bias, torch.float32, w.rows), pa, ld_a, _vector(scale, torch.float32, M), M,
+          py, _dtype(out.dtype), ld_y, _addr(workspace) if n_ws else None, n_ws, _stream_handle())
+    return out
 
 
 class Lstm:
@@ -464,6 +593,102 @@ def beam_step(score: torch.Tensor, fused: torch.Tensor, blank: int = 0, force_bl
     _call("qrnnt_beam_step", _addr(score, torch.float32), _addr(fused, torch.float32), B, W, V, blank,
           1 if force_blank else 0, par.data_ptr(), tok.data_ptr(), ns.data_ptr(), _stream_handle())
     return par, tok, ns
+
+
+def beam_select_workspace(B: int, W: int, V: int, n_out: int) -> int:
+    return int(load().qrnnt_beam_select_workspace(B, W, V, n_out))
+
+
+def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] = None, log_softmax: bool = True,
+                finished: Optional[torch.Tensor] = None, end_token: Optional[int] = None,
+                workspace: Optional[torch.Tensor] = None):
+    """The n_out (default: W) best extensions per utterance from score [B, W] and logits [B * W, V] (float32, float16 or
+    bfloat16; rows may lie apart): (parent, token, score, finished), each [B, n_out] (qrnnt_beam_select).  finished
+    [B, W] (bool or uint8): hypotheses that keep their score and repeat end_token; needs end_token.  The last result is None
+    without end_token."""
+    _here(score, logits, finished, workspace)
+    B, W = score.shape
+    V = logits.shape[-1]
+    K = W if n_out is None else n_out
+    dev = score.device
+    pl, ld = _matrix(logits, logits.dtype, B * W, V)
+    if finished is not None:
+        if end_token is None:
+            raise ValueError("finished hypotheses need an end_token")
+        if finished.dtype not in (torch.uint8, torch.bool):
+            raise TypeError(f"expected uint8 or bool, got {finished.dtype}")
+    par = torch.empty((B, K), dtype=torch.int32, device=dev)
+    tok = torch.empty((B, K), dtype=torch.int32, device=dev)
+    ns = torch.empty((B, K), dtype=torch.float32, device=dev)
+    done = None if end_token is None else torch.empty((B, K), dtype=torch.bool, device=dev)
+    if workspace is None:
+        need = beam_select_workspace(B, W, V, K)
+        if need == 0:
+            _check(7, "qrnnt_beam_select_workspace")
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _call("qrnnt_beam_select", _vector(score, torch.float32, B * W), pl, _dtype(logits.dtype), ld, 1 if log_softmax else 0,
+          None if finished is None else _vector(finished, finished.dtype, B * W), -1 if end_token is None else end_token,
+          B, W, V, K, par.data_ptr(), tok.data_ptr(), ns.data_ptr(), None if done is None else done.data_ptr(),
+          _addr(workspace), workspace.numel() * workspace.element_size(), _stream_handle())
+    return par, tok, ns, done
+
+
+class CStateRows(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("row_bytes", C.c_int64), ("src_pitch", C.c_int64),
+                ("dst_pitch", C.c_int64)]
+
+
+MAX_STATES = 32
+
+
+class StateGroup:
+    """Prepared argument block for qrnnt_reorder_states (built once, launched after every selection)."""
+
+    def __init__(self, states, B: int, W: int, W_out: Optional[int] = None):
+        """states: tensors [B * W, ...] that are reordered in place, or pairs (src [B * W, ...], dst [B * W_out, ...]) of one
+        type.  The first dimension may be strided (rows lie apart), the others are contiguous."""
+        self.B, self.W, self.W_out = int(B), int(W), int(W if W_out is None else W_out)
+        pairs = [s if isinstance(s, (tuple, list)) else (s, s) for s in states]
+        self._keep = pairs
+        self.n = len(pairs)
+        if not 1 <= self.n <= MAX_STATES:
+            raise ValueError(f"1 to {MAX_STATES} states, got {self.n}")
+        self.arr = (CStateRows * self.n)()
+        self.device = pairs[0][0].device
+        for i, (src, dst) in enumerate(pairs):
+            _here(src, dst)
+            if src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
+                raise ValueError("source and destination differ in type or row shape")
+            ps, pitch_s, bytes_ = self._rows(src, self.B * self.W)
+            pd, pitch_d, _ = self._rows(dst, self.B * self.W_out)
+            self.arr[i] = CStateRows(ps, pd, bytes_, pitch_s, pitch_d)
+
+    @staticmethod
+    def _rows(t: torch.Tensor, n: int):
+        """(address, pitch, bytes of a row)"""
+        if t.dim() < 1 or t.shape[0] != n:
+            raise ValueError(f"expected {n} rows, got {tuple(t.shape)}")
+        expected = 1
+        for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+            if size != 1 and stride != expected:
+                raise ValueError("the elements of a row must be contiguous")
+            expected *= size
+        row = expected * t.element_size()
+        return t.data_ptr(), max(t.stride(0) * t.element_size(), row) if n <= 1 else t.stride(0) * t.element_size(), row
+
+    def reorder(self, parent: torch.Tensor):
+        """Row b * W_out + j of every destination becomes row b * W + parent[b, j] of its source; parent [B, W_out] int32."""
+        _here(parent)
+        if parent.device != self.device:
+            raise ValueError("parent is on another device than the states")
+        _call("qrnnt_reorder_states", self.arr, self.n, _vector(parent, torch.int32, self.B * self.W_out), self.B, self.W, self.W_out,
+              _stream_handle())
+
+
+def reorder_states(states, parent: torch.Tensor, W: Optional[int] = None):
+    """StateGroup(states, ...).reorder(parent) for one time; parent [B, W_out], W: the sources' beam (default: W_out)."""
+    B, W_out = parent.shape
+    StateGroup(states, B, W_out if W is None else W, W_out).reorder(parent)
 
 
 class Net:

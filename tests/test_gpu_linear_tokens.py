@@ -1,0 +1,111 @@
+"""8-bit linear layers of rows with a scale each against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from . import plain64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+def make(seed, M, N, K, full=False):
+    r = np.random.RandomState(seed)
+    lo, hi = (-128, 128) if full else (-127, 128)
+    return dict(a=r.randint(lo, hi, (M, K)).astype(np.int8), w=r.randint(lo, hi, (N, K)).astype(np.int8),
+                sa=np.exp(r.randn(M)).astype(np.float32) / 100, sw=np.exp(r.randn(N)).astype(np.float32) / 100,
+                bias=r.randn(N).astype(np.float32))
+
+
+def pad(a, pitch, fill=0):
+    out = np.full((a.shape[0], pitch), fill, np.int8)
+    out[:, :a.shape[1]] = a
+    return torch.from_numpy(out).to(DEV)
+
+
+def weights(q, d):
+    return q.pack_int8(torch.from_numpy(d["w"]).to(DEV), q.LAYOUT_TILED, torch.from_numpy(d["sw"]).to(DEV))
+
+
+def tolerance(y, p, dtype):
+    """The sum is rounded to fp32, multiplied by the row's scale (two roundings of the product), by the token's in one
+    operation with the bias's addition (one rounding of the result), and rounded to its type."""
+    return 2.01 * 2.0 ** -24 * p + (2.0 ** -24 + plain64.HALF_STEP[dtype]) * np.abs(y) * (1 + 2.0 ** -8) + 2.0 ** -25
+
+
+def check(got, d, dtype, with_bias=True):
+    y, p = plain64.linear(d["a"], d["sa"], d["w"], d["sw"], d["bias"] if with_bias else None)
+    off = np.abs(got.float().cpu().numpy().astype(np.float64) - y) - tolerance(y, p, dtype)
+    assert off.max() <= 0, np.unravel_index(off.argmax(), off.shape)
+
+
+SIZES = [(1, 1, 1), (1, 16, 16), (1, 1000, 129), (2, 17, 63), (5, 64, 64), (16, 250, 300), (17, 256, 1280), (31, 130, 4100), (33, 48, 127), (63, 1000, 640),
+         (64, 512, 1024), (65, 100, 257), (77, 333, 1283), (128, 128, 128), (129, 257, 400), (200, 640, 272), (255, 255, 255),
+         (256, 256, 256), (257, 513, 129), (300, 1100, 2064), (513, 300, 96), (700, 768, 1536), (1025, 1031, 515)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_sizes(gpu_lib, dtype, M, N, K):
+    q = gpu_lib
+    d = make(M + 7 * N + 13 * K, M, N, K)
+    a = pad(d["a"], (K + 15) // 16 * 16, fill=113)   # what lies behind the columns may be anything
+    sa, bias = torch.from_numpy(d["sa"]).to(DEV), torch.from_numpy(d["bias"]).to(DEV)
+    m = weights(q, d)
+    check(q.linear_tokens(m, a, sa, bias=bias, dtype=dtype), d, dtype)
+    check(q.linear_tokens(m, a, sa, dtype=dtype), d, dtype, with_bias=False)
+
+
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_largest_sums_are_exact(gpu_lib, M):
+    """Codes of -128 throughout, the longest sum: 131071 * 2^14 is just below 2^31."""
+    q = gpu_lib
+    K, N = 131071, 20
+    a = torch.full((M, K + 1), -128, dtype=torch.int8, device=DEV)
+    m = q.pack_int8(torch.full((N, K), -128, dtype=torch.int8, device=DEV), q.LAYOUT_TILED)
+    y = q.linear_tokens(m, a, torch.ones(M, device=DEV))
+    assert bool((y == float(np.float32(131071 * 2 ** 14))).all())
+
+
+@pytest.mark.parametrize("M", [3, 130, 600])
+def test_rows_apart_and_neighbours(gpu_lib, M):
+    """Codes and results inside larger matrices, results at an odd element; what lies around them stays."""
+    q = gpu_lib
+    N, K = 203, 150
+    d = make(5, M, N, K)
+    a = pad(d["a"], 400, fill=-7)[:, :160]
+    sa, m = torch.from_numpy(d["sa"]).to(DEV), weights(q, d)
+    for dtype in TYPES:
+        big = torch.full((M + 2, 3 * N), 42.0, dtype=dtype, device=DEV)
+        out = big[1:M + 1, N + 1:2 * N + 1]
+        y = q.linear_tokens(m, a, sa, out=out)
+        assert y.data_ptr() == out.data_ptr()
+        check(out, d, dtype, with_bias=False)
+        assert bool((big[0] == 42).all()) and bool((big[-1] == 42).all())
+        assert bool((big[:, :N + 1] == 42).all()) and bool((big[:, 2 * N + 1:] == 42).all())
+
+
+def test_no_tokens_and_scales_that_are_not_finite(gpu_lib):
+    q = gpu_lib
+    d = make(9, 20, 40, 64)
+    m = weights(q, d)
+    assert q.linear_tokens(m, torch.empty((0, 64), dtype=torch.int8, device=DEV), torch.empty(0, device=DEV)).shape == (0, 40)
+    sa = torch.from_numpy(d["sa"]).to(DEV)
+    sa[3] = float("nan")
+    y = q.linear_tokens(m, pad(d["a"], 64), sa)
+    assert bool(torch.isnan(y[3]).all()) and not bool(torch.isnan(torch.cat([y[:3], y[4:]])).any())
+
+
+def test_the_same_call_gives_the_same_bits_whatever_the_workspace_held(gpu_lib):
+    q = gpu_lib
+    for M, N, K in ((16, 96, 8192), (100, 200, 4096), (300, 64, 6000)):
+        d = make(M, M, N, K)
+        a, sa, m = pad(d["a"], (K + 15) // 16 * 16), torch.from_numpy(d["sa"]).to(DEV), weights(q, d)
+        need = q.linear_tokens_workspace(m, M)
+        first = q.linear_tokens(m, a, sa)
+        check(first, d, torch.float32, with_bias=False)
+        for fill in (0, 255, 77):
+            ws = torch.full((need + 256,), fill, dtype=torch.uint8, device=DEV)
+            assert torch.equal(q.linear_tokens(m, a, sa, workspace=ws), first)
+            assert bool((ws[need:] == fill).all())
