@@ -1,7 +1,10 @@
 // 8-bit linear layers whose activations have a scale for each row: y[m,r] = a_scale[m] * row_scale[r] * sum + bias[r]
 // with exact int32 sums on the matrix units.
+#include <type_traits>
+
 #include "elem.h"
 #include "kernels.h"
+#include "mma_pipe.h"
 
 namespace {
 
@@ -14,6 +17,8 @@ struct QrTokensLinear {
     int ld_a, M;
     void *y;
     int64_t ld_y;
+    void *part;                   // [parts][M][ld_part] v4i: sums of the parts of a product that is cut along its columns
+    int ld_part;
 };
 
 // Four neighbouring rows of the layer for one token: the only place where sums are rounded (to fp32, and once more to the
@@ -35,75 +40,415 @@ __device__ __forceinline__ void finish(const QrTokensLinear &p, int m, int r0, v
     }
 }
 
-// Few tokens: the weights are what is read.  A workgroup has 64 rows x 16*NT tokens, its waves take the 128-column chunks in
-// turn (each weight fragment is fetched once) and join their sums through LDS; wave i finishes row tile i.
-// Grid: x = blocks of 64 rows, y = blocks of 16*NT tokens.
-template <class T, int NT>
-__global__ __launch_bounds__(256) void linear_tokens_few_kernel(const QrTokensLinear p)
+// Few tokens: the weights are what is read.  A workgroup has RT tiles of 16 rows x 16*NT tokens; its waves take the 128-column
+// chunks in turn (each weight fragment is fetched once, straight into registers) and join their sums through LDS, where wave i
+// finishes the row tiles i, i + WAVES, ...
+// Grid: x = blocks of 16*RT rows.
+template <class T, int RT, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void linear_tokens_few_kernel(const QrTokensLinear p)
 {
-    __shared__ v4i part[4][4][NT][64];   // [wave that summed][row tile][token tile]
+    __shared__ v4i part[WAVES][RT][NT][64];   // [wave that summed][row tile][token tile]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    const int n_row_tiles = (p.rows + 15) >> 4, rt0 = blockIdx.x * 4, m0 = blockIdx.y * 16 * NT;
-    const v4i *w[4];
+    const int n_row_tiles = (p.rows + 15) >> 4, rt0 = blockIdx.x * RT;
+    const v4i *w[RT];
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt) {
-        const int rt = rt0 + mt < n_row_tiles ? rt0 + mt : n_row_tiles - 1;
-        w[mt] = p.w + (size_t)rt * p.nkc * 128 + lane;
+    for (int i = 0; i < RT; ++i) {
+        const int rt = rt0 + i < n_row_tiles ? rt0 + i : n_row_tiles - 1;
+        w[i] = p.w + (size_t)rt * p.nkc * 128 + lane;
     }
     const int8_t *a[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int m = m0 + nt * 16 + col;
+        const int m = nt * 16 + col;
         a[nt] = p.a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_a;
     }
-    v4i acc[4][NT] = {};
-    for (int kc = wave; kc < p.nkc; kc += 4) {
+    v4i acc[RT][NT] = {};
+#pragma unroll 2
+    for (int kc = wave; kc < p.nkc; kc += WAVES) {
+        // columns behind the row's pitch: any of its bytes do, they meet the zero padding of the weights
+        int k0 = kc * QRNNT_KCHUNK + grp * 16, k1 = k0 + 64;
+        k0 = k0 < p.K ? k0 : 0;
+        k1 = k1 < p.K ? k1 : 0;
+        v4i wf[2][RT], af[2][NT];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            // columns behind the row's pitch: any of its bytes do, they meet the zero padding of the weights
-            int k = kc * QRNNT_KCHUNK + half * 64 + grp * 16;
-            k = k < p.K ? k : 0;
-            v4i wf[4], af[NT];
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt) wf[mt] = w[mt][(size_t)kc * 128 + half * 64];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) af[nt] = *(const v4i *)(a[nt] + k);
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = qr_mfma(wf[mt], af[nt], acc[mt][nt]);
+        for (int i = 0; i < RT; ++i) {
+            wf[0][i] = w[i][(size_t)kc * 128];
+            wf[1][i] = w[i][(size_t)kc * 128 + 64];
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            af[0][nt] = *(const v4i *)(a[nt] + k0);
+            af[1][nt] = *(const v4i *)(a[nt] + k1);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) acc[i][nt] = qr_mfma(wf[h][i], af[h][nt], acc[i][nt]);
     }
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt)
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) part[wave][mt][nt][lane] = acc[mt][nt];
+        for (int nt = 0; nt < NT; ++nt) part[wave][i][nt][lane] = acc[i][nt];
     __syncthreads();
-    const int r0 = (rt0 + wave) * 16 + grp * 4;
-    if (r0 >= p.rows) return;
-    float sw[4], bs[4];
+    // the RT x NT tiles of the result are dealt to the waves
+    for (int u = wave; u < RT * NT; u += WAVES) {
+        const int i = u / NT, nt = u % NT;
+        const int r0 = (rt0 + i) * 16 + grp * 4, m = nt * 16 + col;
+        if (r0 >= p.rows || m >= p.M) continue;
+        v4i sum = part[0][i][nt][lane];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = r0 + i < p.rows ? r0 + i : p.rows - 1;
-        sw[i] = p.s_w[r];
-        bs[i] = p.bias ? p.bias[r] : 0.0f;
-    }
+        for (int v = 1; v < WAVES; ++v) sum += part[v][i][nt][lane];
+        float sw[4], bs[4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int m = m0 + nt * 16 + col;
-        const v4i sum = part[0][wave][nt][lane] + part[1][wave][nt][lane] + part[2][wave][nt][lane] + part[3][wave][nt][lane];
-        if (m < p.M) finish<T>(p, m, r0, sum, sw, bs, p.s_a[m]);
+        for (int j = 0; j < 4; ++j) {
+            const int r = r0 + j < p.rows ? r0 + j : p.rows - 1;
+            sw[j] = p.s_w[r];
+            bs[j] = p.bias ? p.bias[r] : 0.0f;
+        }
+        finish<T>(p, m, r0, sum, sw, bs, p.s_a[m]);
     }
 }
 
-template <class T>
-void launch_linear_tokens(const QrTokensLinear &p, hipStream_t st)
+// One float a lane straight to LDS.
+__device__ __forceinline__ void qr_load_lds4(const void *gptr, unsigned lds_addr)
 {
-    const unsigned gx = (unsigned)((p.rows + 63) / 64);
-    if (p.M <= 16) linear_tokens_few_kernel<T, 1><<<gx, 256, 0, st>>>(p);
-    else if (p.M <= 32) linear_tokens_few_kernel<T, 2><<<gx, 256, 0, st>>>(p);
-    else linear_tokens_few_kernel<T, 4><<<dim3(gx, (unsigned)((p.M + 63) / 64)), 256, 0, st>>>(p);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr), "s"(lds_addr) : "memory");
+}
+
+// Many tokens: the matrix units are what is kept busy.  A workgroup of WN x WM waves has BN = 16*MT*WN weight rows x
+// BM = 16*NT*WM tokens.  LDS holds the weights of 2D steps of 64 columns (1 KiB blocks as the blob has them: operand order) and
+// the activations of D chunks of 128 (1 KiB blocks of 8 tokens x 128 bytes, lane l of the loading wave fetching token l/8's
+// 16-byte piece (l%8) ^ (l/8): whole lines per load, operand reads spread over the banks).  Both arrive by direct loads to LDS up
+// to three steps ahead, and a wave reads the next step's first operands before its last matrix instructions of the present one.
+template <int MT, int NT, int WN, int WM, int D>
+struct QrTile {
+    static constexpr int WAVES = WN * WM, THREADS = 64 * WAVES;
+    static constexpr int BN = 16 * MT * WN, BM = 16 * NT * WM;
+    static constexpr int A_BLOCKS = MT * WN, B_BLOCKS = 2 * NT * WM;      // of 1 KiB: weights of a step, activations of a chunk
+    static constexpr int A_LOADS = A_BLOCKS / WAVES, B_LOADS = B_BLOCKS / WAVES;
+    static constexpr int A_STAGE = A_BLOCKS * 1024, B_STAGE = B_BLOCKS * 1024;
+    static constexpr int B_AT = 2 * D * A_STAGE, TURN = B_AT + D * B_STAGE, SCALES = TURN + WAVES * 2048, LDS = SCALES + (2 * BN + BM) * 4;
+    static_assert(A_BLOCKS % WAVES == 0 && B_BLOCKS % WAVES == 0, "every wave loads as much");
+    static_assert(D == 2 || D == 4, "ring of chunks");
+};
+
+// T: type of y; v4i: the sums themselves go to p.part (a share of a product that is cut along its columns, blockIdx.y).
+template <class T, int MT, int NT, int WN, int WM, int D>
+__global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTokensLinear p, int tiles_n, int tiles_m)
+{
+    using P = QrTile<MT, NT, WN, WM, D>;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, grp = lane >> 4;
+    const int wn = wave % WN, wm = wave / WN;
+    // Workgroups go to the 8 XCDs in turn; each XCD gets a run of tiles, G blocks of rows side by side, so that what runs on it at a
+    // time shares its L2 (G = 2, 4, 8 at 8192^3: 431, 425, 423 us; at 16000 x 2560 x 1280: 78, 79, 84)
+    constexpr int G = 4;
+    const int total = tiles_n * tiles_m;
+    const int xcd = blockIdx.x & 7, each = total >> 3, rest = total & 7;
+    const int tile = xcd * each + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+    const int stripe = tile / (G * tiles_m), in_stripe = tile - stripe * G * tiles_m;
+    const int width = tiles_n - stripe * G < G ? tiles_n - stripe * G : G;
+    const int tn = stripe * G + in_stripe % width, tm = in_stripe / width;
+    const int n_row_tiles = (p.rows + 15) >> 4, rt0 = tn * (P::BN / 16), m0 = tm * P::BM;
+    const unsigned lds0 = (unsigned)(size_t)lds;
+    constexpr bool PART = std::is_same<T, v4i>::value;
+    const int kc0 = PART ? (int)((int64_t)p.nkc * blockIdx.y / gridDim.y) : 0;
+    const int nkc = PART ? (int)((int64_t)p.nkc * (blockIdx.y + 1) / gridDim.y) - kc0 : p.nkc;
+    if (!PART) {   // scales and bias of the tile: 64 to a load, which the waves take in turn
+        constexpr int N_SW = P::BN / 64, N_SA = P::BM / 64;
+        for (int j = wave; j < 2 * N_SW + N_SA; j += P::WAVES) {
+            const float *src;
+            if (j < 2 * N_SW) {
+                const int r = rt0 * 16 + (j % N_SW) * 64 + lane, rr = r < p.rows ? r : p.rows - 1;
+                src = j < N_SW || !p.bias ? p.s_w + rr : p.bias + rr;
+            } else {
+                const int m = m0 + (j - 2 * N_SW) * 64 + lane;
+                src = p.s_a + (m < p.M ? m : p.M - 1);
+            }
+            qr_load_lds4(src, lds0 + P::SCALES + j * 256);
+        }
+    }
+    const v4i *src_a[P::A_LOADS];
+    const int8_t *src_b[P::B_LOADS];
+#pragma unroll
+    for (int i = 0; i < P::A_LOADS; ++i) {
+        const int t = rt0 + wave * P::A_LOADS + i, rt = t < n_row_tiles ? t : n_row_tiles - 1;
+        src_a[i] = p.w + ((size_t)rt * p.nkc + kc0) * 128 + lane;
+    }
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+#pragma unroll
+    for (int i = 0; i < P::B_LOADS; ++i) {
+        const int m = m0 + (wave * P::B_LOADS + i) * 8 + (lane >> 3);
+        src_b[i] = p.a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_a + piece;
+    }
+    auto load_a = [&](int i, int k) { qr_load_lds16(src_a[i] + (size_t)k * 64, lds0 + (k & (2 * D - 1)) * P::A_STAGE + (wave * P::A_LOADS + i) * 1024); };
+    auto load_b = [&](int i, int kc) {
+        const int c = (kc0 + kc) * QRNNT_KCHUNK;   // columns behind the row: its start instead (they meet zero weights)
+        qr_load_lds16(src_b[i] + (c + piece < p.K ? c : -piece), lds0 + P::B_AT + (kc & (D - 1)) * P::B_STAGE + (wave * P::B_LOADS + i) * 1024);
+    };
+    // Order of all loads: A(0), then for every chunk c: B(c), A(2c + 1), A(2c + 2).  Chunks up to D - 2 are on their way before the
+    // loop; the two steps of chunk c start B(c + D - 1) and A(2(c + D) - 1), then A(2(c + D)).
+    auto load_group = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < P::B_LOADS; ++i) load_b(i, c);
+#pragma unroll
+        for (int i = 0; i < P::A_LOADS; ++i) load_a(i, 2 * c + 1);
+        if (c + 1 < nkc) {
+#pragma unroll
+            for (int i = 0; i < P::A_LOADS; ++i) load_a(i, 2 * c + 2);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < P::A_LOADS; ++i) load_a(i, 0);
+#pragma unroll
+    for (int c = 0; c < D - 1; ++c)
+        if (c < nkc) load_group(c);
+    const char *fa = lds + wn * MT * 1024 + lane * 16;
+    const char *fb = lds + P::B_AT + (wm * NT * 2 + (col >> 3)) * 1024 + (col & 7) * 128;
+    const int half0 = (grp ^ (col & 7)) * 16, half1 = ((4 + grp) ^ (col & 7)) * 16;
+
+    constexpr int AHEAD = MT > 2 ? 2 : 1;   // weight operands that are read ahead
+    v4i acc[MT][NT] = {}, b[2][NT] = {}, w[2][MT] = {};
+    auto wait = [&](auto left) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(left)::value) : "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto first_reads = [&](int k, auto half) {
+        constexpr int h = decltype(half)::value;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) b[h][nt] = *(const v4i *)(fb + ((k >> 1) & (D - 1)) * P::B_STAGE + nt * 2048 + (h ? half1 : half0));
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) w[h][j] = *(const v4i *)(fa + (k & (2 * D - 1)) * P::A_STAGE + j * 1024);
+    };
+    using std::integral_constant;
+    // one step of 64 columns.  LA, LB: it starts the loads of weights 2D - 1 steps / activations D - 1 chunks ahead; LEFT: loads that may
+    // be in flight when step k + 1 begins (-1: there is none)
+    auto step = [&](int k, auto half, auto la, auto lb, auto left) {
+        constexpr int h = decltype(half)::value, LEFT = decltype(left)::value;
+        constexpr int NB = decltype(lb)::value ? P::B_LOADS : 0, N = NB + (decltype(la)::value ? P::A_LOADS : 0), ROOM = MT - AHEAD;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            if (i + AHEAD < MT) w[h][i + AHEAD] = *(const v4i *)(fa + (k & (2 * D - 1)) * P::A_STAGE + (i + AHEAD) * 1024);
+#pragma unroll
+            for (int q = i * N / ROOM; i < ROOM && q < (i + 1) * N / ROOM; ++q) {
+                if (q < NB) load_b(q, (k >> 1) + D - 1);
+                else load_a(q - NB, k + 2 * D - 1);
+            }
+            if (i == ROOM && LEFT >= 0) {
+                wait(integral_constant<int, LEFT >= 0 ? LEFT : 0>{});
+                first_reads(k + 1, integral_constant<int, 1 - h>{});
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) acc[i][nt] = qr_mfma(w[h][i], b[h][nt], acc[i][nt]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    constexpr integral_constant<int, 0> zero{};
+    constexpr integral_constant<int, 1> one{};
+    constexpr int A = P::A_LOADS, GROUP = P::B_LOADS + 2 * A;   // loads of a wave: weights of a step, a chunk
+    static_assert((D - 1) * GROUP < 64, "the counter of loads has 6 bits");
+    if (nkc >= D) wait(integral_constant<int, (D - 2) * GROUP + 2 * A>{});
+    else wait(zero);   // (few columns: all of them)
+    first_reads(0, zero);
+    int kc = 0;
+    for (; kc < nkc - D; ++kc) {
+        step(2 * kc, zero, one, one, integral_constant<int, (D - 1) * GROUP>{});
+        step(2 * kc + 1, one, one, zero, integral_constant<int, (D - 2) * GROUP + 2 * A>{});
+    }
+    // the last D chunks, t = 0 .. D - 1 (of less than D: the last of these).  The first one's first step starts the last loads.
+    auto last = [&](auto tt) {
+        constexpr int t = decltype(tt)::value;
+        if (nkc < D - t) return;
+        step(2 * kc, zero, integral_constant<int, t == 0>{}, integral_constant<int, t == 0>{}, integral_constant<int, (D - 1 - t) * GROUP>{});
+        step(2 * kc + 1, one, zero, zero, integral_constant<int, t == D - 1 ? -1 : (D - 2 - t) * GROUP + A>{});
+        ++kc;
+    };
+    last(zero);
+    last(one);
+    if constexpr (D == 4) {
+        last(integral_constant<int, 2>{});
+        last(integral_constant<int, 3>{});
+    }
+    if constexpr (PART) {
+        // four rows of a token to a lane: neighbouring lanes' 64 bytes join in the L2, the sums are read again from there
+        v4i *part = (v4i *)p.part + (int64_t)blockIdx.y * p.M * p.ld_part;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int m = m0 + (wm * NT + nt) * 16 + col;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const int r4 = (rt0 + wn * MT + mt) * 4 + grp;
+                if (m < p.M && r4 < p.ld_part) part[(int64_t)m * p.ld_part + r4] = acc[mt][nt];
+            }
+        }
+        return;
+    } else {
+        const float *sc = (const float *)(lds + P::SCALES);
+        char *turn = lds + P::TURN + wave * 2048;
+        constexpr int E = 16 / sizeof(T), MG = 8 / (int)sizeof(T);   // elements of 16 bytes; row tiles whose 128 bytes of a token turn at a time
+        typedef T vec_e __attribute__((ext_vector_type(E)));
+        typedef T vec_4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float sa = sc[2 * P::BN + (wm * NT + nt) * 16 + col];
+#pragma unroll
+            for (int g = 0; g < MT / MG; ++g) {
+#pragma unroll
+                for (int j = 0; j < MG; ++j) {
+                    const int mt = g * MG + j, r = (wn * MT + mt) * 16 + grp * 4;
+                    const v4f sw = *(const v4f *)(sc + r), bs = *(const v4f *)(sc + P::BN + r);
+                    vec_4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (T)fmaf((float)acc[mt][nt][i] * sw[i], sa, p.bias ? bs[i] : 0.0f);
+                    const int at = (j * 16 + grp * 4) * (int)sizeof(T);
+                    *(vec_4 *)(turn + col * 128 + (((at >> 4) ^ (col & 7)) << 4) + (at & 15)) = v;
+                }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int t = i * 8 + (lane >> 3), m = m0 + (wm * NT + nt) * 16 + t;
+                    const int r = rt0 * 16 + (wn * MT + g * MG) * 16 + (lane & 7) * E;
+                    const vec_e v = *(const vec_e *)(turn + t * 128 + (((lane & 7) ^ (t & 7)) << 4));
+                    T *y = (T *)p.y + (int64_t)m * p.ld_y + r;
+                    if (m < p.M) {
+                        if (r + E <= p.rows) {
+                            *(typename QrVec<T>::any *)y = v;
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < E; ++e)
+                                if (r + e < p.rows) y[e] = v[e];
+                        }
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    }
+}
+
+
+// Joins the sums of a product that was cut along its columns: one thread has four rows of a token.
+template <class T>
+__global__ __launch_bounds__(256) void linear_tokens_join_kernel(const QrTokensLinear p, int n_parts)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int m = (int)(i / p.ld_part), r0 = (int)(i - (int64_t)m * p.ld_part) * 4;
+    if (m >= p.M || r0 >= p.rows) return;
+    const v4i *part = (const v4i *)p.part + i;
+    v4i sum = *part;
+    for (int s = 1; s < n_parts; ++s) sum += part[(int64_t)s * p.M * p.ld_part];
+    float sw[4], bs[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = r0 + j < p.rows ? r0 + j : p.rows - 1;
+        sw[j] = p.s_w[r];
+        bs[j] = p.bias ? p.bias[r] : 0.0f;
+    }
+    finish<T>(p, m, r0, sum, sw, bs, p.s_a[m]);
+}
+
+// How a product is computed.
+enum QrTokensKind { FEW, SMALL, MIDDLE, LARGE };
+struct QrTokensPlan {
+    QrTokensKind kind;
+    int parts;       // the columns are cut into (SMALL)
+};
+
+// Tiles by what they were measured to take (us): a chunk of 128 columns while at most half of the places on the device are
+// taken, and with all of them; what a tile costs besides.  256 compute units hold one large tile each, or two of the others.
+struct QrTileCost {
+    int size, places;
+    float alone, full, fixed;
+    float time(int64_t tiles, int chunks) const
+    {
+        const int64_t rounds = tiles / places, rest = tiles % places;
+        return rounds * (chunks * full + fixed) + (rest == 0 ? 0.0f : chunks * (rest <= places / 2 ? alone : full) + fixed);
+    }
+    int64_t tiles(int rows, int M) const { return (int64_t)((rows + size - 1) / size) * ((M + size - 1) / size); }
+};
+constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.28f, 0.43f, 1.5f}, {128, 512, 0.65f, 1.1f, 4.5f}, {256, 256, 1.0f, 1.4f, 9.0f}};
+
+// Measured at each choice (us; few / small / middle / large): 32 x 1000 x 1000 (tokens x rows x columns) 3.4 / 4.5; 48 x 16000 x
+// 4000 14.1 / 12.3; 200 x 8000 x 500 - / 4.5 / 7.7 / 12.9; 4000 x 1024 x 4096 - / 30.6 / 26.8 / 39.9; 2000 x 5000 x 3000 - / 59 / 46 /
+// 37; 8192^3 - / 879 / 569 / 403.  300 x 1024 x 8192 on small tiles whole 20.7, in two parts 15.1, in four 12.8.
+QrTokensPlan plan_linear_tokens(int rows, int K, int M)
+{
+    const int nkc = qr_round_up(K, QRNNT_KCHUNK) / QRNNT_KCHUNK;
+    // few tokens: beyond 16 their codes are fetched as often as the weights and more, so long or many rows go to tiles
+    if (M <= 16 || (M <= 32 && (rows <= 16384 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= 4096)) return {FEW, 1};
+    QrTokensPlan best = {SMALL, 1};
+    float least = INFINITY;
+    for (int kind = SMALL; kind <= LARGE; ++kind) {
+        const QrTileCost &c = TILE_COST[kind];
+        for (int parts = 1; parts <= (kind == SMALL ? 8 : 1) && (parts == 1 || nkc / parts >= 4); ++parts) {
+            const float join = parts == 1 ? 0.0f : 3.0f + (float)parts * M * rows * 8 / 4e6f;   // a launch, and the sums written and read at 4 TB/s
+            const float t = c.time(c.tiles(rows, M) * parts, (nkc + parts - 1) / parts) + join;
+            if (t < least) {
+                least = t;
+                best = {(QrTokensKind)kind, parts};
+            }
+        }
+    }
+    return best;
+}
+
+template <class T, int MT, int NT, int WN, int WM, int D>
+void launch_tiles(const QrTokensLinear &p, int parts, hipStream_t st)
+{
+    using P = QrTile<MT, NT, WN, WM, D>;
+    const int tn = (p.rows + P::BN - 1) / P::BN, tm = (p.M + P::BM - 1) / P::BM;
+    static bool allowed[QR_MAX_DEVICES];   // per device: more than 64 KiB of LDS
+    const int d = qr_current_device();
+    if (!allowed[d]) {
+        (void)hipFuncSetAttribute((const void *)linear_tokens_kernel<T, MT, NT, WN, WM, D>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
+        allowed[d] = true;
+    }
+    linear_tokens_kernel<T, MT, NT, WN, WM, D><<<dim3((unsigned)(tn * tm), parts), P::THREADS, P::LDS, st>>>(p, tn, tm);
+}
+
+template <class T, int RT, int NT, int WAVES>
+void launch_few(const QrTokensLinear &p, hipStream_t st)
+{
+    linear_tokens_few_kernel<T, RT, NT, WAVES><<<(unsigned)((p.rows + 16 * RT - 1) / (16 * RT)), 64 * WAVES, 0, st>>>(p);
+}
+
+template <class T>
+void launch_linear_tokens(const QrTokensLinear &p, const QrTokensPlan &plan, hipStream_t st)
+{
+    switch (plan.kind) {
+    case FEW:
+        // One row tile to a workgroup while that does not take more than two workgroups a compute unit; 8 waves where there are
+        // few of them (1 x 512 x 8192 3.7 us, with 4 waves 4.4; 16 x 8192 x 4096 7.3, with 4 waves 6.8).  Two row tiles beyond (16 x
+        // 32000 x 4096 24.6 us, one tile 29.5).
+        if (p.M <= 16) {
+            if (p.rows <= 4096) launch_few<T, 1, 1, 8>(p, st);
+            else if (p.rows <= 16384) launch_few<T, 1, 1, 4>(p, st);
+            else launch_few<T, 2, 1, 4>(p, st);
+        } else if (p.M <= 32) {
+            if (p.rows <= 4096) launch_few<T, 1, 2, 4>(p, st);
+            else launch_few<T, 2, 2, 4>(p, st);
+        } else {
+            launch_few<T, 1, 4, 4>(p, st);
+        }
+        return;
+    case SMALL:
+        if (plan.parts > 1) {
+            launch_tiles<v4i, 4, 1, 1, 4, 4>(p, plan.parts, st);
+            linear_tokens_join_kernel<T><<<(unsigned)(((int64_t)p.M * p.ld_part + 255) / 256), 256, 0, st>>>(p, plan.parts);
+        } else {
+            launch_tiles<T, 4, 1, 1, 4, 4>(p, 1, st);
+        }
+        return;
+    case MIDDLE: launch_tiles<T, 4, 4, 2, 2, 2>(p, 1, st); return;
+    case LARGE: launch_tiles<T, 8, 4, 2, 4, 2>(p, 1, st); return;
+    }
 }
 
 bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0 && w->cols > 0 && w->cols <= 131071; }
@@ -113,7 +458,8 @@ bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0
 extern "C" size_t qrnnt_linear_tokens_workspace(const qrnnt_qmat *w, int32_t M)
 {
     if (!tokens_weights_ok(w) || M <= 0) return 0;
-    return 0;
+    const int parts = plan_linear_tokens(w->rows, w->cols, M).parts;
+    return parts > 1 ? (size_t)parts * M * qr_round_up(w->rows, 4) * 4 : 0;
 }
 
 extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const int8_t *a, int32_t ld_a,
@@ -136,8 +482,11 @@ extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bi
     p.w = (const v4i *)w->packed;  p.s_w = w->row_scale;  p.bias = bias;
     p.nkc = qr_round_up(w->cols, QRNNT_KCHUNK) / QRNNT_KCHUNK;  p.rows = w->rows;  p.K = w->cols;
     p.a = a;  p.s_a = a_scale;  p.ld_a = ld_a;  p.M = M;  p.y = y;  p.ld_y = ld_y;
-    if (y_dtype == QRNNT_F32) launch_linear_tokens<float>(p, (hipStream_t)stream);
-    else if (y_dtype == QRNNT_F16) launch_linear_tokens<_Float16>(p, (hipStream_t)stream);
-    else launch_linear_tokens<__bf16>(p, (hipStream_t)stream);
+    p.part = workspace;  p.ld_part = qr_round_up(w->rows, 4) / 4;
+    const QrTokensPlan plan = plan_linear_tokens(w->rows, w->cols, M);
+    QR_REQUIRE(plan.kind == FEW || TILE_COST[plan.kind].tiles(w->rows, M) <= INT32_MAX, QRNNT_ERR_UNSUPPORTED);
+    if (y_dtype == QRNNT_F32) launch_linear_tokens<float>(p, plan, (hipStream_t)stream);
+    else if (y_dtype == QRNNT_F16) launch_linear_tokens<_Float16>(p, plan, (hipStream_t)stream);
+    else launch_linear_tokens<__bf16>(p, plan, (hipStream_t)stream);
     return qr_launch_status();
 }
