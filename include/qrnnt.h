@@ -404,7 +404,7 @@ qrnnt_status qrnnt_beam_step(const float *score, const float *fused, int32_t B, 
  * or +inf has none.  Unfilled ranks get parent = token = -1, score = -inf.
  * score [device] fp32 [B,W]; logits [device] [B*W, V] of `dtype` with row pitch ld elements; finished [device] [B,W] or
  * NULL; finished_out [device] uint8 [B,n_out] or NULL: 1 where the parent was finished or the token is end_token (no
- * token: -1), 0 elsewhere and for unfilled ranks.  W <= 64, n_out <= 64, W*V < 2^31.  No output may overlap an input.
+ * token: -1), 0 elsewhere and for unfilled ranks.  W <= 64, n_out <= 64, V <= 2^30, W*V < 2^31.  No output may overlap an input.
  * workspace [device]: qrnnt_beam_select_workspace bytes (0 on bad sizes), 256-byte aligned; calls that may run at the
  * same time need workspaces of their own.  B = 0 does nothing. */
 size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, int32_t n_out);

@@ -1,9 +1,15 @@
 // Beam selection over large vocabularies, from logits: log-softmax, scores and the best extensions of a beam (Sec. 2: up
 // to W hypotheses are kept per iteration) in one pass over the logits.
 //
-// A hypothesis' candidates are ordered as its logits are, so a stretch of a row can give up all but its n_out largest
-// logits before the row's log-sum-exp is known.  First launch: one workgroup per stretch holds it in registers, finds its
-// maximum, sum of exponentials and n_out largest logits.  Second launch: one workgroup per utterance joins sums and lists.
+// Short rows (a wave holds one in its registers): one launch, one workgroup per utterance.  Long rows: a hypothesis'
+// candidates are ordered as its logits are, so a stretch of a row can give up all but its n_out largest logits before the
+// row's log-sum-exp is known.  First launch: one workgroup per stretch holds it in registers, finds its maximum, sum of
+// exponentials and n_out largest logits.  Second launch: one workgroup per utterance joins sums and lists.
+//
+// The n_out best of many: the n_out-th largest of the best ones of 256 groups bounds the n_out-th best from below; what is not
+// below it (few more than n_out) is gathered in LDS and ranked by counting.  Where very many are equal, rank by rank.
+#include <float.h>
+
 #include "elem.h"
 #include "kernels.h"
 #include "select.h"
@@ -12,6 +18,11 @@ namespace {
 
 constexpr int MAX_OUT = 64;      // ranks
 constexpr int LIST = 512;        // candidates that a selection holds in LDS (more: it goes rank by rank)
+
+struct QrPartHead {
+    float top, pad;              // the stretch's largest logit (-inf: none)
+    double sum;                  // sum of exp(logit - top); NaN where a logit is NaN or +inf
+};
 
 struct QrSelectArgs {
     const float *score;
@@ -24,42 +35,139 @@ struct QrSelectArgs {
     int32_t *parent_out, *token_out;
     float *score_out;
     uint8_t *finished_out;
-    struct QrPartHead *heads;    // [B*W][n_parts]
+    QrPartHead *heads;           // [B*W][n_parts]
     QrCand *cands;               // [B*W][n_parts][K]: (key of the logit, token), best first, 0: none
 };
 
-struct QrPartHead {
-    float top, pad;              // the stretch's largest logit (-inf: none)
-    double sum;                  // sum of exp(logit - top); NaN where a logit is NaN or +inf
-};
+__device__ __forceinline__ bool is_finished(const QrSelectArgs &a, int64_t row) { return a.finished && a.finished[row]; }
+__device__ __forceinline__ bool reads_logits(const QrSelectArgs &a, int64_t row) { return a.score[row] > -INFINITY && !is_finished(a, row); }
 
-__device__ __forceinline__ bool takes_part(const QrSelectArgs &a, int64_t row)
+// A bound from below of the K-th largest of 256 groups' keys, four to a lane: the K-th largest itself, or a little less (as soon as
+// no more than `enough` groups pass); 0 if fewer than K groups have one.  top: the largest.  By bits of the distance from it, which
+// begin where the groups' distances do: the first bits of the keys themselves tell little apart.
+__device__ __forceinline__ unsigned bound_of(const unsigned (&g)[4], unsigned top, int K, int enough)
 {
-    const float s = a.score[row];
-    return s > -INFINITY && !(a.finished && a.finished[row]);
+    unsigned d[4], far = 0u;
+    int some = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        d[i] = g[i] ? top - g[i] : ~0u;
+        far = g[i] && d[i] > far ? d[i] : far;
+        some += (int)__popcll(__ballot(g[i] != 0u));
+    }
+    if (some < K) return 0u;   // uniform
+    far = qr_wave_reduce_u32<true>(far);
+    const int bits = 32 - __builtin_clz(far | 1u);
+    unsigned D = bits == 32 ? ~0u - 1u : (1u << bits) - 1u;
+    for (int bit = bits - 1; bit >= 0; --bit) {
+        const unsigned trial = D & ~(1u << bit);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += (int)__popcll(__ballot(d[i] <= trial));
+        if (n >= K) {
+            D = trial;   // uniform
+            if (n <= enough) break;
+        }
+    }
+    return D < top ? top - D : 1u;
 }
 
-// Grid: x = stretch, y (and z) = row.  256 threads, NV vectors of 16 bytes each.
-template <class T, int NV>
-__global__ __launch_bounds__(256) void select_parts_kernel(const QrSelectArgs a)
+// A value as a word: larger double <=> larger word; 0 for what is never taken.
+typedef unsigned long long QrValue;
+__device__ __forceinline__ QrValue value_word(double v)
 {
-    constexpr int V = QrVec<T>::N, PER = NV * V;
-    __shared__ QrCand list[LIST], best[MAX_OUT], wave_best[4];
-    __shared__ unsigned group_best[256];
-    __shared__ double wave_sum[4];
-    __shared__ int n_list;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
-    if (row >= (int64_t)a.B * a.W || !takes_part(a, row)) return;   // uniform; the second launch does not ask for it either
-    const int first = blockIdx.x * a.part, n = a.V - first < a.part ? a.V - first : a.part;
-    const T *x = (const T *)a.logits + row * a.ld + first;
-    if (tid == 0) n_list = 0;
-    if (tid < MAX_OUT) best[tid] = 0;
-    float f[PER];
+    if (!(v > -INFINITY)) return 0ull;
+    const QrValue u = (QrValue)__double_as_longlong(v + 0.0);
+    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
+}
+__device__ __forceinline__ double word_value(QrValue o)
+{
+    return __longlong_as_double((long long)((o >> 63) ? (o & 0x7FFFFFFFFFFFFFFFull) : ~o));
+}
+// A candidate of a beam: value, hypothesis, (logit, token).  Better: larger value, then lower hypothesis, then larger logit, then
+// lower token.
+struct QrPick {
+    QrValue v;
+    QrCand c;
+    int w;
+};
+__device__ __forceinline__ bool better(const QrPick &p, const QrPick &q) { return p.v != q.v ? p.v > q.v : (p.w != q.w ? p.w < q.w : p.c > q.c); }
+
+struct QrPickList {
+    QrValue v[LIST];
+    QrCand c[LIST];
+    int w[LIST];
+    int n;
+    QrPick wave_best[16];
+};
+__device__ __forceinline__ void push(QrPickList &l, const QrPick &p)
+{
+    const int at = atomicAdd(&l.n, 1);
+    if (at < LIST) {
+        l.v[at] = p.v;
+        l.c[at] = p.c;
+        l.w[at] = p.w;
+    }
+}
+
+__device__ __forceinline__ void put(const QrSelectArgs &a, int b, int r, const QrPick &p)
+{
+    const int64_t at = (int64_t)b * a.K + r;
+    a.parent_out[at] = p.v ? p.w : -1;
+    a.token_out[at] = p.v ? qr_cand_index(p.c) : -1;
+    a.score_out[at] = p.v ? (float)word_value(p.v) : -INFINITY;
+    if (a.finished_out) a.finished_out[at] = p.v && (is_finished(a, (int64_t)b * a.W + p.w) || qr_cand_index(p.c) == a.end_token) ? 1 : 0;
+}
+
+// Writes the utterance's ranks from the list, four threads counting for one candidate; each(visit) visits all candidates and is
+// what is gone by where the list did not hold them.
+template <int THREADS, class Each>
+__device__ __forceinline__ void write_ranks(const QrSelectArgs &a, int b, QrPickList &l, Each &&each)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, M = l.n;
+    if (M <= LIST) {
+        for (int i0 = 0; i0 < M; i0 += THREADS / 4) {   // uniform
+            const int i = i0 + (tid >> 2);
+            const QrPick mine = {l.v[i < M ? i : 0], l.c[i < M ? i : 0], l.w[i < M ? i : 0]};
+            int rank = 0;
+            for (int j = tid & 3; j < M; j += 4) rank += better({l.v[j], l.c[j], l.w[j]}, mine) ? 1 : 0;
+            rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
+            rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
+            if ((tid & 3) == 0 && i < M && rank < a.K) put(a, b, rank, mine);
+        }
+        for (int r = M + tid; r < a.K; r += THREADS) put(a, b, r, {0ull, 0ull, 0});
+        return;
+    }
+    QrPick last = {~0ull, ~0ull, -1};
+    for (int r = 0; r < a.K; ++r) {
+        QrPick best = {0ull, 0ull, 0x7fffffff};
+        each([&](const QrPick &p) {
+            if (better(last, p) && better(p, best)) best = p;
+        });
+        for (int off = 32; off > 0; off >>= 1) {
+            const QrPick o = {(QrValue)__shfl_xor(best.v, off), (QrCand)__shfl_xor(best.c, off), __shfl_xor(best.w, off)};
+            if (better(o, best)) best = o;
+        }
+        if (lane == 0) l.wave_best[wave] = best;
+        __syncthreads();
+        for (int i = 0; i < THREADS / 64; ++i)
+            if (better(l.wave_best[i], best)) best = l.wave_best[i];
+        __syncthreads();
+        if (tid == 0) put(a, b, r, best);
+        last = best;
+    }
+}
+
+// This lane's NV vectors of n logits: vector v of thread t of `threads` starts at element (v * threads + t) * V, wherever the
+// row begins (sums have to come out the same for the same row); -inf behind the end.
+template <class T, int NV>
+__device__ __forceinline__ void load_logits(const T *x, int n, int t, int threads, float (&f)[NV * QrVec<T>::N])
+{
+    constexpr int V = QrVec<T>::N;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         float u[V];
-        const int c = (v * 256 + tid) * V;
+        const int c = (v * threads + t) * V;
         if (c + V <= n) {
             qr_load_vec(x + c, u);
         } else {
@@ -69,52 +177,104 @@ __global__ __launch_bounds__(256) void select_parts_kernel(const QrSelectArgs a)
 #pragma unroll
         for (int i = 0; i < V; ++i) f[v * V + i] = u[i];
     }
+}
+__device__ __forceinline__ unsigned logit_key(float f) { return f > -INFINITY ? qr_float_key(f + 0.0f) : 0u; }   // (0 for NaN, too)
+// Sum over the wave, on the DPP path (row scans, then the two cross-row broadcasts of gfx9), in all lanes.
+__device__ __forceinline__ double wave_sum(double d)
+{
+#define QR_DPP_ADD(ctrl, rmask)                                                                                          \
+    {                                                                                                                    \
+        const unsigned long long u = (unsigned long long)__double_as_longlong(d);                                        \
+        const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, rmask, 0xf, false);          \
+        const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, rmask, 0xf, false);  \
+        d += __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));                                       \
+    }
+    QR_DPP_ADD(0x111, 0xf)   // row_shr:1
+    QR_DPP_ADD(0x112, 0xf)   // row_shr:2
+    QR_DPP_ADD(0x114, 0xf)   // row_shr:4
+    QR_DPP_ADD(0x118, 0xf)   // row_shr:8
+    QR_DPP_ADD(0x142, 0xa)   // row_bcast:15 into rows 1 and 3
+    QR_DPP_ADD(0x143, 0xc)   // row_bcast:31 into rows 2 and 3
+#undef QR_DPP_ADD
+    const unsigned long long u = (unsigned long long)__double_as_longlong(d);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, 63), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), 63);
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+// Largest of four neighbouring lanes.
+__device__ __forceinline__ unsigned quad_max(unsigned v)
+{
+    unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true);
+    v = o > v ? o : v;
+    o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true);
+    return o > v ? o : v;
+}
+
+// Long rows, first launch.  Grid: x = stretch, y (and z) = row; NT = 256 or 1024 threads with NV vectors each.
+template <class T, int NV, int NT>
+__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 5) void select_parts_kernel(const QrSelectArgs a)
+{
+    constexpr int V = QrVec<T>::N, PER = NV * V, NW = NT / 64;
+    __shared__ QrCand list[LIST], best[MAX_OUT], wave_best[NW];
+    __shared__ unsigned group_best[256];
+    __shared__ double sums[NW];
+    __shared__ int n_list;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
+    if (row >= (int64_t)a.B * a.W || !reads_logits(a, row)) return;   // uniform; the second launch does not ask for it either
+    const int first = blockIdx.x * a.part, n = a.V - first < a.part ? a.V - first : a.part;
+    if (tid == 0) n_list = 0;
+    if (tid < MAX_OUT) best[tid] = 0;
+    float f[PER];
+    load_logits<T, NV>((const T *)a.logits + row * a.ld + first, n, tid, NT, f);
     float largest = -INFINITY;   // (NaN is passed over here and found again in the sum)
 #pragma unroll
     for (int i = 0; i < PER; ++i) largest = fmaxf(largest, f[i]);
-    group_best[tid] = largest > -INFINITY ? qr_float_key(largest + 0.0f) : 0u;
+    if (NT == 256) {
+        group_best[tid] = logit_key(largest);
+    } else {
+        const unsigned k = quad_max(logit_key(largest));
+        if ((tid & 3) == 0) group_best[tid >> 2] = k;
+    }
     __syncthreads();
-    unsigned g[4];
+    unsigned g[4], top_key = 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g[i] = group_best[i * 64 + lane];
-    const QrBound bound(g, a.K);
-    const float top = bound.top ? bound.v_max : -INFINITY;
+    for (int i = 0; i < 4; ++i) {
+        g[i] = group_best[i * 64 + lane];
+        top_key = g[i] > top_key ? g[i] : top_key;
+    }
+    top_key = qr_wave_reduce_u32<true>(top_key);
+    const float top = top_key ? qr_key_float(top_key) : -INFINITY;
     if (a.log_softmax) {
-        const float m = bound.top ? top : 0.0f;
+        const float m = top_key ? top : 0.0f;
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) s += qr_exp(f[i] - m);
-        double d = (double)s;
-        for (int off = 32; off > 0; off >>= 1) d += __shfl_xor(d, off);
-        if (lane == 0) wave_sum[wave] = d;
+        const double d = wave_sum((double)s);
+        if (lane == 0) sums[wave] = d;
     }
-    auto cand = [&](int i) -> QrCand {
-        return f[i] > -INFINITY ? qr_cand(qr_float_key(f[i] + 0.0f), first + ((i / V) * 256 + tid) * V + i % V) : 0ull;
-    };
-    // what passes the bound goes to the list
-    int n_pass = 0;
-    bool in[PER];
+    const unsigned T_key = bound_of(g, top_key, a.K, a.K + a.K / 4);
+    const float least = T_key > 0x00800000u ? qr_key_float(T_key) : -FLT_MAX;   // (keys up to there are those of -inf and below)
+    auto cand = [&](int i) { return qr_cand(qr_float_key(f[i] + 0.0f), first + ((i / V) * NT + tid) * V + i % V); };
+    if (largest >= least) {
+        int n_pass = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        in[i] = f[i] > -INFINITY && bound.passes(qr_float_key(f[i] + 0.0f));
-        n_pass += in[i] ? 1 : 0;
-    }
-    if (n_pass) {
+        for (int i = 0; i < PER; ++i) n_pass += f[i] >= least ? 1 : 0;
         int pos = atomicAdd(&n_list, n_pass);
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (in[i] && pos < LIST) list[pos++] = cand(i);
+            if (f[i] >= least && pos < LIST) list[pos++] = cand(i);
     }
     __syncthreads();
-    if (n_list <= LIST) {
-        qr_rank(list, n_list, a.K, tid, best);
+    const int M = n_list;
+    if (M <= LIST) {
+        if (tid < 256) qr_rank(list, M, a.K, tid, best);
     } else {   // many equal logits: rank by rank over what the threads hold
         QrCand last = ~0ull;
         for (int r = 0; r < a.K; ++r) {
             QrCand mine = 0;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const QrCand c = cand(i);
+                const QrCand c = f[i] > -INFINITY ? cand(i) : 0ull;
                 if (c < last && c > mine) mine = c;
             }
             for (int off = 32; off > 0; off >>= 1) {
@@ -123,7 +283,7 @@ __global__ __launch_bounds__(256) void select_parts_kernel(const QrSelectArgs a)
             }
             if (lane == 0) wave_best[wave] = mine;
             __syncthreads();
-            for (int w = 0; w < 4; ++w) mine = wave_best[w] > mine ? wave_best[w] : mine;
+            for (int w = 0; w < NW; ++w) mine = wave_best[w] > mine ? wave_best[w] : mine;
             __syncthreads();
             if (tid == 0) best[r] = mine;
             last = mine;   // 0: nothing is smaller, the ranks that follow stay empty
@@ -132,147 +292,185 @@ __global__ __launch_bounds__(256) void select_parts_kernel(const QrSelectArgs a)
     __syncthreads();
     const int64_t part = row * a.n_parts + blockIdx.x;
     if (tid < a.K) a.cands[part * a.K + tid] = best[tid];
-    if (tid == 0) a.heads[part] = {top, 0.0f, a.log_softmax ? wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3] : 0.0};
+    if (tid == 0) {
+        double sum = 0.0;
+        if (a.log_softmax)
+            for (int w = 0; w < NW; ++w) sum += sums[w];
+        a.heads[part] = {top, 0.0f, sum};
+    }
 }
 
-// Values of the whole beam's candidates as words.
-__device__ __forceinline__ unsigned long long order_of(double v)   // larger double <=> larger word; 0 for what is never taken
-{
-    if (!(v > -INFINITY)) return 0ull;
-    const unsigned long long u = __double_as_longlong(v + 0.0);
-    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
-}
-__device__ __forceinline__ double value_of(unsigned long long o)
-{
-    return __longlong_as_double((o >> 63) ? (o & 0x7FFFFFFFFFFFFFFFull) : ~o);
-}
+// What turns a row's logits into values: logit - lse = (logit - top) - log(sum of exp(logit - top)).  With the two apart also
+// logits of the type's lowest value, next to which the logarithm vanishes, give what they mean.
+struct QrRowValue {
+    double score, top, log_sum;   // log_sum NaN: no candidates
+    __device__ __forceinline__ QrValue operator()(float logit) const { return value_word(score + (((double)logit - top) - log_sum)); }
+};
 
-// Grid: one workgroup an utterance.
+// Long rows, second launch.  Grid: one workgroup an utterance.
 __global__ __launch_bounds__(256) void select_beam_kernel(const QrSelectArgs a)
 {
-    __shared__ unsigned long long l_val[LIST], l_cand[LIST];   // value; (logit, token)
-    __shared__ int l_hyp[LIST];
+    __shared__ QrPickList list;
+    __shared__ QrRowValue rows[64];
     __shared__ unsigned group_best[256];
-    // logit - lse = (logit - top) - log(sum of exp(logit - top)): with the two apart also logits of the type's lowest value, next
-    // to which the logarithm vanishes, give what they mean.  log_sum NaN: no candidates.
-    __shared__ double row_top[64], log_sum[64];
-    __shared__ int n_list;
-    __shared__ unsigned long long r_val[4], r_cand[4];
-    __shared__ int r_hyp[4];
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int64_t row0 = (int64_t)b * a.W;
     const int per = a.n_parts * a.K;
-    if (tid == 0) n_list = 0;
-    if (tid < a.W) {
-        const int64_t row = row0 + tid;
+    if (tid == 0) list.n = 0;
+    // four threads to a row
+    if (tid < 4 * a.W) {
+        const int64_t row = row0 + (tid >> 2);
         double ls = NAN;
         float top = -INFINITY;
-        if (takes_part(a, row)) {
-            const QrPartHead *h = a.heads + row * a.n_parts;
+        if (reads_logits(a, row)) {
             ls = 0.0;
             if (a.log_softmax) {
-                for (int i = 0; i < a.n_parts; ++i) top = fmaxf(top, h[i].top);
-                for (int i = 0; i < a.n_parts; ++i) ls += h[i].sum * exp((double)h[i].top - (double)top);   // (of -inf alone: NaN)
-                ls = log(ls);
+                const QrPartHead *h = a.heads + row * a.n_parts;
+                for (int i = tid & 3; i < a.n_parts; i += 4) top = fmaxf(top, h[i].top);
+                top = fmaxf(top, __shfl_xor(top, 1));
+                top = fmaxf(top, __shfl_xor(top, 2));
+                for (int i = tid & 3; i < a.n_parts; i += 4) ls += h[i].top > -INFINITY ? h[i].sum * (double)qr_exp(h[i].top - top) : h[i].sum;
+                ls += __shfl_xor(ls, 1);
+                ls += __shfl_xor(ls, 2);
+                ls = top > -INFINITY ? log(ls) : NAN;
             }
         }
-        row_top[tid] = a.log_softmax ? (double)top : 0.0;
-        log_sum[tid] = ls;
+        if ((tid & 3) == 0) rows[tid >> 2] = {(double)a.score[row], a.log_softmax ? (double)top : 0.0, ls};
     }
     __syncthreads();
-    auto value = [&](int w, QrCand c) -> double {
-        return c == 0 ? -INFINITY : (double)a.score[row0 + w] + (((double)qr_cand_value(c) - row_top[w]) - log_sum[w]);
-    };
-    // every candidate of the beam: visit(value order, (logit, token), hypothesis)
     auto each = [&](auto &&visit) {
         for (int i = tid; i < a.W * per; i += 256) {
             const int w = i / per;
-            if (log_sum[w] == log_sum[w]) {
+            const QrRowValue row = rows[w];
+            if (row.log_sum == row.log_sum) {
                 const QrCand c = a.cands[row0 * per + i];
-                const unsigned long long o = order_of(value(w, c));
-                if (o) visit(o, c, w);
+                const QrPick p = {c ? row(qr_cand_value(c)) : 0ull, c, w};
+                if (p.v) visit(p);
             }
         }
-        if (a.finished && tid < a.W && a.finished[row0 + tid]) {
-            const unsigned long long o = order_of((double)a.score[row0 + tid]);
-            if (o) visit(o, qr_cand(1u, a.end_token), tid);
+        if (tid < a.W && is_finished(a, row0 + tid)) {
+            const QrPick p = {value_word((double)a.score[row0 + tid]), qr_cand(1u, a.end_token), tid};
+            if (p.v) visit(p);
         }
     };
     unsigned top = 0u;
-    each([&](unsigned long long o, QrCand, int) { const unsigned k = (unsigned)(o >> 32); top = k > top ? k : top; });
+    each([&](const QrPick &p) { top = (unsigned)(p.v >> 32) > top ? (unsigned)(p.v >> 32) : top; });
     group_best[tid] = top;
     __syncthreads();
-    // the K-th largest of the 256 threads' best is a bound from below of the K-th best (upper 32 bits of the order)
-    unsigned g[4], T = 0u;
+    unsigned g[4], most = 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g[i] = group_best[i * 64 + lane];
-    for (int bit = 31; bit >= 0; --bit) {
-        const unsigned trial = T | (1u << bit);
-        int cnt = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) cnt += (int)__popcll(__ballot(g[i] >= trial));
-        if (cnt >= a.K) T = trial;
-        if (cnt == a.K) break;
+    for (int i = 0; i < 4; ++i) {
+        g[i] = group_best[i * 64 + lane];
+        most = g[i] > most ? g[i] : most;
     }
-    each([&](unsigned long long o, QrCand c, int w) {
-        if ((unsigned)(o >> 32) >= T) {
-            const int at = atomicAdd(&n_list, 1);
-            if (at < LIST) { l_val[at] = o; l_cand[at] = c; l_hyp[at] = w; }
-        }
-    });
-    __syncthreads();
-    const int64_t out0 = (int64_t)b * a.K;
-    auto put = [&](int r, unsigned long long o, QrCand c, int w) {
-        a.parent_out[out0 + r] = o ? w : -1;
-        a.token_out[out0 + r] = o ? qr_cand_index(c) : -1;
-        a.score_out[out0 + r] = o ? (float)value_of(o) : -INFINITY;
-        if (a.finished_out) a.finished_out[out0 + r] = o && ((a.finished && a.finished[row0 + w]) || qr_cand_index(c) == a.end_token) ? 1 : 0;
-    };
-    auto better = [](unsigned long long o, QrCand c, int w, unsigned long long o2, QrCand c2, int w2) {
-        return o != o2 ? o > o2 : (w != w2 ? w < w2 : c > c2);
-    };
-    if (n_list <= LIST) {
-        const int M = n_list;
-        for (int i = tid; i < M; i += 256) {
-            const unsigned long long o = l_val[i], c = l_cand[i];
-            const int w = l_hyp[i];
-            int rank = 0;
-            for (int j = 0; j < M; ++j) rank += better(l_val[j], l_cand[j], l_hyp[j], o, c, w) ? 1 : 0;
-            if (rank < a.K) put(rank, o, c, w);
-        }
-        for (int r = M + tid; r < a.K; r += 256) put(r, 0ull, 0ull, 0);
-        return;
-    }
-    // many equal values: rank by rank
-    unsigned long long last_o = ~0ull, last_c = ~0ull;
-    int last_w = -1;
-    for (int r = 0; r < a.K; ++r) {
-        unsigned long long bo = 0, bc = 0;
-        int bw = 0x7fffffff;
-        each([&](unsigned long long o, QrCand c, int w) {
-            if (better(last_o, last_c, last_w, o, c, w) && better(o, c, w, bo, bc, bw)) { bo = o; bc = c; bw = w; }
+    const unsigned T = bound_of(g, qr_wave_reduce_u32<true>(most), a.K, a.K + a.K / 4);
+    if (top >= T)
+        each([&](const QrPick &p) {
+            if ((unsigned)(p.v >> 32) >= T) push(list, p);
         });
-        for (int off = 32; off > 0; off >>= 1) {
-            const unsigned long long o = __shfl_xor(bo, off), c = __shfl_xor(bc, off);
-            const int w = __shfl_xor(bw, off);
-            if (better(o, c, w, bo, bc, bw)) { bo = o; bc = c; bw = w; }
-        }
-        if (lane == 0) { r_val[wave] = bo; r_cand[wave] = bc; r_hyp[wave] = bw; }
-        __syncthreads();
-        for (int i = 0; i < 4; ++i)
-            if (better(r_val[i], r_cand[i], r_hyp[i], bo, bc, bw)) { bo = r_val[i]; bc = r_cand[i]; bw = r_hyp[i]; }
-        __syncthreads();
-        if (tid == 0) put(r, bo, bc, bw);
-        last_o = bo;
-        last_c = bc;
-        last_w = bw;
-    }
+    __syncthreads();
+    write_ranks<256>(a, b, list, each);
 }
 
-// How a row is cut: stretches of at most 8192 logits, shorter ones where there are few rows.
+// Short rows: one launch, one workgroup of 16 waves an utterance, wave i takes the rows i, i + 16, ...; a row has at most 64 * PER
+// logits.
+template <class T, int NV>
+__global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a)
+{
+    constexpr int V = QrVec<T>::N, PER = NV * V;
+    __shared__ QrPickList list;
+    __shared__ QrRowValue rows[64];
+    __shared__ unsigned group_best[256];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row0 = (int64_t)b * a.W;
+    const T *x = (const T *)a.logits + row0 * a.ld;
+    if (tid == 0) list.n = 0;
+    float f[PER];
+    unsigned best = 0u;
+    for (int w = wave; w < a.W; w += 16) {   // uniform in a wave
+        QrRowValue row = {(double)a.score[row0 + w], 0.0, NAN};
+        if (reads_logits(a, row0 + w)) {
+            load_logits<T, NV>(x + w * a.ld, a.V, lane, 64, f);
+            float largest = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) largest = fmaxf(largest, f[i]);
+            row.log_sum = 0.0;
+            if (a.log_softmax) {
+                const unsigned k = qr_wave_reduce_u32<true>(logit_key(largest));
+                const float top = k ? qr_key_float(k) : -INFINITY;
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) s += qr_exp(f[i] - top);   // (of -inf alone: NaN)
+                row.top = (double)top;
+                row.log_sum = log(wave_sum((double)s));
+            }
+            if (largest > -INFINITY) {
+                const unsigned k = (unsigned)(row(largest) >> 32);
+                best = k > best ? k : best;
+            }
+        } else if (is_finished(a, row0 + w) && lane == 0) {
+            const unsigned k = (unsigned)(value_word(row.score) >> 32);
+            best = k > best ? k : best;
+        }
+        if (lane == 0) rows[w] = row;
+    }
+    if (a.W <= 4) {   // groups: lanes of 4 waves, or quads of 16
+        if (wave < 4) group_best[tid] = best;
+    } else {
+        best = quad_max(best);
+        if ((lane & 3) == 0) group_best[tid >> 2] = best;
+    }
+    __syncthreads();
+    unsigned g[4], most = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        g[i] = group_best[i * 64 + lane];
+        most = g[i] > most ? g[i] : most;
+    }
+    const unsigned Tk = bound_of(g, qr_wave_reduce_u32<true>(most), a.K, a.K + a.K / 4);
+    for (int w = wave; w < a.W; w += 16) {
+        const QrRowValue row = rows[w];
+        if (row.log_sum == row.log_sum) {
+            if (a.W > 16) load_logits<T, NV>(x + w * a.ld, a.V, lane, 64, f);
+            // the bound as a logit of this row, a little lower than it is; where it has none every logit passes
+            const double at = Tk ? ((word_value((QrValue)Tk << 32) - row.score) + row.log_sum) + row.top : -INFINITY;
+            const float least = at == at ? fmaxf((float)(at - 1e-6 * fabs(at)), -FLT_MAX) : -FLT_MAX;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (f[i] >= least) {
+                    const QrPick p = {row(f[i]), qr_cand(qr_float_key(f[i] + 0.0f), ((i / V) * 64 + lane) * V + i % V), w};
+                    if ((unsigned)(p.v >> 32) >= Tk && p.v) push(list, p);
+                }
+        } else if (lane == 0 && is_finished(a, row0 + w)) {
+            const QrPick p = {value_word(row.score), qr_cand(1u, a.end_token), w};
+            if ((unsigned)(p.v >> 32) >= Tk && p.v) push(list, p);
+        }
+    }
+    __syncthreads();
+    write_ranks<1024>(a, b, list, [&](auto &&visit) {
+        for (int w = wave; w < a.W; w += 16) {
+            const QrRowValue row = rows[w];
+            if (row.log_sum == row.log_sum) {
+                for (int c = lane; c < a.V; c += 64) {
+                    const float l = (float)x[w * a.ld + c];
+                    const QrPick p = {row(l), qr_cand(qr_float_key(l + 0.0f), c), w};
+                    if (p.v) visit(p);
+                }
+            } else if (lane == 0 && is_finished(a, row0 + w)) {
+                const QrPick p = {value_word(row.score), qr_cand(1u, a.end_token), w};
+                if (p.v) visit(p);
+            }
+        }
+    });
+}
+
+// How rows are cut: whole up to SHORT logits (one launch); stretches of up to 8192 logits for 256 threads, or of 32768 for 1024 where
+// rows are long and fill the device.
+constexpr int SHORT = 2048;
+bool long_stretches(int64_t rows, int V) { return rows >= 256 && V > 16384; }
 void plan_select(int64_t rows, int V, int &n_parts, int &part)
 {
-    const int len = rows * ((V + 8191) / 8192) >= 256 ? 8192 : 2048;
+    const int len = long_stretches(rows, V) ? 32768 : 8192;
     n_parts = (V + len - 1) / len;
     part = qr_round_up((V + n_parts - 1) / n_parts, 8);
     n_parts = (V + part - 1) / part;
@@ -280,19 +478,31 @@ void plan_select(int64_t rows, int V, int &n_parts, int &part)
 
 bool select_sizes_ok(int32_t B, int32_t W, int32_t V, int32_t K)
 {
-    return B >= 0 && W > 0 && V > 0 && K > 0 && W <= 64 && K <= MAX_OUT && (int64_t)W * V <= INT32_MAX && (int64_t)B * W <= INT32_MAX;
+    return B >= 0 && W > 0 && V > 0 && K > 0 && W <= 64 && K <= MAX_OUT && (int64_t)W * V <= INT32_MAX && V <= 1 << 30 && (int64_t)B * W <= INT32_MAX;
 }
 
 size_t heads_bytes(int64_t rows, int n_parts) { return ((size_t)rows * n_parts * sizeof(QrPartHead) + 255) / 256 * 256; }
 
 template <class T>
-void launch_parts(const QrSelectArgs &a, hipStream_t st)
+void launch_select(QrSelectArgs &a, void *workspace, hipStream_t st)
 {
-    const int64_t rows = (int64_t)a.B * a.W;
-    const dim3 grid(a.n_parts, (unsigned)(rows < 32768 ? rows : 32768), (unsigned)((rows + 32767) / 32768));
     constexpr int V = QrVec<T>::N;
-    if (a.part <= 2048) select_parts_kernel<T, 2048 / 256 / V><<<grid, 256, 0, st>>>(a);
-    else select_parts_kernel<T, 8192 / 256 / V><<<grid, 256, 0, st>>>(a);
+    if (a.V <= 512) {
+        select_short_kernel<T, 512 / 64 / V><<<a.B, 1024, 0, st>>>(a);
+        return;
+    }
+    if (a.V <= SHORT) {
+        select_short_kernel<T, SHORT / 64 / V><<<a.B, 1024, 0, st>>>(a);
+        return;
+    }
+    const int64_t rows = (int64_t)a.B * a.W;
+    plan_select(rows, a.V, a.n_parts, a.part);
+    a.heads = (QrPartHead *)workspace;
+    a.cands = (QrCand *)((char *)workspace + heads_bytes(rows, a.n_parts));
+    const dim3 grid(a.n_parts, (unsigned)(rows < 32768 ? rows : 32768), (unsigned)((rows + 32767) / 32768));
+    if (!long_stretches(rows, a.V)) select_parts_kernel<T, 8192 / 256 / V, 256><<<grid, 256, 0, st>>>(a);
+    else select_parts_kernel<T, 32768 / 1024 / V, 1024><<<grid, 1024, 0, st>>>(a);
+    select_beam_kernel<<<a.B, 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -300,6 +510,7 @@ void launch_parts(const QrSelectArgs &a, hipStream_t st)
 extern "C" size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, int32_t n_out)
 {
     if (!select_sizes_ok(B, W, V, n_out)) return 0;
+    if (V <= SHORT) return 256;   // (not used)
     int n_parts, part;
     const int64_t rows = (int64_t)(B > 0 ? B : 1) * W;
     plan_select(rows, V, n_parts, part);
@@ -324,14 +535,8 @@ extern "C" qrnnt_status qrnnt_beam_select(const float *score, const void *logits
     a.score = score;  a.logits = logits;  a.ld = ld;  a.finished = finished;  a.log_softmax = log_softmax;  a.end_token = end_token;
     a.B = B;  a.W = W;  a.V = V;  a.K = n_out;
     a.parent_out = parent_out;  a.token_out = token_out;  a.score_out = score_out;  a.finished_out = finished_out;
-    const int64_t rows = (int64_t)B * W;
-    plan_select(rows, V, a.n_parts, a.part);
-    a.heads = (QrPartHead *)workspace;
-    a.cands = (QrCand *)((char *)workspace + heads_bytes(rows, a.n_parts));
-    hipStream_t st = (hipStream_t)stream;
-    if (dtype == QRNNT_F32) launch_parts<float>(a, st);
-    else if (dtype == QRNNT_F16) launch_parts<_Float16>(a, st);
-    else launch_parts<__bf16>(a, st);
-    select_beam_kernel<<<B, 256, 0, st>>>(a);
+    if (dtype == QRNNT_F32) launch_select<float>(a, workspace, (hipStream_t)stream);
+    else if (dtype == QRNNT_F16) launch_select<_Float16>(a, workspace, (hipStream_t)stream);
+    else launch_select<__bf16>(a, workspace, (hipStream_t)stream);
     return qr_launch_status();
 }

@@ -278,57 +278,74 @@ def _dtype(t: torch.dtype) -> int:
 
 def _here(*tensors):
     """The tensors a call works on have to be on the current device, on whose current stream it runs."""
-    current = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else -1
     for t in tensors:
-        if t is not None and t.get_device() != current:
+        if t is not None and (not t.is_cuda or t.get_device() != torch._C._cuda_getDevice()):
             raise ValueError(f"expected a tensor on the current GPU, got one on {t.device}")
-        if t is not None and t.get_device() < 0:
-            raise ValueError("expected a tensor on the GPU")
 
 
 def _matrix(t: torch.Tensor, dtype, rows: int, cols: int):
     """(address, pitch) of a [rows, cols] matrix whose rows may lie apart."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError(f"expected a matrix of {rows} x {cols}, got {tuple(t.shape)}")
-    if cols > 1 and t.stride(1) != 1:
+    pitch, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("the elements of a row must be contiguous")
-    pitch = t.stride(0) if rows > 1 else max(t.stride(0), cols)
     if pitch < cols:
-        raise ValueError("rows must not overlap")
+        if rows > 1:
+            raise ValueError("rows must not overlap")
+        pitch = cols
     return t.data_ptr(), pitch
 
 
 def _vector(t: Optional[torch.Tensor], dtype, n: int):
     if t is None:
         return None
+    if t.dtype is not dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
     if t.numel() != n:
         raise ValueError(f"expected {n} elements, got {t.numel()}")
-    return _addr(t, dtype)
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_of(x: torch.Tensor):
+    """(rows, columns, dtype, address, pitch) of the matrix that a call is about."""
+    if not x.is_cuda or x.get_device() != torch._C._cuda_getDevice():
+        _here(x)
+    if x.dim() != 2:
+        raise ValueError(f"expected a matrix, got {tuple(x.shape)}")
+    rows, cols = x.shape
+    address, pitch = _matrix(x, x.dtype, rows, cols)
+    return rows, cols, _DTYPES.get(x.dtype) if x.dtype in _DTYPES else _dtype(x.dtype), address, pitch
 
 
 def _code_outputs(rows: int, cols: int, codes, scale, device):
-    ld = (cols + 15) // 16 * 16   # qrnnt_act_pitch
+    """(codes, scale, address and pitch of the codes, address of the scales), made where they are not given."""
+    width = (cols + 15) & ~15   # qrnnt_act_pitch
     if codes is None:
-        codes = torch.empty((rows, ld), dtype=torch.int8, device=device)
+        codes = torch.empty((rows, width), dtype=torch.int8, device=device)
+        address, pitch = codes.data_ptr(), width
+    else:
+        _here(codes)
+        address, pitch = _matrix(codes, torch.int8, rows, codes.shape[-1])
+        if codes.shape[1] < width:
+            raise ValueError(f"codes have {codes.shape[1]} columns, rows of {cols} take {width}")
     if scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=device)
-    _here(codes, scale)
-    addr, ld = _matrix(codes, torch.int8, rows, codes.shape[1] if codes.dim() == 2 else ld)
-    if codes.shape[1] < (cols + 15) // 16 * 16:
-        raise ValueError(f"codes have {codes.shape[1]} columns, rows of {cols} take {(cols + 15) // 16 * 16}")
-    return codes, scale, addr, ld
+        return codes, scale, address, pitch, scale.data_ptr()
+    _here(scale)
+    return codes, scale, address, pitch, _vector(scale, torch.float32, rows)
 
 
 def quantize_tokens(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """[rows, cols] of float32, float16 or bfloat16 (rows may lie apart) -> int8 codes [rows, act_pitch(cols)] with zeros behind
     the columns, and the scale of each row: 8 bits over the row's own range (qrnnt_quantize_tokens)."""
-    _here(x)
-    rows, cols = x.shape
-    px, ld = _matrix(x, x.dtype, rows, cols)
-    codes, scale, pq, ld_q = _code_outputs(rows, cols, codes, scale, x.device)
-    _call("qrnnt_quantize_tokens", px, _dtype(x.dtype), rows, cols, ld, pq, ld_q, _vector(scale, torch.float32, rows), _stream_handle())
+    rows, cols, dtype, px, ld = _rows_of(x)
+    codes, scale, pq, ld_q, ps = _code_outputs(rows, cols, codes, scale, x.device)
+    _call("qrnnt_quantize_tokens", px, dtype, rows, cols, ld, pq, ld_q, ps, _stream_handle())
     return codes, scale
 
 
@@ -337,21 +354,20 @@ def rms_norm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: 
                    codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """Residual sum, root-mean-square norm and 8-bit quantizer with a scale for each row (qrnnt_rms_norm_quant): returns
     (codes, scale, x + residual, or x itself without a residual).  sum_out may be x or residual."""
-    _here(x, weight, residual, sum_out)
-    rows, cols = x.shape
-    px, ld = _matrix(x, x.dtype, rows, cols)
-    pr = ps = None
+    rows, cols, dtype, px, ld = _rows_of(x)
+    _here(weight, residual, sum_out)
+    pr = psum = None
     ld_r = ld_s = cols
     if residual is not None:
         pr, ld_r = _matrix(residual, x.dtype, rows, cols)
         if sum_out is None:
             sum_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-        ps, ld_s = _matrix(sum_out, x.dtype, rows, cols)
+        psum, ld_s = _matrix(sum_out, x.dtype, rows, cols)
     elif sum_out is not None:
         raise ValueError("sum_out needs a residual")
-    codes, scale, pq, ld_q = _code_outputs(rows, cols, codes, scale, x.device)
-    _call("qrnnt_rms_norm_quant", px, pr, _vector(weight, x.dtype, cols), _dtype(x.dtype), rows, cols, ld, ld_r, eps, ps, ld_s,
-          pq, ld_q, _vector(scale, torch.float32, rows), _stream_handle())
+    codes, scale, pq, ld_q, ps = _code_outputs(rows, cols, codes, scale, x.device)
+    _call("qrnnt_rms_norm_quant", px, pr, _vector(weight, x.dtype, cols), dtype, rows, cols, ld, ld_r, eps, psum, ld_s, pq, ld_q, ps,
+          _stream_handle())
     return codes, scale, x if residual is None else sum_out
 
 
@@ -365,21 +381,26 @@ def linear_tokens(w: QMat, codes: torch.Tensor, scale: torch.Tensor, bias: Optio
                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """8-bit linear layer of rows with a scale each, as quantize_tokens and rms_norm_quant return them: w from
     pack_int8(..., LAYOUT_TILED), codes [M, act_pitch(cols)] (qrnnt_linear_tokens).  out may be a matrix whose rows lie apart."""
-    _here(codes, scale, bias, out, workspace, w.packed)
+    _here(codes, scale, bias, workspace, w.packed, w.row_scale)
     M = codes.shape[0]
-    pa, ld_a = _matrix(codes, torch.int8, M, codes.shape[1])
-    if codes.shape[1] < act_pitch(w.cols):
-        raise ValueError(f"codes have {codes.shape[1]} columns, a layer of {w.cols} reads {act_pitch(w.cols)}")
+    pa, ld_a = _matrix(codes, torch.int8, M, codes.shape[-1])
+    if codes.shape[1] < (w.cols + 15) & ~15:
+        raise ValueError(f"codes have {codes.shape[1]} columns, a layer of {w.cols} reads {(w.cols + 15) & ~15}")
     if out is None:
+        kind = _dtype(dtype)
         out = torch.empty((M, w.rows), dtype=dtype, device=codes.device)
-    py, ld_y = _matrix(out, out.dtype, M, w.rows)
+        py, ld_y = out.data_ptr(), w.rows
+    else:
+        _here(out)
+        kind = _dtype(out.dtype)
+        py, ld_y = _matrix(out, out.dtype, M, w.rows)
     cw = w.c()
     if workspace is None:
-        need = int(load().qrnnt_linear_tokens_workspace(C.byref(cw), M))
+        need = load().qrnnt_linear_tokens_workspace(C.byref(cw), M)
         workspace = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
-    n_ws = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    n_ws = 0 if workspace is None else workspace.nbytes
     _call("qrnnt_linear_tokens", C.byref(cw), _vector(bias, torch.float32, w.rows), pa, ld_a, _vector(scale, torch.float32, M), M,
-          py, _dtype(out.dtype), ld_y, _addr(workspace) if n_ws else None, n_ws, _stream_handle())
+          py, kind, ld_y, _addr(workspace) if n_ws else None, n_ws, _stream_handle())
     return out
 
 
@@ -606,30 +627,32 @@ def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] 
     bfloat16; rows may lie apart): (parent, token, score, finished), each [B, n_out] (qrnnt_beam_select).  finished
     [B, W] (bool or uint8): hypotheses that keep their score and repeat end_token; needs end_token.  The last result is None
     without end_token."""
-    _here(score, logits, finished, workspace)
+    rows, V, dtype, pl, ld = _rows_of(logits)
+    _here(score, finished, workspace)
     B, W = score.shape
-    V = logits.shape[-1]
+    if rows != B * W:
+        raise ValueError(f"expected logits of {B * W} hypotheses, got {rows}")
     K = W if n_out is None else n_out
     dev = score.device
-    pl, ld = _matrix(logits, logits.dtype, B * W, V)
+    pf = None
     if finished is not None:
         if end_token is None:
             raise ValueError("finished hypotheses need an end_token")
-        if finished.dtype not in (torch.uint8, torch.bool):
+        if finished.dtype is not torch.bool and finished.dtype is not torch.uint8:
             raise TypeError(f"expected uint8 or bool, got {finished.dtype}")
-    par = torch.empty((B, K), dtype=torch.int32, device=dev)
-    tok = torch.empty((B, K), dtype=torch.int32, device=dev)
-    ns = torch.empty((B, K), dtype=torch.float32, device=dev)
-    done = None if end_token is None else torch.empty((B, K), dtype=torch.bool, device=dev)
+        pf = _vector(finished, finished.dtype, rows)
     if workspace is None:
         need = beam_select_workspace(B, W, V, K)
         if need == 0:
             _check(7, "qrnnt_beam_select_workspace")
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _call("qrnnt_beam_select", _vector(score, torch.float32, B * W), pl, _dtype(logits.dtype), ld, 1 if log_softmax else 0,
-          None if finished is None else _vector(finished, finished.dtype, B * W), -1 if end_token is None else end_token,
-          B, W, V, K, par.data_ptr(), tok.data_ptr(), ns.data_ptr(), None if done is None else done.data_ptr(),
-          _addr(workspace), workspace.numel() * workspace.element_size(), _stream_handle())
+    par = torch.empty((B, K), dtype=torch.int32, device=dev)
+    tok = torch.empty((B, K), dtype=torch.int32, device=dev)
+    ns = torch.empty((B, K), dtype=torch.float32, device=dev)
+    done = None if end_token is None else torch.empty((B, K), dtype=torch.bool, device=dev)
+    _call("qrnnt_beam_select", _vector(score, torch.float32, rows), pl, dtype, ld, 1 if log_softmax else 0,
+          pf, -1 if end_token is None else end_token, B, W, V, K, par.data_ptr(), tok.data_ptr(), ns.data_ptr(),
+          None if done is None else done.data_ptr(), _addr(workspace), workspace.nbytes, _stream_handle())
     return par, tok, ns, done
 
 
@@ -654,7 +677,7 @@ class StateGroup:
         if not 1 <= self.n <= MAX_STATES:
             raise ValueError(f"1 to {MAX_STATES} states, got {self.n}")
         self.arr = (CStateRows * self.n)()
-        self.device = pairs[0][0].device
+        self.device = pairs[0][0].get_device()
         for i, (src, dst) in enumerate(pairs):
             _here(src, dst)
             if src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
@@ -679,7 +702,7 @@ class StateGroup:
     def reorder(self, parent: torch.Tensor):
         """Row b * W_out + j of every destination becomes row b * W + parent[b, j] of its source; parent [B, W_out] int32."""
         _here(parent)
-        if parent.device != self.device:
+        if parent.get_device() != self.device:
             raise ValueError("parent is on another device than the states")
         _call("qrnnt_reorder_states", self.arr, self.n, _vector(parent, torch.int32, self.B * self.W_out), self.B, self.W, self.W_out,
               _stream_handle())
