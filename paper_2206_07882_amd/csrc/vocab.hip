@@ -158,26 +158,70 @@ __device__ __forceinline__ void write_ranks(const QrSelectArgs &a, int b, QrPick
     }
 }
 
-// This lane's NV vectors of n logits: vector v of thread t of `threads` starts at element (v * threads + t) * V, wherever the
-// row begins (sums have to come out the same for the same row); -inf behind the end.
+// A thread's NV vectors of n logits: vector v of thread t of `threads` starts at element (v * threads + t) * V, wherever the row begins
+// in memory (sums have to come out the same for the same row); -inf behind the end.  Kept in their own type: as fp32 16-bit logits
+// would take twice the registers.
 template <class T, int NV>
-__device__ __forceinline__ void load_logits(const T *x, int n, int t, int threads, float (&f)[NV * QrVec<T>::N])
-{
-    constexpr int V = QrVec<T>::N;
+struct QrLogits {
+    static constexpr int V = QrVec<T>::N, PER = NV * V;
+    typename QrVec<T>::type raw[NV];
+    __device__ __forceinline__ void load(const T *x, int n, int t, int threads)
+    {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        float u[V];
-        const int c = (v * threads + t) * V;
-        if (c + V <= n) {
-            qr_load_vec(x + c, u);
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * threads + t) * V;
+            if (c + V <= n) {
+                raw[v] = *(const typename QrVec<T>::any *)(x + c);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) raw[v][i] = c + i < n ? x[c + i] : (T)-INFINITY;
+            }
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return (float)raw[i / V][i % V]; }
+    // Before a further pass: what the last one made of the logits is not kept.
+    __device__ __forceinline__ void anew()
+    {
+        if (sizeof(T) == 2)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) asm volatile("" : "+v"(raw[v]));
+    }
+    __device__ __forceinline__ float largest() const   // (NaN is passed over)
+    {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) m = fmaxf(m, (*this)[i]);
+        return m;
+    }
+    __device__ __forceinline__ float sum_exp(float top) const
+    {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) s += qr_exp((*this)[i] - top);
+        return s;
+    }
+    // take(logit, i) for those that are not below `least`.  A thread that has any most often has one, its largest: that one is found
+    // without a branch for each.
+    template <class Take>
+    __device__ __forceinline__ void hits(float largest, float least, Take &&take) const
+    {
+        if (!(largest >= least)) return;
+        int n = 0, at = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const bool hit = (*this)[i] >= least;
+            n += hit ? 1 : 0;
+            at = hit ? i : at;
+        }
+        if (n == 1) {
+            take(largest, at);
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) u[i] = c + i < n ? (float)x[c + i] : -INFINITY;
+            for (int i = 0; i < PER; ++i)
+                if ((*this)[i] >= least) take((*this)[i], i);
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[v * V + i] = u[i];
     }
-}
+};
 __device__ __forceinline__ unsigned logit_key(float f) { return f > -INFINITY ? qr_float_key(f + 0.0f) : 0u; }   // (0 for NaN, too)
 // Sum over the wave, on the DPP path (row scans, then the two cross-row broadcasts of gfx9), in all lanes.
 __device__ __forceinline__ double wave_sum(double d)
@@ -209,12 +253,14 @@ __device__ __forceinline__ unsigned quad_max(unsigned v)
     return o > v ? o : v;
 }
 
-// Long rows, first launch.  Grid: x = stretch, y (and z) = row; NT = 256 or 1024 threads with NV vectors each.
+// Long rows, first launch.  Grid: x = stretch, y (and z) = row; NT = 256 or 512 threads with NV vectors each.
+// Bound by the chain of its steps and the exponentials: of 28 us for 64 x 16 x 32000 bf16 logits reading them and their maximum take 10,
+// sums 4, bound 2, gathering and ranks 5, the second launch 5; other numbers of waves and logits to one change little.
 template <class T, int NV, int NT>
-__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 5) void select_parts_kernel(const QrSelectArgs a)
+__global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs a)
 {
     constexpr int V = QrVec<T>::N, PER = NV * V, NW = NT / 64;
-    __shared__ QrCand list[LIST], best[MAX_OUT], wave_best[NW];
+    __shared__ QrCand list[LIST], wave_best[NW];
     __shared__ unsigned group_best[256];
     __shared__ double sums[NW];
     __shared__ int n_list;
@@ -223,17 +269,14 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 5) void select_parts_kernel(co
     if (row >= (int64_t)a.B * a.W || !reads_logits(a, row)) return;   // uniform; the second launch does not ask for it either
     const int first = blockIdx.x * a.part, n = a.V - first < a.part ? a.V - first : a.part;
     if (tid == 0) n_list = 0;
-    if (tid < MAX_OUT) best[tid] = 0;
-    float f[PER];
-    load_logits<T, NV>((const T *)a.logits + row * a.ld + first, n, tid, NT, f);
-    float largest = -INFINITY;   // (NaN is passed over here and found again in the sum)
-#pragma unroll
-    for (int i = 0; i < PER; ++i) largest = fmaxf(largest, f[i]);
+    QrLogits<T, NV> f;
+    f.load((const T *)a.logits + row * a.ld + first, n, tid, NT);
+    const float largest = f.largest();   // (NaN is found in the sum)
     if (NT == 256) {
         group_best[tid] = logit_key(largest);
     } else {
-        const unsigned k = quad_max(logit_key(largest));
-        if ((tid & 3) == 0) group_best[tid >> 2] = k;
+        const unsigned k = logit_key(largest), o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)k, 0xB1, 0xf, 0xf, true);   // its neighbour's
+        if ((tid & 1) == 0) group_best[tid >> 1] = o > k ? o : k;
     }
     __syncthreads();
     unsigned g[4], top_key = 0u;
@@ -245,58 +288,62 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 5) void select_parts_kernel(co
     top_key = qr_wave_reduce_u32<true>(top_key);
     const float top = top_key ? qr_key_float(top_key) : -INFINITY;
     if (a.log_softmax) {
-        const float m = top_key ? top : 0.0f;
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) s += qr_exp(f[i] - m);
-        const double d = wave_sum((double)s);
+        f.anew();
+        const double d = wave_sum((double)f.sum_exp(top_key ? top : 0.0f));
         if (lane == 0) sums[wave] = d;
     }
     const unsigned T_key = bound_of(g, top_key, a.K, a.K + a.K / 4);
     const float least = T_key > 0x00800000u ? qr_key_float(T_key) : -FLT_MAX;   // (keys up to there are those of -inf and below)
-    auto cand = [&](int i) { return qr_cand(qr_float_key(f[i] + 0.0f), first + ((i / V) * NT + tid) * V + i % V); };
-    if (largest >= least) {
-        int n_pass = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) n_pass += f[i] >= least ? 1 : 0;
-        int pos = atomicAdd(&n_list, n_pass);
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (f[i] >= least && pos < LIST) list[pos++] = cand(i);
-    }
+    auto cand = [&](float l, int i) { return qr_cand(qr_float_key(l + 0.0f), first + ((i / V) * NT + tid) * V + i % V); };
+    f.anew();
+    f.hits(largest, least, [&](float l, int i) {
+        const int at = atomicAdd(&n_list, 1);
+        if (at < LIST) list[at] = cand(l, i);
+    });
     __syncthreads();
     const int M = n_list;
-    if (M <= LIST) {
-        if (tid < 256) qr_rank(list, M, a.K, tid, best);
-    } else {   // many equal logits: rank by rank over what the threads hold
-        QrCand last = ~0ull;
-        for (int r = 0; r < a.K; ++r) {
-            QrCand mine = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const QrCand c = f[i] > -INFINITY ? cand(i) : 0ull;
-                if (c < last && c > mine) mine = c;
-            }
-            for (int off = 32; off > 0; off >>= 1) {
-                const QrCand o = __shfl_xor(mine, off);
-                mine = o > mine ? o : mine;
-            }
-            if (lane == 0) wave_best[wave] = mine;
-            __syncthreads();
-            for (int w = 0; w < NW; ++w) mine = wave_best[w] > mine ? wave_best[w] : mine;
-            __syncthreads();
-            if (tid == 0) best[r] = mine;
-            last = mine;   // 0: nothing is smaller, the ranks that follow stay empty
-        }
-    }
-    __syncthreads();
     const int64_t part = row * a.n_parts + blockIdx.x;
-    if (tid < a.K) a.cands[part * a.K + tid] = best[tid];
+    QrCand *out = a.cands + part * a.K;
     if (tid == 0) {
         double sum = 0.0;
         if (a.log_softmax)
             for (int w = 0; w < NW; ++w) sum += sums[w];
         a.heads[part] = {top, 0.0f, sum};
+    }
+    if (M <= LIST) {   // a candidate's rank is how many are better, four threads counting for each
+        for (int i0 = 0; i0 < M; i0 += NT / 4) {   // uniform
+            const int i = i0 + (tid >> 2);
+            const QrCand mine = list[i < M ? i : 0];
+            int rank = 0;
+#pragma unroll 4
+            for (int j = tid & 3; j < M; j += 4) rank += list[j] > mine ? 1 : 0;
+            rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
+            rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
+            if ((tid & 3) == 0 && i < M && rank < a.K) out[rank] = mine;
+        }
+        if (tid >= M && tid < a.K) out[tid] = 0ull;
+        return;
+    }
+    // many equal logits: rank by rank over what the threads hold
+    QrCand last = ~0ull;
+    f.anew();
+    for (int r = 0; r < a.K; ++r) {
+        QrCand mine = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const QrCand c = f[i] > -INFINITY ? cand(f[i], i) : 0ull;
+            if (c < last && c > mine) mine = c;
+        }
+        for (int off = 32; off > 0; off >>= 1) {
+            const QrCand o = __shfl_xor(mine, off);
+            mine = o > mine ? o : mine;
+        }
+        if (lane == 0) wave_best[wave] = mine;
+        __syncthreads();
+        for (int w = 0; w < NW; ++w) mine = wave_best[w] > mine ? wave_best[w] : mine;
+        __syncthreads();
+        if (tid == 0) out[r] = mine;
+        last = mine;   // 0: nothing is smaller, the ranks that follow stay empty
     }
 }
 
@@ -307,15 +354,25 @@ struct QrRowValue {
     __device__ __forceinline__ QrValue operator()(float logit) const { return value_word(score + (((double)logit - top) - log_sum)); }
 };
 
-// Long rows, second launch.  Grid: one workgroup an utterance.
-__global__ __launch_bounds__(256) void select_beam_kernel(const QrSelectArgs a)
+// Long rows, second launch.  Grid: one workgroup of NT = 256 or 1024 threads an utterance.  HELD: what the lists have in all fits four
+// to a thread, which are fetched at once and kept (otherwise they are read in every pass).
+template <int NT, bool HELD>
+__global__ __launch_bounds__(NT) void select_beam_kernel(const QrSelectArgs a)
 {
     __shared__ QrPickList list;
     __shared__ QrRowValue rows[64];
     __shared__ unsigned group_best[256];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int64_t row0 = (int64_t)b * a.W;
-    const int per = a.n_parts * a.K;
+    const int per = a.n_parts * a.K, total = a.W * per;
+    QrCand held[4];
+    if (HELD) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int i = tid + NT * q;
+            held[q] = a.cands[row0 * per + (i < total ? i : 0)];
+        }
+    }
     if (tid == 0) list.n = 0;
     // four threads to a row
     if (tid < 4 * a.W) {
@@ -338,24 +395,41 @@ __global__ __launch_bounds__(256) void select_beam_kernel(const QrSelectArgs a)
         if ((tid & 3) == 0) rows[tid >> 2] = {(double)a.score[row], a.log_softmax ? (double)top : 0.0, ls};
     }
     __syncthreads();
+    auto pick = [&](int i, QrCand c) -> QrPick {
+        const int w = i / per;
+        const QrRowValue row = rows[w];
+        return {row.log_sum == row.log_sum && c ? row(qr_cand_value(c)) : 0ull, c, w};   // (rows that were not asked for hold anything)
+    };
+    QrPick kept[4];
+    if (HELD) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) kept[q] = tid + NT * q < total ? pick(tid + NT * q, held[q]) : QrPick{0ull, 0ull, 0};
+    }
     auto each = [&](auto &&visit) {
-        for (int i = tid; i < a.W * per; i += 256) {
-            const int w = i / per;
-            const QrRowValue row = rows[w];
-            if (row.log_sum == row.log_sum) {
-                const QrCand c = a.cands[row0 * per + i];
-                const QrPick p = {c ? row(qr_cand_value(c)) : 0ull, c, w};
+        if (HELD) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (kept[q].v) visit(kept[q]);
+        } else {
+            #pragma unroll 4
+            for (int i = tid; i < total; i += NT) {
+                const QrPick p = pick(i, a.cands[row0 * per + i]);
                 if (p.v) visit(p);
             }
         }
-        if (tid < a.W && is_finished(a, row0 + tid)) {
+        if (a.finished && tid < a.W && a.finished[row0 + tid]) {
             const QrPick p = {value_word((double)a.score[row0 + tid]), qr_cand(1u, a.end_token), tid};
             if (p.v) visit(p);
         }
     };
     unsigned top = 0u;
     each([&](const QrPick &p) { top = (unsigned)(p.v >> 32) > top ? (unsigned)(p.v >> 32) : top; });
-    group_best[tid] = top;
+    if (NT == 256) {
+        group_best[tid] = top;
+    } else {
+        const unsigned k = quad_max(top);
+        if ((tid & 3) == 0) group_best[tid >> 2] = k;
+    }
     __syncthreads();
     unsigned g[4], most = 0u;
 #pragma unroll
@@ -369,7 +443,7 @@ __global__ __launch_bounds__(256) void select_beam_kernel(const QrSelectArgs a)
             if ((unsigned)(p.v >> 32) >= T) push(list, p);
         });
     __syncthreads();
-    write_ranks<256>(a, b, list, each);
+    write_ranks<NT>(a, b, list, each);
 }
 
 // Short rows: one launch, one workgroup of 16 waves an utterance, wave i takes the rows i, i + 16, ...; a row has at most 64 * PER
@@ -377,7 +451,7 @@ __global__ __launch_bounds__(256) void select_beam_kernel(const QrSelectArgs a)
 template <class T, int NV>
 __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a)
 {
-    constexpr int V = QrVec<T>::N, PER = NV * V;
+    constexpr int V = QrVec<T>::N;
     __shared__ QrPickList list;
     __shared__ QrRowValue rows[64];
     __shared__ unsigned group_best[256];
@@ -385,24 +459,20 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
     const int64_t row0 = (int64_t)b * a.W;
     const T *x = (const T *)a.logits + row0 * a.ld;
     if (tid == 0) list.n = 0;
-    float f[PER];
+    QrLogits<T, NV> f;
     unsigned best = 0u;
     for (int w = wave; w < a.W; w += 16) {   // uniform in a wave
         QrRowValue row = {(double)a.score[row0 + w], 0.0, NAN};
         if (reads_logits(a, row0 + w)) {
-            load_logits<T, NV>(x + w * a.ld, a.V, lane, 64, f);
-            float largest = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) largest = fmaxf(largest, f[i]);
+            f.load(x + w * a.ld, a.V, lane, 64);
+            const float largest = f.largest();
             row.log_sum = 0.0;
             if (a.log_softmax) {
                 const unsigned k = qr_wave_reduce_u32<true>(logit_key(largest));
                 const float top = k ? qr_key_float(k) : -INFINITY;
-                float s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) s += qr_exp(f[i] - top);   // (of -inf alone: NaN)
                 row.top = (double)top;
-                row.log_sum = log(wave_sum((double)s));
+                f.anew();
+                row.log_sum = log(wave_sum((double)f.sum_exp(top)));   // (of -inf alone: NaN)
             }
             if (largest > -INFINITY) {
                 const unsigned k = (unsigned)(row(largest) >> 32);
@@ -431,16 +501,15 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
     for (int w = wave; w < a.W; w += 16) {
         const QrRowValue row = rows[w];
         if (row.log_sum == row.log_sum) {
-            if (a.W > 16) load_logits<T, NV>(x + w * a.ld, a.V, lane, 64, f);
+            if (a.W > 16) f.load(x + w * a.ld, a.V, lane, 64);
+            f.anew();
             // the bound as a logit of this row, a little lower than it is; where it has none every logit passes
             const double at = Tk ? ((word_value((QrValue)Tk << 32) - row.score) + row.log_sum) + row.top : -INFINITY;
             const float least = at == at ? fmaxf((float)(at - 1e-6 * fabs(at)), -FLT_MAX) : -FLT_MAX;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (f[i] >= least) {
-                    const QrPick p = {row(f[i]), qr_cand(qr_float_key(f[i] + 0.0f), ((i / V) * 64 + lane) * V + i % V), w};
-                    if ((unsigned)(p.v >> 32) >= Tk && p.v) push(list, p);
-                }
+            f.hits(f.largest(), least, [&](float l, int i) {
+                const QrPick p = {row(l), qr_cand(qr_float_key(l + 0.0f), ((i / V) * 64 + lane) * V + i % V), w};
+                if ((unsigned)(p.v >> 32) >= Tk && p.v) push(list, p);
+            });
         } else if (lane == 0 && is_finished(a, row0 + w)) {
             const QrPick p = {value_word(row.score), qr_cand(1u, a.end_token), w};
             if ((unsigned)(p.v >> 32) >= Tk && p.v) push(list, p);
@@ -464,13 +533,14 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
     });
 }
 
-// How rows are cut: whole up to SHORT logits (one launch); stretches of up to 8192 logits for 256 threads, or of 32768 for 1024 where
-// rows are long and fill the device.
+// How rows are cut: whole up to SHORT logits (one launch); stretches of up to 8192 logits for 256 threads, or of 16384 for 512 where
+// there are rows enough to fill the device (64 x 16 x 32000 bf16, n_out 16: 28 us, by 8192 28, by 32768 30; 16 x 16 x 32000 fp32, n_out
+// 32: 18, by 8192 26).
 constexpr int SHORT = 2048;
-bool long_stretches(int64_t rows, int V) { return rows >= 256 && V > 16384; }
+bool long_stretches(int64_t rows, int V) { return rows >= 256 && V > 8192; }
 void plan_select(int64_t rows, int V, int &n_parts, int &part)
 {
-    const int len = long_stretches(rows, V) ? 32768 : 8192;
+    const int len = long_stretches(rows, V) ? 16384 : 8192;
     n_parts = (V + len - 1) / len;
     part = qr_round_up((V + n_parts - 1) / n_parts, 8);
     n_parts = (V + part - 1) / part;
@@ -501,8 +571,11 @@ void launch_select(QrSelectArgs &a, void *workspace, hipStream_t st)
     a.cands = (QrCand *)((char *)workspace + heads_bytes(rows, a.n_parts));
     const dim3 grid(a.n_parts, (unsigned)(rows < 32768 ? rows : 32768), (unsigned)((rows + 32767) / 32768));
     if (!long_stretches(rows, a.V)) select_parts_kernel<T, 8192 / 256 / V, 256><<<grid, 256, 0, st>>>(a);
-    else select_parts_kernel<T, 32768 / 1024 / V, 1024><<<grid, 1024, 0, st>>>(a);
-    select_beam_kernel<<<a.B, 256, 0, st>>>(a);
+    else select_parts_kernel<T, 16384 / 512 / V, 512><<<grid, 512, 0, st>>>(a);
+    const int64_t total = (int64_t)a.W * a.n_parts * a.K;
+    if (total <= 1024) select_beam_kernel<256, true><<<a.B, 256, 0, st>>>(a);
+    else if (total <= 4096) select_beam_kernel<1024, true><<<a.B, 1024, 0, st>>>(a);
+    else select_beam_kernel<1024, false><<<a.B, 1024, 0, st>>>(a);
 }
 
 }  // namespace
