@@ -168,7 +168,8 @@ qrnnt_status qrnnt_quantize_act_rows(const float *x, int64_t rows, int32_t cols,
  * codes a value next to their border gets is decided by the exact quotient (ties to even), not by its fp32 rounding.
  *
  * Element types of the floating arrays of these and the following calls.  Pitches (ld_*) are in elements and at least
- * cols; rows may start at any element, 16-byte aligned ones are fastest. */
+ * cols; rows may start at any element, 16-byte aligned ones are fastest.  Counts above 2^30 (rows of quantizers: 2^31 - 1)
+ * and matrices of more than 2^60 elements are QRNNT_ERR_UNSUPPORTED. */
 enum { QRNNT_F32 = 0, QRNNT_F16 = 1, QRNNT_BF16 = 2 };
 
 /* scale[r] = max_k |x[r,k]| / 127, q[r,k] = rne(127 x[r,k] / max_k |x[r,k]|).  x [device] [rows, cols] of `dtype` with

@@ -13,6 +13,9 @@ static inline bool qr_overlap(const void *p, size_t pn, const void *q, size_t qn
     const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
     return a < b + qn && b < a + pn;
 }
+// Rows, columns and pitches whose products and sums stay far from the ends of 64 and, for the counts, 32 bits.
+static inline bool qr_counts_ok(int64_t rows, int64_t cols) { return rows <= INT32_MAX && cols <= 1 << 30; }
+static inline bool qr_pitch_ok(int64_t rows, int64_t ld) { return ld <= ((int64_t)1 << 60) / (rows > 0 ? rows : 1); }
 // Bytes from the first to behind the last element of a matrix.
 static inline size_t qr_matrix_bytes(int64_t rows, int64_t cols, int64_t ld, size_t size)
 {

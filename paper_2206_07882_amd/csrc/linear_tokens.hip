@@ -451,13 +451,13 @@ void launch_linear_tokens(const QrTokensLinear &p, const QrTokensPlan &plan, hip
     }
 }
 
-bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0 && w->cols > 0 && w->cols <= 131071; }
+bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0 && w->rows <= 1 << 30 && w->cols > 0 && w->cols <= 131071; }
 
 }  // namespace
 
 extern "C" size_t qrnnt_linear_tokens_workspace(const qrnnt_qmat *w, int32_t M)
 {
-    if (!tokens_weights_ok(w) || M <= 0) return 0;
+    if (!tokens_weights_ok(w) || M <= 0 || M > 1 << 30) return 0;
     const int parts = plan_linear_tokens(w->rows, w->cols, M).parts;
     return parts > 1 ? (size_t)parts * M * qr_round_up(w->rows, 4) * 4 : 0;
 }
@@ -470,7 +470,7 @@ extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bi
     if (s != QRNNT_OK) return s;
     QR_REQUIRE(qr_is_dtype(y_dtype), QRNNT_ERR_RANGE);
     QR_REQUIRE(M >= 0 && ld_a >= qr_act_pitch(w->cols) && ld_a % 16 == 0 && ld_y >= w->rows, QRNNT_ERR_SHAPE);
-    QR_REQUIRE(qr_bits(w) == 8 && tokens_weights_ok(w), QRNNT_ERR_UNSUPPORTED);
+    QR_REQUIRE(qr_bits(w) == 8 && tokens_weights_ok(w) && M <= 1 << 30 && qr_pitch_ok(M, ld_y), QRNNT_ERR_UNSUPPORTED);
     if (M == 0) return QRNNT_OK;
     QR_REQUIRE(a != nullptr && a_scale != nullptr && y != nullptr, QRNNT_ERR_NULL);
     const size_t e = qr_dtype_size(y_dtype), need = qrnnt_linear_tokens_workspace(w, M);

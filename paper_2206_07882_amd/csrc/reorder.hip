@@ -34,9 +34,10 @@ __global__ __launch_bounds__(256) void reorder_kernel(const QrReorderArgs a)
     const int64_t whole = a.s[k].row_bytes / SIZE, pieces = whole + a.s[k].row_bytes % SIZE;
     const int groups = IN_PLACE ? 1 : (a.W_out + NR - 1) / NR;
     const int64_t i = (int64_t)block * 256 + threadIdx.x;
-    const int64_t bg = i / pieces, piece = i - bg * pieces;
-    const int b = (int)(bg / groups), j0 = (int)(bg - (int64_t)b * groups) * NR;
-    if (b >= a.B) return;
+    // (quotients of 64 bits take longer than all else here)
+    const int64_t bg = i < 1ll << 31 && pieces < 1ll << 31 ? (int64_t)((unsigned)i / (unsigned)pieces) : i / pieces, piece = i - bg * pieces;
+    if (bg >= (int64_t)a.B * groups) return;
+    const int b = IN_PLACE ? (int)bg : (int)((unsigned)bg / (unsigned)groups), j0 = IN_PLACE ? 0 : ((int)bg - b * groups) * NR;
     const bool single = piece >= whole;   // a byte behind the last whole piece
     const int64_t at = single ? whole * SIZE + (piece - whole) : piece * SIZE;
     const int32_t *parent = a.parent + (int64_t)b * a.W_out + j0;
@@ -77,7 +78,7 @@ bool plan_reorder(QrReorderArgs &a)
     for (int k = 0; k < a.n; ++k) {
         const int64_t pieces = a.s[k].row_bytes / (int)sizeof(PIECE) + a.s[k].row_bytes % (int)sizeof(PIECE);
         const int64_t groups = IN_PLACE ? 1 : (a.W_out + NR - 1) / NR;
-        if (pieces > INT64_MAX / 256 / groups / a.B) return false;
+        if (groups * a.B > INT32_MAX || pieces > INT64_MAX / 256 / groups / a.B) return false;
         end += (pieces * groups * a.B + 255) / 256;
         if (end > INT32_MAX) return false;
         a.end[k] = (unsigned)end;
@@ -109,9 +110,12 @@ extern "C" qrnnt_status qrnnt_reorder_states(const qrnnt_state_rows *states, int
     QR_REQUIRE(B >= 0 && W > 0 && W_out > 0, QRNNT_ERR_SHAPE);
     QR_REQUIRE(W <= 64 && W_out <= 64, QRNNT_ERR_UNSUPPORTED);
     QR_REQUIRE(states != nullptr, QRNNT_ERR_NULL);
-    for (int k = 0; k < n_states; ++k)
-        QR_REQUIRE(states[k].row_bytes > 0 && states[k].src_pitch >= states[k].row_bytes && states[k].dst_pitch >= states[k].row_bytes &&
-                       states[k].src_pitch <= (int64_t)1 << 40 && states[k].dst_pitch <= (int64_t)1 << 40, QRNNT_ERR_SHAPE);
+    const int64_t rows = (int64_t)B * (W > W_out ? W : W_out);
+    for (int k = 0; k < n_states; ++k) {
+        const qrnnt_state_rows &s = states[k];
+        QR_REQUIRE(s.row_bytes > 0 && s.src_pitch >= s.row_bytes && s.dst_pitch >= s.row_bytes, QRNNT_ERR_SHAPE);
+        QR_REQUIRE(qr_pitch_ok(rows, s.src_pitch) && qr_pitch_ok(rows, s.dst_pitch), QRNNT_ERR_UNSUPPORTED);
+    }
     if (B == 0) return QRNNT_OK;
     QR_REQUIRE(parent != nullptr, QRNNT_ERR_NULL);
     QR_REQUIRE(qr_aligned(parent, 4), QRNNT_ERR_ALIGN);

@@ -282,7 +282,8 @@ extern "C" qrnnt_status qrnnt_quantize_tokens(const void *x, int32_t dtype, int6
                                               int32_t ld_q, float *scale, void *stream)
 {
     QR_REQUIRE(qr_is_dtype(dtype), QRNNT_ERR_RANGE);
-    QR_REQUIRE(rows >= 0 && rows <= INT32_MAX && cols > 0 && ld_x >= cols && ld_q >= cols && ld_q % 16 == 0, QRNNT_ERR_SHAPE);
+    QR_REQUIRE(rows >= 0 && cols > 0 && ld_x >= cols && ld_q >= cols && ld_q % 16 == 0, QRNNT_ERR_SHAPE);
+    QR_REQUIRE(qr_counts_ok(rows, cols) && qr_pitch_ok(rows, ld_x), QRNNT_ERR_UNSUPPORTED);
     if (rows == 0) return QRNNT_OK;
     QR_REQUIRE(x != nullptr && q != nullptr && scale != nullptr, QRNNT_ERR_NULL);
     QR_REQUIRE(qr_aligned(x, qr_dtype_size(dtype)) && qr_aligned(q, 16) && qr_aligned(scale, 4), QRNNT_ERR_ALIGN);
@@ -296,8 +297,10 @@ extern "C" qrnnt_status qrnnt_rms_norm_quant(const void *x, const void *residual
                                              int64_t ld_sum, int8_t *q, int32_t ld_q, float *scale, void *stream)
 {
     QR_REQUIRE(qr_is_dtype(dtype) && eps >= 0.0f && eps < INFINITY, QRNNT_ERR_RANGE);
-    QR_REQUIRE(rows >= 0 && rows <= INT32_MAX && cols > 0 && ld_x >= cols && ld_q >= cols && ld_q % 16 == 0, QRNNT_ERR_SHAPE);
+    QR_REQUIRE(rows >= 0 && cols > 0 && ld_x >= cols && ld_q >= cols && ld_q % 16 == 0, QRNNT_ERR_SHAPE);
     QR_REQUIRE(residual == nullptr || (ld_residual >= cols && ld_sum >= cols), QRNNT_ERR_SHAPE);
+    QR_REQUIRE(qr_counts_ok(rows, cols) && qr_pitch_ok(rows, ld_x), QRNNT_ERR_UNSUPPORTED);
+    QR_REQUIRE(residual == nullptr || (qr_pitch_ok(rows, ld_residual) && qr_pitch_ok(rows, ld_sum)), QRNNT_ERR_UNSUPPORTED);
     if (rows == 0) return QRNNT_OK;
     QR_REQUIRE(x != nullptr && q != nullptr && scale != nullptr && (residual == nullptr || sum_out != nullptr), QRNNT_ERR_NULL);
     const size_t e = qr_dtype_size(dtype);

@@ -597,7 +597,7 @@ extern "C" qrnnt_status qrnnt_beam_select(const float *score, const void *logits
 {
     QR_REQUIRE(qr_is_dtype(dtype), QRNNT_ERR_RANGE);
     QR_REQUIRE(B >= 0 && W > 0 && V > 0 && n_out > 0 && ld >= V, QRNNT_ERR_SHAPE);
-    QR_REQUIRE(select_sizes_ok(B, W, V, n_out), QRNNT_ERR_UNSUPPORTED);
+    QR_REQUIRE(select_sizes_ok(B, W, V, n_out) && qr_pitch_ok((int64_t)B * W, ld), QRNNT_ERR_UNSUPPORTED);
     QR_REQUIRE(finished == nullptr || (end_token >= 0 && end_token < V), QRNNT_ERR_RANGE);
     if (B == 0) return QRNNT_OK;
     QR_REQUIRE(score && logits && parent_out && token_out && score_out && workspace, QRNNT_ERR_NULL);

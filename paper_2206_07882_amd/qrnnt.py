@@ -271,16 +271,21 @@ _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 
 def _dtype(t: torch.dtype) -> int:
-    if t not in _DTYPES:
+    code = _DTYPES.get(t)
+    if code is None:
         raise TypeError(f"expected float32, float16 or bfloat16, got {t}")
-    return _DTYPES[t]
+    return code
 
 
-def _here(*tensors):
+def _here(first: torch.Tensor, *others):
     """The tensors a call works on have to be on the current device, on whose current stream it runs."""
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch._C._cuda_getDevice()):
-            raise ValueError(f"expected a tensor on the current GPU, got one on {t.device}")
+    device = torch._C._cuda_getDevice() if first.is_cuda else -1
+    if device >= 0 and first.get_device() == device:
+        for t in others:
+            if t is not None and t.get_device() != device:
+                raise ValueError(f"expected a tensor on the current GPU, got one on {t.device}")
+    else:
+        raise ValueError(f"expected a tensor on the current GPU, got one on {first.device}")
 
 
 def _matrix(t: torch.Tensor, dtype, rows: int, cols: int):
@@ -311,17 +316,6 @@ def _vector(t: Optional[torch.Tensor], dtype, n: int):
     return t.data_ptr()
 
 
-def _rows_of(x: torch.Tensor):
-    """(rows, columns, dtype, address, pitch) of the matrix that a call is about."""
-    if not x.is_cuda or x.get_device() != torch._C._cuda_getDevice():
-        _here(x)
-    if x.dim() != 2:
-        raise ValueError(f"expected a matrix, got {tuple(x.shape)}")
-    rows, cols = x.shape
-    address, pitch = _matrix(x, x.dtype, rows, cols)
-    return rows, cols, _DTYPES.get(x.dtype) if x.dtype in _DTYPES else _dtype(x.dtype), address, pitch
-
-
 def _code_outputs(rows: int, cols: int, codes, scale, device):
     """(codes, scale, address and pitch of the codes, address of the scales), made where they are not given."""
     width = (cols + 15) & ~15   # qrnnt_act_pitch
@@ -329,23 +323,24 @@ def _code_outputs(rows: int, cols: int, codes, scale, device):
         codes = torch.empty((rows, width), dtype=torch.int8, device=device)
         address, pitch = codes.data_ptr(), width
     else:
-        _here(codes)
         address, pitch = _matrix(codes, torch.int8, rows, codes.shape[-1])
         if codes.shape[1] < width:
             raise ValueError(f"codes have {codes.shape[1]} columns, rows of {cols} take {width}")
     if scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=device)
         return codes, scale, address, pitch, scale.data_ptr()
-    _here(scale)
     return codes, scale, address, pitch, _vector(scale, torch.float32, rows)
 
 
 def quantize_tokens(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """[rows, cols] of float32, float16 or bfloat16 (rows may lie apart) -> int8 codes [rows, act_pitch(cols)] with zeros behind
     the columns, and the scale of each row: 8 bits over the row's own range (qrnnt_quantize_tokens)."""
-    rows, cols, dtype, px, ld = _rows_of(x)
+    _here(x, codes, scale)
+    dtype = x.dtype
+    rows, cols = x.shape
+    px, ld = _matrix(x, dtype, rows, cols)
     codes, scale, pq, ld_q, ps = _code_outputs(rows, cols, codes, scale, x.device)
-    _call("qrnnt_quantize_tokens", px, dtype, rows, cols, ld, pq, ld_q, ps, _stream_handle())
+    _call("qrnnt_quantize_tokens", px, _dtype(dtype), rows, cols, ld, pq, ld_q, ps, _stream_handle())
     return codes, scale
 
 
@@ -354,20 +349,22 @@ def rms_norm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: 
                    codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """Residual sum, root-mean-square norm and 8-bit quantizer with a scale for each row (qrnnt_rms_norm_quant): returns
     (codes, scale, x + residual, or x itself without a residual).  sum_out may be x or residual."""
-    rows, cols, dtype, px, ld = _rows_of(x)
-    _here(weight, residual, sum_out)
+    _here(x, weight, residual, sum_out, codes, scale)
+    dtype = x.dtype
+    rows, cols = x.shape
+    px, ld = _matrix(x, dtype, rows, cols)
     pr = psum = None
     ld_r = ld_s = cols
     if residual is not None:
-        pr, ld_r = _matrix(residual, x.dtype, rows, cols)
+        pr, ld_r = _matrix(residual, dtype, rows, cols)
         if sum_out is None:
-            sum_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-        psum, ld_s = _matrix(sum_out, x.dtype, rows, cols)
+            sum_out = torch.empty((rows, cols), dtype=dtype, device=x.device)
+        psum, ld_s = _matrix(sum_out, dtype, rows, cols)
     elif sum_out is not None:
         raise ValueError("sum_out needs a residual")
     codes, scale, pq, ld_q, ps = _code_outputs(rows, cols, codes, scale, x.device)
-    _call("qrnnt_rms_norm_quant", px, pr, _vector(weight, x.dtype, cols), dtype, rows, cols, ld, ld_r, eps, psum, ld_s, pq, ld_q, ps,
-          _stream_handle())
+    _call("qrnnt_rms_norm_quant", px, pr, _vector(weight, dtype, cols), _dtype(dtype), rows, cols, ld, ld_r, eps, psum, ld_s, pq, ld_q,
+          ps, _stream_handle())
     return codes, scale, x if residual is None else sum_out
 
 
@@ -381,7 +378,7 @@ def linear_tokens(w: QMat, codes: torch.Tensor, scale: torch.Tensor, bias: Optio
                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """8-bit linear layer of rows with a scale each, as quantize_tokens and rms_norm_quant return them: w from
     pack_int8(..., LAYOUT_TILED), codes [M, act_pitch(cols)] (qrnnt_linear_tokens).  out may be a matrix whose rows lie apart."""
-    _here(codes, scale, bias, workspace, w.packed, w.row_scale)
+    _here(codes, scale, bias, workspace, w.packed, out)
     M = codes.shape[0]
     pa, ld_a = _matrix(codes, torch.int8, M, codes.shape[-1])
     if codes.shape[1] < (w.cols + 15) & ~15:
@@ -391,7 +388,6 @@ def linear_tokens(w: QMat, codes: torch.Tensor, scale: torch.Tensor, bias: Optio
         out = torch.empty((M, w.rows), dtype=dtype, device=codes.device)
         py, ld_y = out.data_ptr(), w.rows
     else:
-        _here(out)
         kind = _dtype(out.dtype)
         py, ld_y = _matrix(out, out.dtype, M, w.rows)
     cw = w.c()
@@ -627,8 +623,9 @@ def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] 
     bfloat16; rows may lie apart): (parent, token, score, finished), each [B, n_out] (qrnnt_beam_select).  finished
     [B, W] (bool or uint8): hypotheses that keep their score and repeat end_token; needs end_token.  The last result is None
     without end_token."""
-    rows, V, dtype, pl, ld = _rows_of(logits)
-    _here(score, finished, workspace)
+    _here(logits, score, finished, workspace)
+    rows, V = logits.shape
+    pl, ld = _matrix(logits, logits.dtype, rows, V)
     B, W = score.shape
     if rows != B * W:
         raise ValueError(f"expected logits of {B * W} hypotheses, got {rows}")
@@ -650,7 +647,7 @@ def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] 
     tok = torch.empty((B, K), dtype=torch.int32, device=dev)
     ns = torch.empty((B, K), dtype=torch.float32, device=dev)
     done = None if end_token is None else torch.empty((B, K), dtype=torch.bool, device=dev)
-    _call("qrnnt_beam_select", _vector(score, torch.float32, rows), pl, dtype, ld, 1 if log_softmax else 0,
+    _call("qrnnt_beam_select", _vector(score, torch.float32, rows), pl, _dtype(logits.dtype), ld, 1 if log_softmax else 0,
           pf, -1 if end_token is None else end_token, B, W, V, K, par.data_ptr(), tok.data_ptr(), ns.data_ptr(),
           None if done is None else done.data_ptr(), _addr(workspace), workspace.nbytes, _stream_handle())
     return par, tok, ns, done

@@ -109,3 +109,41 @@ def test_the_same_call_gives_the_same_bits_whatever_the_workspace_held(gpu_lib):
             ws = torch.full((need + 256,), fill, dtype=torch.uint8, device=DEV)
             assert torch.equal(q.linear_tokens(m, a, sa, workspace=ws), first)
             assert bool((ws[need:] == fill).all())
+
+
+def test_every_way_captured_and_replayed(gpu_lib):
+    """Few tokens, each size of tile, a sum in parts: replays on new inputs in the captured places against eager calls."""
+    q = gpu_lib
+    for M, N, K in ((7, 100, 300), (90, 700, 640), (700, 2600, 300), (3000, 4200, 256), (300, 64, 8192)):
+        d = [make(M + i, M, N, K) for i in range(3)]
+        a, sa, m = pad(d[0]["a"], (K + 15) // 16 * 16), torch.from_numpy(d[0]["sa"]).to(DEV), weights(q, d[0])
+        ws = torch.empty(max(1, q.linear_tokens_workspace(m, M)), dtype=torch.uint8, device=DEV)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = q.linear_tokens(m, a, sa, dtype=torch.float16, workspace=ws)
+        for e in d[1:]:
+            a[:, :K] = torch.from_numpy(e["a"]).to(DEV)
+            sa.copy_(torch.from_numpy(e["sa"]))
+            graph.replay()
+            torch.cuda.synchronize()
+            check(y, dict(d[0], a=e["a"], sa=e["sa"]), torch.float16, with_bias=False)
+            assert torch.equal(q.linear_tokens(m, a, sa, dtype=torch.float16), y)
+            ws.fill_(255)
+
+
+def test_two_streams_at_once(gpu_lib):
+    """Calls that overlap, each with a workspace of its own."""
+    q = gpu_lib
+    d = [make(i, M, 64, 8192) for i, M in enumerate((300, 200))]
+    ins = [(weights(q, e), pad(e["a"], 8192), torch.from_numpy(e["sa"]).to(DEV)) for e in d]
+    want = [q.linear_tokens(*i) for i in ins]
+    streams = [torch.cuda.Stream() for _ in ins]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(5):
+        for k, (s, i) in enumerate(zip(streams, ins)):
+            with torch.cuda.stream(s):
+                outs[k].append(q.linear_tokens(*i))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(o, want[k]) for o in outs[k])

@@ -19,7 +19,8 @@ def test_quantize_tokens(lib):
     f = lambda x=0x1000, dt=0, rows=4, cols=20, ld=20, q=0x20000, ld_q=32, s=0x30000: lib.qrnnt_quantize_tokens(x, dt, rows, cols, ld, q, ld_q, s, None)
     assert f(x=None) == NULL and f(q=None) == NULL and f(s=None) == NULL
     assert f(dt=3) == RANGE and f(dt=-1) == RANGE
-    assert f(rows=-1) == SHAPE and f(cols=0) == SHAPE and f(ld=19) == SHAPE and f(ld_q=16) == SHAPE and f(ld_q=40) == SHAPE and f(rows=1 << 31) == SHAPE
+    assert f(rows=-1) == SHAPE and f(cols=0) == SHAPE and f(ld=19) == SHAPE and f(ld_q=16) == SHAPE and f(ld_q=40) == SHAPE
+    assert f(rows=1 << 31) == UNSUPPORTED and f(cols=(1 << 30) + 1, ld=1 << 31, ld_q=(1 << 30) + 16) == UNSUPPORTED and f(ld=1 << 59) == UNSUPPORTED
     assert f(x=0x1002) == ALIGN and f(q=0x20008) == ALIGN and f(s=0x30002) == ALIGN and f(x=0x1001, dt=2) == ALIGN
     assert f(rows=0) == OK and f(rows=0, x=None) == OK
 
@@ -33,6 +34,7 @@ def test_rms_norm_quant(lib):
     assert f(x=0x10001) == ALIGN and f(res=0x20002) == ALIGN and f(w=0x30001) == ALIGN and f(out=0x40003) == ALIGN and f(q=0x50001) == ALIGN
     # the sum may take the place of an input, not overlap it otherwise
     assert f(out=0x10004) == RANGE and f(out=0x20000 - 4) == RANGE and f(out=0x10000, ld_s=24) == RANGE and f(out=0x20000 + 79 * 4) == RANGE
+    assert f(ld_r=1 << 60) == UNSUPPORTED and f(ld_s=1 << 60) == UNSUPPORTED and f(ld_r=1 << 60, res=None, x=None) == NULL
     assert f(rows=0) == OK
 
 
@@ -49,6 +51,7 @@ def test_linear_tokens(lib):
     assert f(dt=3) == RANGE
     assert f(M=-1) == SHAPE and f(ld_a=96) == SHAPE and f(ld_a=120) == SHAPE and f(ld_y=63) == SHAPE and f(_mat(rows=0)) == SHAPE
     assert f(a=0x10008) == ALIGN and f(y=0x40002) == ALIGN and f(y=0x40001, dt=1) == ALIGN and f(bias=0x5001) == ALIGN and f(sa=0x3002) == ALIGN
+    assert f(M=(1 << 30) + 1) == UNSUPPORTED and f(_mat(rows=(1 << 30) + 1), ld_y=1 << 31) == UNSUPPORTED and f(ld_y=1 << 60) == UNSUPPORTED
     assert f(M=0) == OK and f(M=0, a=None, y=None) == OK
     assert lib.qrnnt_linear_tokens_workspace(None, 4) == 0 and lib.qrnnt_linear_tokens_workspace(C.byref(_mat()), 0) == 0
     for rows, cols, M in ((64, 131071, 33), (64, 8192, 16), (100, 4096, 200), (8192, 8192, 8192)):
@@ -69,6 +72,7 @@ def test_beam_select(lib):
     assert f(dt=3) == RANGE and f(fin=0x5000) == RANGE and f(fin=0x5000, end=100) == RANGE
     assert f(B=-1) == SHAPE and f(W=0) == SHAPE and f(V=0) == SHAPE and f(n=0) == SHAPE and f(ld=99) == SHAPE
     assert f(W=65) == UNSUPPORTED and f(n=65) == UNSUPPORTED and f(W=64, V=1 << 25, ld=1 << 25) == UNSUPPORTED and f(B=1 << 30, W=4) == UNSUPPORTED
+    assert f(W=1, V=(1 << 30) + 1, ld=1 << 31) == UNSUPPORTED and f(ld=1 << 60) == UNSUPPORTED
     assert f(score=0x1002) == ALIGN and f(logits=0x10001, dt=1) == ALIGN and f(par=0x2001) == ALIGN and f(ws=0x100008) == ALIGN
     need = qrnnt.beam_select_workspace(2, 4, 100, 4)
     assert need > 0 and f(size=need - 1) == WORKSPACE
@@ -87,7 +91,8 @@ def test_reorder_states(lib):
     assert f([], n=0) == RANGE and f([good] * 33) == RANGE
     assert f([good], B=-1) == SHAPE and f([good], W=0) == SHAPE and f([good], W_out=0) == SHAPE and f([good], W=65) == UNSUPPORTED and f([good], W_out=65) == UNSUPPORTED
     assert f([S(0x10000, 0x20000, 0, 64, 64)]) == SHAPE and f([S(0x10000, 0x20000, 64, 63, 64)]) == SHAPE and f([S(0x10000, 0x20000, 64, 64, 63)]) == SHAPE
-    assert f([good], parent=0x900002) == ALIGN
+    assert f([good], parent=0x900002) == ALIGN and f([S(0x10000, 0x20000, 64, 1 << 60, 64)]) == UNSUPPORTED and f([S(0x10000, 0x20000, 64, 64, 1 << 60)]) == UNSUPPORTED
+    assert f([good], B=1 << 30, W=1, W_out=1, parent=0x9000000000) == RANGE
     # overlaps: a destination with another row of its source, with another array, with the parents; the same rows at another beam
     assert f([S(0x10000, 0x10040, 64, 64, 64)]) == RANGE and f([S(0x10000, 0x10000, 64, 64, 128)]) == RANGE
     assert f([S(0x10000, 0x10000, 64, 64, 64)], W_out=3) == RANGE
