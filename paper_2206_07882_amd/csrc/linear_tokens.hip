@@ -319,7 +319,10 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
                     T *y = (T *)p.y + (int64_t)m * p.ld_y + r;
                     if (m < p.M) {
                         if (r + E <= p.rows) {
-                            *(typename QrVec<T>::any *)y = v;
+                            // Not kept in the L2 (whose lines the operands are in, and which a launch ends with writing back): large tiles past
+                        // it (16000 x 2560 x 1280 fp32 77 us, now 70), the others through it (1024 x 2048 x 2048 10.1, now 9.1; past it 9.4)
+                        if (MT * WN >= 16) __builtin_nontemporal_store(v, (typename QrVec<T>::any *)y);
+                        else qr_store_through((float *)y, __builtin_bit_cast(v4f, v));
                         } else {
 #pragma unroll
                             for (int e = 0; e < E; ++e)
@@ -354,11 +357,16 @@ __global__ __launch_bounds__(256) void linear_tokens_join_kernel(const QrTokensL
     finish<T>(p, m, r0, sum, sw, bs, p.s_a[m]);
 }
 
-// How a product is computed.
+// How a product is computed: all tokens in one way, or full rounds of large tiles and the tokens that remain in another.
 enum QrTokensKind { FEW, SMALL, MIDDLE, LARGE };
-struct QrTokensPlan {
+struct QrTokensPiece {
     QrTokensKind kind;
     int parts;       // the columns are cut into (SMALL)
+    int M;           // tokens
+};
+struct QrTokensPlan {
+    QrTokensPiece piece[2];
+    int n;
 };
 
 // Tiles by what they were measured to take (us): a chunk of 128 columns while at most half of the places on the device are
@@ -378,13 +386,11 @@ constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.28f, 0.43f, 1.5f}, {128, 512
 // Measured at each choice (us; few / small / middle / large): 32 x 1000 x 1000 (tokens x rows x columns) 3.4 / 4.5; 48 x 16000 x
 // 4000 14.1 / 12.3; 200 x 8000 x 500 - / 4.5 / 7.7 / 12.9; 4000 x 1024 x 4096 - / 30.6 / 26.8 / 39.9; 2000 x 5000 x 3000 - / 59 / 46 /
 // 37; 8192^3 - / 879 / 569 / 403.  300 x 1024 x 8192 on small tiles whole 20.7, in two parts 15.1, in four 12.8.
-QrTokensPlan plan_linear_tokens(int rows, int K, int M)
+QrTokensPiece plan_piece(int rows, int K, int M, float &least)
 {
     const int nkc = qr_round_up(K, QRNNT_KCHUNK) / QRNNT_KCHUNK;
-    // few tokens: beyond 16 their codes are fetched as often as the weights and more, so long or many rows go to tiles
-    if (M <= 16 || (M <= 32 && (rows <= 16384 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= 4096)) return {FEW, 1};
-    QrTokensPlan best = {SMALL, 1};
-    float least = INFINITY;
+    QrTokensPiece best = {SMALL, 1, M};
+    least = INFINITY;
     for (int kind = SMALL; kind <= LARGE; ++kind) {
         const QrTileCost &c = TILE_COST[kind];
         for (int parts = 1; parts <= (kind == SMALL ? 8 : 1) && (parts == 1 || nkc / parts >= 4); ++parts) {
@@ -392,8 +398,33 @@ QrTokensPlan plan_linear_tokens(int rows, int K, int M)
             const float t = c.time(c.tiles(rows, M) * parts, (nkc + parts - 1) / parts) + join;
             if (t < least) {
                 least = t;
-                best = {(QrTokensKind)kind, parts};
+                best = {(QrTokensKind)kind, parts, M};
             }
+        }
+    }
+    return best;
+}
+
+QrTokensPlan plan_linear_tokens(int rows, int K, int M)
+{
+    // few tokens: beyond 16 their codes are fetched as often as the weights and more, so long or many rows go to tiles
+    if (M <= 16 || (M <= 32 && (rows <= 16384 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= 4096)) return {{{FEW, 1, M}}, 1};
+    float least;
+    QrTokensPlan best = {{plan_piece(rows, K, M, least)}, 1};
+    // whole rounds of large tiles first, what would leave a round part empty in a launch of its own (6000 x 3000 x 5000: 114 us
+    // in two rounds, 93 in one and middle tiles; 2100 x 8192 x 4096 88 and 66)
+    const QrTileCost &c = TILE_COST[LARGE];
+    const int nkc = qr_round_up(K, QRNNT_KCHUNK) / QRNNT_KCHUNK, across = (rows + c.size - 1) / c.size;
+    const int64_t rounds = c.tiles(rows, M) / c.places;
+    for (int64_t r = rounds > 1 ? rounds - 1 : rounds; r >= 1 && r <= rounds; ++r) {
+        const int64_t first = r * c.places / across * c.size;   // tokens of the whole rounds
+        if (first < c.size || first >= M) continue;
+        float rest;
+        const QrTokensPiece second = plan_piece(rows, K, M - (int)first, rest);
+        const float t = c.time(c.tiles(rows, (int)first), nkc) + rest + 2.0f;
+        if (t < least) {
+            least = t;
+            best = {{{LARGE, 1, (int)first}, second}, 2};
         }
     }
     return best;
@@ -420,9 +451,9 @@ void launch_few(const QrTokensLinear &p, hipStream_t st)
 }
 
 template <class T>
-void launch_linear_tokens(const QrTokensLinear &p, const QrTokensPlan &plan, hipStream_t st)
+void launch_piece(const QrTokensLinear &p, const QrTokensPiece &piece, hipStream_t st)
 {
-    switch (plan.kind) {
+    switch (piece.kind) {
     case FEW:
         // One row tile to a workgroup while that does not take more than two workgroups a compute unit; 8 waves where there are
         // few of them (1 x 512 x 8192 3.7 us, with 4 waves 4.4; 16 x 8192 x 4096 7.3, with 4 waves 6.8).  Two row tiles beyond (16 x
@@ -439,15 +470,27 @@ void launch_linear_tokens(const QrTokensLinear &p, const QrTokensPlan &plan, hip
         }
         return;
     case SMALL:
-        if (plan.parts > 1) {
-            launch_tiles<v4i, 4, 1, 1, 4, 4>(p, plan.parts, st);
-            linear_tokens_join_kernel<T><<<(unsigned)(((int64_t)p.M * p.ld_part + 255) / 256), 256, 0, st>>>(p, plan.parts);
+        if (piece.parts > 1) {
+            launch_tiles<v4i, 4, 1, 1, 4, 4>(p, piece.parts, st);
+            linear_tokens_join_kernel<T><<<(unsigned)(((int64_t)p.M * p.ld_part + 255) / 256), 256, 0, st>>>(p, piece.parts);
         } else {
             launch_tiles<T, 4, 1, 1, 4, 4>(p, 1, st);
         }
         return;
     case MIDDLE: launch_tiles<T, 4, 4, 2, 2, 2>(p, 1, st); return;
     case LARGE: launch_tiles<T, 8, 4, 2, 4, 2>(p, 1, st); return;
+    }
+}
+
+template <class T>
+void launch_linear_tokens(QrTokensLinear p, const QrTokensPlan &plan, hipStream_t st)
+{
+    for (int i = 0; i < plan.n; ++i) {
+        p.M = plan.piece[i].M;
+        launch_piece<T>(p, plan.piece[i], st);
+        p.a += (int64_t)p.M * p.ld_a;
+        p.s_a += p.M;
+        p.y = (T *)p.y + p.M * p.ld_y;
     }
 }
 
@@ -458,8 +501,9 @@ bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0
 extern "C" size_t qrnnt_linear_tokens_workspace(const qrnnt_qmat *w, int32_t M)
 {
     if (!tokens_weights_ok(w) || M <= 0 || M > 1 << 30) return 0;
-    const int parts = plan_linear_tokens(w->rows, w->cols, M).parts;
-    return parts > 1 ? (size_t)parts * M * qr_round_up(w->rows, 4) * 4 : 0;
+    const QrTokensPlan plan = plan_linear_tokens(w->rows, w->cols, M);
+    const QrTokensPiece &last = plan.piece[plan.n - 1];   // (large tiles in front of it are not cut)
+    return last.parts > 1 ? (size_t)last.parts * last.M * qr_round_up(w->rows, 4) * 4 : 0;
 }
 
 extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const int8_t *a, int32_t ld_a,
@@ -484,7 +528,7 @@ extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bi
     p.a = a;  p.s_a = a_scale;  p.ld_a = ld_a;  p.M = M;  p.y = y;  p.ld_y = ld_y;
     p.part = workspace;  p.ld_part = qr_round_up(w->rows, 4) / 4;
     const QrTokensPlan plan = plan_linear_tokens(w->rows, w->cols, M);
-    QR_REQUIRE(plan.kind == FEW || TILE_COST[plan.kind].tiles(w->rows, M) <= INT32_MAX, QRNNT_ERR_UNSUPPORTED);
+    QR_REQUIRE(plan.piece[0].kind == FEW || TILE_COST[plan.piece[0].kind].tiles(w->rows, M) <= INT32_MAX, QRNNT_ERR_UNSUPPORTED);
     if (y_dtype == QRNNT_F32) launch_linear_tokens<float>(p, plan, (hipStream_t)stream);
     else if (y_dtype == QRNNT_F16) launch_linear_tokens<_Float16>(p, plan, (hipStream_t)stream);
     else launch_linear_tokens<__bf16>(p, plan, (hipStream_t)stream);
