@@ -36,13 +36,14 @@ __device__ __forceinline__ void qr_load_vec(const T *p, float (&v)[QrVec<T>::N])
 #pragma unroll
     for (int i = 0; i < QrVec<T>::N; ++i) v[i] = (float)u[i];
 }
+// (past the caches: what is written is as a rule not read again soon)
 template <class T>
 __device__ __forceinline__ void qr_store_vec(T *p, const float (&v)[QrVec<T>::N])
 {
     typename QrVec<T>::type u;
 #pragma unroll
     for (int i = 0; i < QrVec<T>::N; ++i) u[i] = (T)v[i];
-    *(typename QrVec<T>::any *)p = u;
+    __builtin_nontemporal_store(u, (typename QrVec<T>::any *)p);
 }
 // The same for the first n elements; the others read as `fill`.
 template <class T>

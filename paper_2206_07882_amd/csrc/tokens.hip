@@ -99,12 +99,14 @@ __device__ __forceinline__ void odd_row(const T *h, const T *weight, int cols, f
     }
 }
 
+// Bound by memory: 16384 x 4096 bf16 with residual, 470 MB, in 84 us is 5.6 TB/s (a copy of 1 GiB on this card: 5.2); one row of
+// 4096 takes 4 us, the length of its chain.
 // TPR threads to a row (64: four rows to a workgroup), PER vectors of 16 bytes to a thread; PER = 0: rows of any length, read
 // a second time for the codes.
 template <class T, bool NORM, int TPR, int PER>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void tokens_kernel(const QrTokenArgs a)
+__global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrTokenArgs a)
 {
-    constexpr int V = QrVec<T>::N, RPB = TPR < 256 ? 256 / TPR : 1, NW = TPR / 64;
+    constexpr int V = QrVec<T>::N, RPB = TPR < 128 ? 256 / TPR : 1, NW = TPR / 64;
     constexpr bool WIDE = NORM && sizeof(T) == 4;   // products of two fp32 values do not fit fp32
     __shared__ QrRowSums<WIDE> red[NW > 1 ? NW : 1];
     __shared__ double red64[3 * NW];
@@ -253,14 +255,19 @@ template <class T, bool NORM>
 void launch_tokens(const QrTokenArgs &a, hipStream_t st)
 {
     constexpr int V = QrVec<T>::N;
+    // A row to as few threads as its registers allow (us, at the rows of 4 to 16 thousand tokens; a copy of as many bytes): 4096 bf16 with
+    // residual 84 (90), 1280 fp32 19.5 with 64 threads, 20.5 with 256 (19.7), 2000 fp16 with residual 14.8 with 128, 17.7 with 256 (10.8),
+    // 8192 bf16 with residual 34.9 with 512, 37.2 with 256 (33.1), 10000 bf16 27.0 with 256, 32.5 with 1024 (17.3).
     const int nv = (a.cols + V - 1) / V;
 #define QR_TOKENS(tpr, per) \
-    tokens_kernel<T, NORM, tpr, per><<<(unsigned)((a.rows + (tpr < 256 ? 256 / tpr : 1) - 1) / (tpr < 256 ? 256 / tpr : 1)), tpr < 256 ? 256 : tpr, 0, st>>>(a)
+    tokens_kernel<T, NORM, tpr, per><<<(unsigned)((a.rows + (tpr < 128 ? 256 / tpr : 1) - 1) / (tpr < 128 ? 256 / tpr : 1)), tpr < 128 ? 256 : tpr, 0, st>>>(a)
     if (nv <= 64) QR_TOKENS(64, 1);
     else if (nv <= 128) QR_TOKENS(64, 2);
-    else if (nv <= 256) QR_TOKENS(256, 1);
+    else if (nv <= 256) QR_TOKENS(128, 2);
+    else if (nv <= 320) QR_TOKENS(64, 5);
     else if (nv <= 512) QR_TOKENS(256, 2);
-    else if (nv <= 1024) QR_TOKENS(256, 4);
+    else if (nv <= 1024) QR_TOKENS(512, 2);
+    else if (nv <= 1280) QR_TOKENS(256, 5);
     else if (nv <= 2048) QR_TOKENS(1024, 2);
     else if (nv <= 4096) QR_TOKENS(1024, 4);
     else QR_TOKENS(1024, 0);

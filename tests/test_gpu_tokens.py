@@ -20,7 +20,7 @@ def scale_tolerance(cols, dtype):
     workgroup, each half a step of fp32 and halved by the root; mean, eps, root, reciprocal, product, quotient: 1 + 1
     (halved), then 4 of them."""
     V = 4 if dtype == torch.float32 else 8
-    chain = V * max(4, -(-cols // (1024 * V)))
+    chain = V * max(5, -(-cols // (1024 * V)))
     return ((chain + 6 + 16 + 2) / 2 + 4) * 2.0 ** -24
 
 
