@@ -118,6 +118,13 @@ __device__ __forceinline__ void qr_load_lds4(const void *gptr, unsigned lds_addr
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr), "s"(lds_addr) : "memory");
 }
 
+// Past the caches.  In asm: the compiler makes one ordinary store of a nontemporal and an ordinary one in two branches.
+// (s_nop 1: two wait states before the data registers of a wide store may be rewritten.)
+__device__ __forceinline__ void store_past(float *p, v4f v)
+{
+    asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" ::"v"(p), "v"(v) : "memory");
+}
+
 // Many tokens: the matrix units are what is kept busy.  A workgroup of WN x WM waves has BN = 16*MT*WN weight rows x
 // BM = 16*NT*WM tokens.  LDS holds the weights of 2D steps of 64 columns (1 KiB blocks as the blob has them: operand order) and
 // the activations of D chunks of 128 (1 KiB blocks of 8 tokens x 128 bytes, lane l of the loading wave fetching token l/8's
@@ -295,6 +302,11 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
         constexpr int E = 16 / sizeof(T), MG = 8 / (int)sizeof(T);   // elements of 16 bytes; row tiles whose 128 bytes of a token turn at a time
         typedef T vec_e __attribute__((ext_vector_type(E)));
         typedef T vec_4 __attribute__((ext_vector_type(4)));
+        // Rows of whole 16-byte pieces are not kept in the L2 (whose lines the operands are in, and which a launch ends with
+        // writing back): large tiles store past it (16000 x 2560 x 1280 fp32 77 us, so 70), the others through it (1024 x 2048 x
+        // 2048 10.1, so 9.1; past it 9.4).  Pieces at any other address share lines and their 32-byte sectors with their
+        // neighbours, which only the L2 can join: 11206 x 9405 x 136 bf16 92 us kept in the L2, 160 past it, 144 through it.
+        const bool pieces = (((uintptr_t)p.y | ((uintptr_t)p.ld_y * sizeof(T))) & 15) == 0;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const float sa = sc[2 * P::BN + (wm * NT + nt) * 16 + col];
@@ -319,10 +331,9 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
                     T *y = (T *)p.y + (int64_t)m * p.ld_y + r;
                     if (m < p.M) {
                         if (r + E <= p.rows) {
-                            // Not kept in the L2 (whose lines the operands are in, and which a launch ends with writing back): large tiles past
-                        // it (16000 x 2560 x 1280 fp32 77 us, now 70), the others through it (1024 x 2048 x 2048 10.1, now 9.1; past it 9.4)
-                        if (MT * WN >= 16) __builtin_nontemporal_store(v, (typename QrVec<T>::any *)y);
-                        else qr_store_through((float *)y, __builtin_bit_cast(v4f, v));
+                            if (!pieces) *(typename QrVec<T>::any *)y = v;
+                            else if (MT * WN >= 16) store_past((float *)y, __builtin_bit_cast(v4f, v));
+                            else qr_store_through((float *)y, __builtin_bit_cast(v4f, v));
                         } else {
 #pragma unroll
                             for (int e = 0; e < E; ++e)
