@@ -168,8 +168,9 @@ qrnnt_status qrnnt_quantize_act_rows(const float *x, int64_t rows, int32_t cols,
  * codes a value next to their border gets is decided by the exact quotient (ties to even), not by its fp32 rounding.
  *
  * Element types of the floating arrays of these and the following calls.  Pitches (ld_*) are in elements and at least
- * cols; rows may start at any element, 16-byte aligned ones are fastest.  Counts above 2^30 (rows of quantizers: 2^31 - 1)
- * and matrices of more than 2^60 elements are QRNNT_ERR_UNSUPPORTED. */
+ * cols; rows may start at any element, 16-byte aligned ones are fastest.  QRNNT_ERR_UNSUPPORTED: more than 2^31 - 1 rows
+ * or 2^30 columns to quantize, 2^28 rows or tokens of a linear layer, 2^21 utterances of a selection, 2^32 pieces of at most 16
+ * bytes x 4 rows (in place: all rows) of a reordering, matrices of more than 2^60 elements. */
 enum { QRNNT_F32 = 0, QRNNT_F16 = 1, QRNNT_BF16 = 2 };
 
 /* scale[r] = max_k |x[r,k]| / 127, q[r,k] = rne(127 x[r,k] / max_k |x[r,k]|).  x [device] [rows, cols] of `dtype` with
@@ -405,7 +406,8 @@ qrnnt_status qrnnt_beam_step(const float *score, const float *fused, int32_t B, 
  * or +inf has none.  Unfilled ranks get parent = token = -1, score = -inf.
  * score [device] fp32 [B,W]; logits [device] [B*W, V] of `dtype` with row pitch ld elements; finished [device] [B,W] or
  * NULL; finished_out [device] uint8 [B,n_out] or NULL: 1 where the parent was finished or the token is end_token (no
- * token: -1), 0 elsewhere and for unfilled ranks.  W <= 64, n_out <= 64, V <= 2^30, W*V < 2^31.  No output may overlap an input.
+ * token: -1), 0 elsewhere and for unfilled ranks.  W <= 64, n_out <= 64, B <= 2^21, V <= 2^30, W*V < 2^31.  No output may overlap an
+ * input.
  * workspace [device]: qrnnt_beam_select_workspace bytes (0 on bad sizes), 256-byte aligned; calls that may run at the
  * same time need workspaces of their own.  B = 0 does nothing. */
 size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, int32_t n_out);

@@ -505,13 +505,13 @@ void launch_linear_tokens(QrTokensLinear p, const QrTokensPlan &plan, hipStream_
     }
 }
 
-bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0 && w->rows <= 1 << 30 && w->cols > 0 && w->cols <= 131071; }
+bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0 && w->rows <= 1 << 28 && w->cols > 0 && w->cols <= 131071; }
 
 }  // namespace
 
 extern "C" size_t qrnnt_linear_tokens_workspace(const qrnnt_qmat *w, int32_t M)
 {
-    if (!tokens_weights_ok(w) || M <= 0 || M > 1 << 30) return 0;
+    if (!tokens_weights_ok(w) || M <= 0 || M > 1 << 28) return 0;
     const QrTokensPlan plan = plan_linear_tokens(w->rows, w->cols, M);
     const QrTokensPiece &last = plan.piece[plan.n - 1];   // (large tiles in front of it are not cut)
     return last.parts > 1 ? (size_t)last.parts * last.M * qr_round_up(w->rows, 4) * 4 : 0;
@@ -525,7 +525,7 @@ extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bi
     if (s != QRNNT_OK) return s;
     QR_REQUIRE(qr_is_dtype(y_dtype), QRNNT_ERR_RANGE);
     QR_REQUIRE(M >= 0 && ld_a >= qr_act_pitch(w->cols) && ld_a % 16 == 0 && ld_y >= w->rows, QRNNT_ERR_SHAPE);
-    QR_REQUIRE(qr_bits(w) == 8 && tokens_weights_ok(w) && M <= 1 << 30 && qr_pitch_ok(M, ld_y), QRNNT_ERR_UNSUPPORTED);
+    QR_REQUIRE(qr_bits(w) == 8 && tokens_weights_ok(w) && M <= 1 << 28 && qr_pitch_ok(M, ld_y), QRNNT_ERR_UNSUPPORTED);
     if (M == 0) return QRNNT_OK;
     QR_REQUIRE(a != nullptr && a_scale != nullptr && y != nullptr, QRNNT_ERR_NULL);
     const size_t e = qr_dtype_size(y_dtype), need = qrnnt_linear_tokens_workspace(w, M);
@@ -539,7 +539,7 @@ extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bi
     p.a = a;  p.s_a = a_scale;  p.ld_a = ld_a;  p.M = M;  p.y = y;  p.ld_y = ld_y;
     p.part = workspace;  p.ld_part = qr_round_up(w->rows, 4) / 4;
     const QrTokensPlan plan = plan_linear_tokens(w->rows, w->cols, M);
-    QR_REQUIRE(plan.piece[0].kind == FEW || TILE_COST[plan.piece[0].kind].tiles(w->rows, M) <= INT32_MAX, QRNNT_ERR_UNSUPPORTED);
+    QR_REQUIRE(plan.piece[0].kind == FEW || TILE_COST[plan.piece[0].kind].tiles(w->rows, M) < 1 << 23, QRNNT_ERR_UNSUPPORTED);   // (a grid has less than 2^32 threads)
     if (y_dtype == QRNNT_F32) launch_linear_tokens<float>(p, plan, (hipStream_t)stream);
     else if (y_dtype == QRNNT_F16) launch_linear_tokens<_Float16>(p, plan, (hipStream_t)stream);
     else launch_linear_tokens<__bf16>(p, plan, (hipStream_t)stream);

@@ -80,7 +80,7 @@ bool plan_reorder(QrReorderArgs &a)
         const int64_t groups = IN_PLACE ? 1 : (a.W_out + NR - 1) / NR;
         if (groups * a.B > INT32_MAX || pieces > INT64_MAX / 256 / groups / a.B) return false;
         end += (pieces * groups * a.B + 255) / 256;
-        if (end > INT32_MAX) return false;
+        if (end >= 1 << 24) return false;   // (a grid has less than 2^32 threads)
         a.end[k] = (unsigned)end;
     }
     return true;

@@ -179,6 +179,7 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
             take(u[p], w[p]);
         }
     } else {
+        double ss = 0.0;   // (a thread adds up any number of vectors)
         for (int c = t * V; c < cols; c += TPR * V) {
             float r[V], w[V];
             qr_load_vec(x + c, cols - c, 0.0f, u[0]);
@@ -187,7 +188,10 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
             else ones(w);
             form(c, u[0], r);
             take(u[0], w);
+            ss += (double)s.ss;
+            s.ss = 0.0f;
         }
+        s.ss = (float)ss;
     }
     s.reduce_wave(NORM);
     if (NW > 1) {
@@ -251,6 +255,24 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
     if (t == 0) a.scale[row] = NORM ? (peak * (1.0f / sqrtf(s.ss / (float)cols + a.eps))) / 127.0f : peak / 127.0f;
 }
 
+template <class T, bool NORM, int TPR, int PER>
+void launch_rows(QrTokenArgs a, hipStream_t st)
+{
+    constexpr int THREADS = TPR < 128 ? 256 : TPR, RPB = THREADS / TPR;
+    constexpr int64_t MOST = ((int64_t)1 << 31) / THREADS * RPB;   // rows of a launch: a grid has less than 2^32 threads
+    for (int64_t left = a.rows; left > 0; left -= MOST) {
+        a.rows = left < MOST ? left : MOST;
+        tokens_kernel<T, NORM, TPR, PER><<<(unsigned)((a.rows + RPB - 1) / RPB), THREADS, 0, st>>>(a);
+        a.x = (const T *)a.x + MOST * a.ld_x;
+        if (a.residual) {
+            a.residual = (const T *)a.residual + MOST * a.ld_res;
+            a.sum = (T *)a.sum + MOST * a.ld_sum;
+        }
+        a.q += MOST * a.ld_q;
+        a.scale += MOST;
+    }
+}
+
 template <class T, bool NORM>
 void launch_tokens(const QrTokenArgs &a, hipStream_t st)
 {
@@ -259,8 +281,7 @@ void launch_tokens(const QrTokenArgs &a, hipStream_t st)
     // residual 84 (90), 1280 fp32 19.5 with 64 threads, 20.5 with 256 (19.7), 2000 fp16 with residual 14.8 with 128, 17.7 with 256 (10.8),
     // 8192 bf16 with residual 34.9 with 512, 37.2 with 256 (33.1), 10000 bf16 27.0 with 256, 32.5 with 1024 (17.3).
     const int nv = (a.cols + V - 1) / V;
-#define QR_TOKENS(tpr, per) \
-    tokens_kernel<T, NORM, tpr, per><<<(unsigned)((a.rows + (tpr < 128 ? 256 / tpr : 1) - 1) / (tpr < 128 ? 256 / tpr : 1)), tpr < 128 ? 256 : tpr, 0, st>>>(a)
+#define QR_TOKENS(tpr, per) launch_rows<T, NORM, tpr, per>(a, st)
     if (nv <= 64) QR_TOKENS(64, 1);
     else if (nv <= 128) QR_TOKENS(64, 2);
     else if (nv <= 256) QR_TOKENS(128, 2);

@@ -548,7 +548,7 @@ void plan_select(int64_t rows, int V, int &n_parts, int &part)
 
 bool select_sizes_ok(int32_t B, int32_t W, int32_t V, int32_t K)
 {
-    return B >= 0 && W > 0 && V > 0 && K > 0 && W <= 64 && K <= MAX_OUT && (int64_t)W * V <= INT32_MAX && V <= 1 << 30 && (int64_t)B * W <= INT32_MAX;
+    return B >= 0 && W > 0 && V > 0 && K > 0 && W <= 64 && K <= MAX_OUT && (int64_t)W * V <= INT32_MAX && V <= 1 << 30 && B <= 1 << 21;   // (a grid has less than 2^32 threads)
 }
 
 size_t heads_bytes(int64_t rows, int n_parts) { return ((size_t)rows * n_parts * sizeof(QrPartHead) + 255) / 256 * 256; }

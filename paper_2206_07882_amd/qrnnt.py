@@ -267,6 +267,7 @@ def linear_quant(w: QMat, bias: Optional[torch.Tensor], a_scale: float, a: torch
 
 
 F32, F16, BF16 = 0, 1, 2
+_INT_MAX = 2 ** 31 - 1
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 
@@ -301,6 +302,8 @@ def _matrix(t: torch.Tensor, dtype, rows: int, cols: int):
         if rows > 1:
             raise ValueError("rows must not overlap")
         pitch = cols
+    if rows > _INT_MAX or cols > _INT_MAX or pitch > _INT_MAX and dtype is torch.int8:   # (ctypes would drop the upper bits)
+        raise ValueError(f"a matrix of {rows} x {cols}, pitch {pitch}, is too large")
     return t.data_ptr(), pitch
 
 
@@ -630,6 +633,8 @@ def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] 
     if rows != B * W:
         raise ValueError(f"expected logits of {B * W} hypotheses, got {rows}")
     K = W if n_out is None else n_out
+    if K > 64:
+        _check(7, "qrnnt_beam_select")
     dev = score.device
     pf = None
     if finished is not None:
@@ -671,6 +676,8 @@ class StateGroup:
         pairs = [s if isinstance(s, (tuple, list)) else (s, s) for s in states]
         self._keep = pairs
         self.n = len(pairs)
+        if max(self.B, self.W, self.W_out) > _INT_MAX:
+            raise ValueError("too many hypotheses")
         if not 1 <= self.n <= MAX_STATES:
             raise ValueError(f"1 to {MAX_STATES} states, got {self.n}")
         self.arr = (CStateRows * self.n)()

@@ -150,3 +150,29 @@ def test_many_rows(gpu_lib):
     codes, scale = q.quantize_tokens(x)
     tail = x[-50:].cpu()
     check(codes[-50:], scale[-50:], plain64.token_codes(tail.double().numpy()), 24, torch.float32, False)
+
+
+def test_more_rows_than_a_grid_has_threads_for(gpu_lib):
+    """2^26 + 70 rows of 64 threads each are more than 2^32 threads."""
+    q, rows = gpu_lib, (1 << 26) + 70
+    x = torch.randn((rows, 1), device=DEV, dtype=torch.float16, generator=torch.Generator(DEV).manual_seed(1))
+    codes, scale = q.quantize_tokens(x)
+    at = torch.cat([torch.arange(5), torch.arange(1 << 25, (1 << 25) + 5), torch.arange(rows - 140, rows)]).to(DEV)
+    want = plain64.token_codes(x[at].cpu().double().numpy())
+    check(codes[at], scale[at], want, 1, torch.float16, False)
+    assert torch.equal(codes[:, 0].float(), 127.0 * torch.sign(x[:, 0].float()))
+    assert not codes[:, 1:].any()
+
+
+@pytest.mark.parametrize("value", [1.1, 1.3330078125, 0.7])
+def test_long_rows_of_equal_values(gpu_lib, value):
+    """Sums of very many equal squares, which fp32 would round to the same side for long stretches: a vector's squares are added
+    in fp32, vectors in fp64, 6 + 16 sums of fp32 join them."""
+    q, cols = gpu_lib, (1 << 24) + 5
+    x = torch.full((1, cols), value, dtype=torch.float32)
+    codes, scale, _ = q.rms_norm_quant(x.to(DEV), None, 0.0)
+    h = float(x[0, 0])
+    want = h / np.sqrt(h * h) / 127.0
+    # 4 + 1 + 6 + 16 + 2 roundings halved by the root, 4 behind it; the count of columns itself is rounded to fp32: half of one
+    assert abs(float(scale[0]) - want) <= ((4 + 1 + 6 + 16 + 2) / 2 + 4 + 0.5) * 2.0 ** -24 * want
+    assert bool((codes[0, :cols] == 127).all()) and not bool(codes[0, cols:].any())

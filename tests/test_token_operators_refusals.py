@@ -52,6 +52,8 @@ def test_linear_tokens(lib):
     assert f(M=-1) == SHAPE and f(ld_a=96) == SHAPE and f(ld_a=120) == SHAPE and f(ld_y=63) == SHAPE and f(_mat(rows=0)) == SHAPE
     assert f(a=0x10008) == ALIGN and f(y=0x40002) == ALIGN and f(y=0x40001, dt=1) == ALIGN and f(bias=0x5001) == ALIGN and f(sa=0x3002) == ALIGN
     assert f(M=(1 << 30) + 1) == UNSUPPORTED and f(_mat(rows=(1 << 30) + 1), ld_y=1 << 31) == UNSUPPORTED and f(ld_y=1 << 60) == UNSUPPORTED
+    assert f(M=(1 << 28) + 1) == UNSUPPORTED and f(_mat(rows=(1 << 28) + 1), ld_y=1 << 31) == UNSUPPORTED
+    assert f(_mat(rows=1 << 20), M=1 << 20, ld_y=1 << 20) == UNSUPPORTED   # more tiles than a grid has
     assert f(M=0) == OK and f(M=0, a=None, y=None) == OK
     assert lib.qrnnt_linear_tokens_workspace(None, 4) == 0 and lib.qrnnt_linear_tokens_workspace(C.byref(_mat()), 0) == 0
     for rows, cols, M in ((64, 131071, 33), (64, 8192, 16), (100, 4096, 200), (8192, 8192, 8192)):
@@ -73,6 +75,7 @@ def test_beam_select(lib):
     assert f(B=-1) == SHAPE and f(W=0) == SHAPE and f(V=0) == SHAPE and f(n=0) == SHAPE and f(ld=99) == SHAPE
     assert f(W=65) == UNSUPPORTED and f(n=65) == UNSUPPORTED and f(W=64, V=1 << 25, ld=1 << 25) == UNSUPPORTED and f(B=1 << 30, W=4) == UNSUPPORTED
     assert f(W=1, V=(1 << 30) + 1, ld=1 << 31) == UNSUPPORTED and f(ld=1 << 60) == UNSUPPORTED
+    assert f(B=(1 << 21) + 1, W=1) == UNSUPPORTED and qrnnt.beam_select_workspace((1 << 21) + 1, 1, 100, 1) == 0
     assert f(score=0x1002) == ALIGN and f(logits=0x10001, dt=1) == ALIGN and f(par=0x2001) == ALIGN and f(ws=0x100008) == ALIGN
     need = qrnnt.beam_select_workspace(2, 4, 100, 4)
     assert need > 0 and f(size=need - 1) == WORKSPACE
@@ -99,7 +102,19 @@ def test_reorder_states(lib):
     assert f([good, S(0x30000, 0x20040, 64, 64, 64)]) == RANGE and f([good, S(0x20000, 0x30000, 64, 64, 64)]) == RANGE
     assert f([S(0x10000, 0x10000, 40, 64, 64), S(0x10020, 0x10020, 32, 64, 64)]) == RANGE
     assert f([good], parent=0x20020) == RANGE
+    assert f([S(1 << 44, 1 << 45, 15, 15, 15)], B=1 << 29, W=1, W_out=1, parent=1 << 46) == UNSUPPORTED   # 15 single bytes a row
     assert f([good], B=0) == OK
+
+
+def test_wrappers_refuse_counts_that_do_not_fit_32_bits():
+    x = torch.zeros(1, dtype=torch.int8)
+    for rows, cols, pitch in ((1, 1 << 31, 1 << 31), (1 << 31, 1, 1), (2, 16, 1 << 31)):
+        with pytest.raises(ValueError):
+            qrnnt._matrix(torch.empty_strided((rows, cols), (pitch, 1), dtype=torch.int8, device="meta"), torch.int8, rows, cols)
+    with pytest.raises(ValueError):
+        qrnnt.StateGroup([x], 1 << 32, 1)
+    with pytest.raises(RuntimeError):
+        qrnnt._check(UNSUPPORTED, "qrnnt_beam_select")
 
 
 def test_wrappers_refuse_tensors_that_are_not_on_the_gpu():
