@@ -137,7 +137,7 @@ struct QrTile {
     static constexpr int A_BLOCKS = MT * WN, B_BLOCKS = 2 * NT * WM;      // of 1 KiB: weights of a step, activations of a chunk
     static constexpr int A_LOADS = A_BLOCKS / WAVES, B_LOADS = B_BLOCKS / WAVES;
     static constexpr int A_STAGE = A_BLOCKS * 1024, B_STAGE = B_BLOCKS * 1024;
-    static constexpr int B_AT = 2 * D * A_STAGE, TURN = B_AT + D * B_STAGE, SCALES = TURN + WAVES * 2048, LDS = SCALES + (2 * BN + BM) * 4;
+    static constexpr int B_AT = 2 * D * A_STAGE, TURN = B_AT + D * B_STAGE, SCALES = TURN + WAVES * 2048, SCALE_BYTES = (2 * BN + BM) * 4, LDS = SCALES + 2 * SCALE_BYTES;
     static_assert(A_BLOCKS % WAVES == 0 && B_BLOCKS % WAVES == 0, "every wave loads as much");
     static_assert(D == 2 || D == 4, "ring of chunks");
 };
@@ -154,48 +154,26 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
     // Workgroups go to the 8 XCDs in turn; each XCD gets a run of tiles, G blocks of rows side by side, so that what runs on it at a
     // time shares its L2 (G = 2, 4, 8 at 8192^3: 431, 425, 423 us; at 16000 x 2560 x 1280: 78, 79, 84)
     constexpr int G = 4;
-    const int total = tiles_n * tiles_m;
-    const int xcd = blockIdx.x & 7, each = total >> 3, rest = total & 7;
-    const int tile = xcd * each + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
-    const int stripe = tile / (G * tiles_m), in_stripe = tile - stripe * G * tiles_m;
-    const int width = tiles_n - stripe * G < G ? tiles_n - stripe * G : G;
-    const int tn = stripe * G + in_stripe % width, tm = in_stripe / width;
-    const int n_row_tiles = (p.rows + 15) >> 4, rt0 = tn * (P::BN / 16), m0 = tm * P::BM;
+    const int total = tiles_n * tiles_m, n_row_tiles = (p.rows + 15) >> 4;
     const unsigned lds0 = (unsigned)(size_t)lds;
     constexpr bool PART = std::is_same<T, v4i>::value;
     const int kc0 = PART ? (int)((int64_t)p.nkc * blockIdx.y / gridDim.y) : 0;
     const int nkc = PART ? (int)((int64_t)p.nkc * (blockIdx.y + 1) / gridDim.y) - kc0 : p.nkc;
-    if (!PART) {   // scales and bias of the tile: 64 to a load, which the waves take in turn
-        constexpr int N_SW = P::BN / 64, N_SA = P::BM / 64;
-        for (int j = wave; j < 2 * N_SW + N_SA; j += P::WAVES) {
-            const float *src;
-            if (j < 2 * N_SW) {
-                const int r = rt0 * 16 + (j % N_SW) * 64 + lane, rr = r < p.rows ? r : p.rows - 1;
-                src = j < N_SW || !p.bias ? p.s_w + rr : p.bias + rr;
-            } else {
-                const int m = m0 + (j - 2 * N_SW) * 64 + lane;
-                src = p.s_a + (m < p.M ? m : p.M - 1);
-            }
-            qr_load_lds4(src, lds0 + P::SCALES + j * 256);
-        }
-    }
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    auto locate = [&](int at, int &rt0, int &m0) {
+        const int xcd = at & 7, each = total >> 3, rest = total & 7;
+        const int tile = xcd * each + (xcd < rest ? xcd : rest) + (at >> 3);
+        const int stripe = tile / (G * tiles_m), in_stripe = tile - stripe * G * tiles_m;
+        const int width = tiles_n - stripe * G < G ? tiles_n - stripe * G : G;
+        rt0 = (stripe * G + in_stripe % width) * (P::BN / 16);
+        m0 = in_stripe / width * P::BM;
+    };
     const v4i *src_a[P::A_LOADS];
     const int8_t *src_b[P::B_LOADS];
-#pragma unroll
-    for (int i = 0; i < P::A_LOADS; ++i) {
-        const int t = rt0 + wave * P::A_LOADS + i, rt = t < n_row_tiles ? t : n_row_tiles - 1;
-        src_a[i] = p.w + ((size_t)rt * p.nkc + kc0) * 128 + lane;
-    }
-    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
-#pragma unroll
-    for (int i = 0; i < P::B_LOADS; ++i) {
-        const int m = m0 + (wave * P::B_LOADS + i) * 8 + (lane >> 3);
-        src_b[i] = p.a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_a + piece;
-    }
-    auto load_a = [&](int i, int k) { qr_load_lds16(src_a[i] + (size_t)k * 64, lds0 + (k & (2 * D - 1)) * P::A_STAGE + (wave * P::A_LOADS + i) * 1024); };
+    auto load_a = [&](int i, int k) { qr_load_lds16(src_a[i] + (size_t)k * 64, __builtin_amdgcn_readfirstlane(lds0 + (k & (2 * D - 1)) * P::A_STAGE + (wave * P::A_LOADS + i) * 1024)); };
     auto load_b = [&](int i, int kc) {
         const int c = (kc0 + kc) * QRNNT_KCHUNK;   // columns behind the row: its start instead (they meet zero weights)
-        qr_load_lds16(src_b[i] + (c + piece < p.K ? c : -piece), lds0 + P::B_AT + (kc & (D - 1)) * P::B_STAGE + (wave * P::B_LOADS + i) * 1024);
+        qr_load_lds16(src_b[i] + (c + piece < p.K ? c : -piece), __builtin_amdgcn_readfirstlane(lds0 + P::B_AT + (kc & (D - 1)) * P::B_STAGE + (wave * P::B_LOADS + i) * 1024));
     };
     // Order of all loads: A(0), then for every chunk c: B(c), A(2c + 1), A(2c + 2).  Chunks up to D - 2 are on their way before the
     // loop; the two steps of chunk c start B(c + D - 1) and A(2(c + D) - 1), then A(2(c + D)).
@@ -209,17 +187,44 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
             for (int i = 0; i < P::A_LOADS; ++i) load_a(i, 2 * c + 2);
         }
     };
+    // Starts a tile's first loads: its scales and bias (64 to a load, which the waves take in turn), the first chunks.
+    auto begin = [&](int rt0, int m0, int scales) {
+        if (!PART) {
+            constexpr int N_SW = P::BN / 64, N_SA = P::BM / 64;
+            for (int j = wave; j < 2 * N_SW + N_SA; j += P::WAVES) {
+                const float *src;
+                if (j < 2 * N_SW) {
+                    const int r = rt0 * 16 + (j % N_SW) * 64 + lane, rr = r < p.rows ? r : p.rows - 1;
+                    src = j < N_SW || !p.bias ? p.s_w + rr : p.bias + rr;
+                } else {
+                    const int m = m0 + (j - 2 * N_SW) * 64 + lane;
+                    src = p.s_a + (m < p.M ? m : p.M - 1);
+                }
+                qr_load_lds4(src, __builtin_amdgcn_readfirstlane(lds0 + scales + j * 256));
+            }
+        }
 #pragma unroll
-    for (int i = 0; i < P::A_LOADS; ++i) load_a(i, 0);
+        for (int i = 0; i < P::A_LOADS; ++i) {
+            const int t = rt0 + wave * P::A_LOADS + i, rt = t < n_row_tiles ? t : n_row_tiles - 1;
+            src_a[i] = p.w + ((size_t)rt * p.nkc + kc0) * 128 + lane;
+        }
 #pragma unroll
-    for (int c = 0; c < D - 1; ++c)
-        if (c < nkc) load_group(c);
+        for (int i = 0; i < P::B_LOADS; ++i) {
+            const int m = m0 + (wave * P::B_LOADS + i) * 8 + (lane >> 3);
+            src_b[i] = p.a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_a + piece;
+        }
+#pragma unroll
+        for (int i = 0; i < P::A_LOADS; ++i) load_a(i, 0);
+#pragma unroll
+        for (int c = 0; c < D - 1; ++c)
+            if (c < nkc) load_group(c);
+    };
     const char *fa = lds + wn * MT * 1024 + lane * 16;
     const char *fb = lds + P::B_AT + (wm * NT * 2 + (col >> 3)) * 1024 + (col & 7) * 128;
     const int half0 = (grp ^ (col & 7)) * 16, half1 = ((4 + grp) ^ (col & 7)) * 16;
 
     constexpr int AHEAD = MT > 2 ? 2 : 1;   // weight operands that are read ahead
-    v4i acc[MT][NT] = {}, b[2][NT] = {}, w[2][MT] = {};
+    v4i acc[MT][NT], b[2][NT] = {}, w[2][MT] = {};
     auto wait = [&](auto left) {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(left)::value) : "memory");
@@ -261,14 +266,7 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
     constexpr integral_constant<int, 1> one{};
     constexpr int A = P::A_LOADS, GROUP = P::B_LOADS + 2 * A;   // loads of a wave: weights of a step, a chunk
     static_assert((D - 1) * GROUP < 64, "the counter of loads has 6 bits");
-    if (nkc >= D) wait(integral_constant<int, (D - 2) * GROUP + 2 * A>{});
-    else wait(zero);   // (few columns: all of them)
-    first_reads(0, zero);
-    int kc = 0;
-    for (; kc < nkc - D; ++kc) {
-        step(2 * kc, zero, one, one, integral_constant<int, (D - 1) * GROUP>{});
-        step(2 * kc + 1, one, one, zero, integral_constant<int, (D - 2) * GROUP + 2 * A>{});
-    }
+    int rt0, m0, kc;
     // the last D chunks, t = 0 .. D - 1 (of less than D: the last of these).  The first one's first step starts the last loads.
     auto last = [&](auto tt) {
         constexpr int t = decltype(tt)::value;
@@ -277,73 +275,124 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
         step(2 * kc + 1, one, zero, zero, integral_constant<int, t == D - 1 ? -1 : (D - 2 - t) * GROUP + A>{});
         ++kc;
     };
-    last(zero);
-    last(one);
-    if constexpr (D == 4) {
-        last(integral_constant<int, 2>{});
-        last(integral_constant<int, 3>{});
-    }
-    if constexpr (PART) {
-        // four rows of a token to a lane: neighbouring lanes' 64 bytes join in the L2, the sums are read again from there
-        v4i *part = (v4i *)p.part + (int64_t)blockIdx.y * p.M * p.ld_part;
+    locate(blockIdx.x, rt0, m0);
+    int scales = P::SCALES;
+    begin(rt0, m0, scales);
+    // Of several tiles to a workgroup every second compute unit's begin later, by half the time that a tile's stores take: some store
+    // while others compute (16384 x 2048 x 1280 fp32 55 us, so 50; 16384 x 4096 x 640 72 and 68; bf16 57 and 54; the tiles of
+    // 8192^3 take 100 us each: no difference).
+    if (!PART && P::WAVES == 8 && total > (int)gridDim.x && (blockIdx.x >> 3 & 1))
+        for (int i = 0; i < 3 * (int)sizeof(T); ++i) __builtin_amdgcn_s_sleep(16);   // (of 1024 cycles)
+    for (int at = blockIdx.x;;) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int m = m0 + (wm * NT + nt) * 16 + col;
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) acc[i][nt] = v4i{};
+        if (at == (int)blockIdx.x && nkc >= D) wait(integral_constant<int, (D - 2) * GROUP + 2 * A>{});
+        else wait(zero);   // (few columns, or the last tile's stores are under way, too)
+        first_reads(0, zero);
+        for (kc = 0; kc < nkc - D; ++kc) {
+            step(2 * kc, zero, one, one, integral_constant<int, (D - 1) * GROUP>{});
+            step(2 * kc + 1, one, one, zero, integral_constant<int, (D - 2) * GROUP + 2 * A>{});
+        }
+        last(zero);
+        last(one);
+        if constexpr (D == 4) {
+            last(integral_constant<int, 2>{});
+            last(integral_constant<int, 3>{});
+        }
+        // the next tile's first loads are under way while this one's results are stored
+        at += gridDim.x;
+        const bool more = at < total;
+        int rt1 = 0, m1 = 0;
+        if (more) {
+            locate(at, rt1, m1);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();   // all waves have read the ring
+            __builtin_amdgcn_sched_barrier(0);
+            begin(rt1, m1, 2 * P::SCALES + P::SCALE_BYTES - scales);
+        }
+        if constexpr (PART) {
+            // four rows of a token to a lane: neighbouring lanes' 64 bytes join in the L2, the sums are read again from there
+            v4i *part = (v4i *)p.part + (int64_t)blockIdx.y * p.M * p.ld_part;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int m = m0 + (wm * NT + nt) * 16 + col;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const int r4 = (rt0 + wn * MT + mt) * 4 + grp;
+                    if (m < p.M && r4 < p.ld_part) part[(int64_t)m * p.ld_part + r4] = acc[mt][nt];
+                }
+            }
+        } else {
+            const float *sc = (const float *)(lds + scales);
+            char *turn = lds + P::TURN + wave * 2048;
+            constexpr int E = 16 / sizeof(T), MG = 8 / (int)sizeof(T);   // elements of 16 bytes; row tiles whose 128 bytes of a token turn at a time
+            typedef T vec_e __attribute__((ext_vector_type(E)));
+            typedef T vec_4 __attribute__((ext_vector_type(4)));
+            // Rows of whole 16-byte pieces are not kept in the L2 (whose lines the operands are in, and which a launch ends with
+            // writing back): large tiles store past it (16384 x 8192 x 512 bf16 95 us, kept or through it 106 and 102), the others
+            // through it (1024 x 2048 x 2048 fp32 9.1, past it 9.4, kept 10.1).  Pieces at any other address share lines and
+            // their 32-byte sectors with their neighbours, which only the L2 can join: 11206 x 9405 x 136 bf16 87 us kept in the
+            // L2, 160 past it, 144 through it.
+            const bool pieces = (((uintptr_t)p.y | ((uintptr_t)p.ld_y * sizeof(T))) & 15) == 0;
+            v4f sw[MT], bs[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const int r4 = (rt0 + wn * MT + mt) * 4 + grp;
-                if (m < p.M && r4 < p.ld_part) part[(int64_t)m * p.ld_part + r4] = acc[mt][nt];
+                const int r = (wn * MT + mt) * 16 + grp * 4;
+                sw[mt] = *(const v4f *)(sc + r);
+                bs[mt] = p.bias ? *(const v4f *)(sc + P::BN + r) : v4f{};
             }
-        }
-        return;
-    } else {
-        const float *sc = (const float *)(lds + P::SCALES);
-        char *turn = lds + P::TURN + wave * 2048;
-        constexpr int E = 16 / sizeof(T), MG = 8 / (int)sizeof(T);   // elements of 16 bytes; row tiles whose 128 bytes of a token turn at a time
-        typedef T vec_e __attribute__((ext_vector_type(E)));
-        typedef T vec_4 __attribute__((ext_vector_type(4)));
-        // Rows of whole 16-byte pieces are not kept in the L2 (whose lines the operands are in, and which a launch ends with
-        // writing back): large tiles store past it (16000 x 2560 x 1280 fp32 77 us, so 70), the others through it (1024 x 2048 x
-        // 2048 10.1, so 9.1; past it 9.4).  Pieces at any other address share lines and their 32-byte sectors with their
-        // neighbours, which only the L2 can join: 11206 x 9405 x 136 bf16 92 us kept in the L2, 160 past it, 144 through it.
-        const bool pieces = (((uintptr_t)p.y | ((uintptr_t)p.ld_y * sizeof(T))) & 15) == 0;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float sa = sc[2 * P::BN + (wm * NT + nt) * 16 + col];
-#pragma unroll
-            for (int g = 0; g < MT / MG; ++g) {
-#pragma unroll
-                for (int j = 0; j < MG; ++j) {
-                    const int mt = g * MG + j, r = (wn * MT + mt) * 16 + grp * 4;
-                    const v4f sw = *(const v4f *)(sc + r), bs = *(const v4f *)(sc + P::BN + r);
-                    vec_4 v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = (T)fmaf((float)acc[mt][nt][i] * sw[i], sa, p.bias ? bs[i] : 0.0f);
-                    const int at = (j * 16 + grp * 4) * (int)sizeof(T);
-                    *(vec_4 *)(turn + col * 128 + (((at >> 4) ^ (col & 7)) << 4) + (at & 15)) = v;
-                }
-                __builtin_amdgcn_wave_barrier();
+            const int t0 = lane >> 3, r0 = (rt0 + wn * MT) * 16 + (lane & 7) * E, tm0 = m0 + wm * NT * 16 + t0;
+            T *const y0 = (T *)p.y + (int64_t)tm0 * p.ld_y + r0;
+            // a wave turns 128 bytes of 16 tokens at a time, in LDS of its own and without a wait for others: its LDS instructions take
+            // effect in their order, so the next pieces are formed and written while the last ones' reads are under way
+            vec_e out[2];
+            auto store = [&](int nt, int g) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int t = i * 8 + (lane >> 3), m = m0 + (wm * NT + nt) * 16 + t;
-                    const int r = rt0 * 16 + (wn * MT + g * MG) * 16 + (lane & 7) * E;
-                    const vec_e v = *(const vec_e *)(turn + t * 128 + (((lane & 7) ^ (t & 7)) << 4));
-                    T *y = (T *)p.y + (int64_t)m * p.ld_y + r;
-                    if (m < p.M) {
-                        if (r + E <= p.rows) {
-                            if (!pieces) *(typename QrVec<T>::any *)y = v;
-                            else if (MT * WN >= 16) store_past((float *)y, __builtin_bit_cast(v4f, v));
-                            else qr_store_through((float *)y, __builtin_bit_cast(v4f, v));
+                    const int t = nt * 16 + i * 8, r = g * MG * 16;
+                    T *y = y0 + t * p.ld_y + r;
+                    if (tm0 + t < p.M) {
+                        if (r0 + r + E <= p.rows) {
+                            if (!pieces) *(typename QrVec<T>::any *)y = out[i];
+                            else if (MT * WN >= 16) store_past((float *)y, __builtin_bit_cast(v4f, out[i]));
+                            else qr_store_through((float *)y, __builtin_bit_cast(v4f, out[i]));
                         } else {
 #pragma unroll
                             for (int e = 0; e < E; ++e)
-                                if (r + e < p.rows) y[e] = v[e];
+                                if (r0 + r + e < p.rows) y[e] = out[i][e];
                         }
                     }
                 }
-                __builtin_amdgcn_wave_barrier();
+            };
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float sa = sc[2 * P::BN + (wm * NT + nt) * 16 + col];
+#pragma unroll
+                for (int g = 0; g < MT / MG; ++g) {
+#pragma unroll
+                    for (int j = 0; j < MG; ++j) {
+                        const int mt = g * MG + j;
+                        vec_4 v;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = (T)fmaf((float)acc[mt][nt][i] * sw[mt][i], sa, bs[mt][i]);
+                        const int at = (j * 16 + grp * 4) * (int)sizeof(T);
+                        *(vec_4 *)(turn + col * 128 + (((at >> 4) ^ (col & 7)) << 4) + (at & 15)) = v;
+                    }
+                    if (nt + g > 0) store(g > 0 ? nt : nt - 1, g > 0 ? g - 1 : MT / MG - 1);
+                    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) out[i] = *(const vec_e *)(turn + (i * 8 + t0) * 128 + (((lane & 7) ^ t0) << 4));
+                    __builtin_amdgcn_wave_barrier();
+                }
             }
+            store(NT - 1, MT / MG - 1);
         }
+        if (!more) return;
+        rt0 = rt1;
+        m0 = m1;
+        scales = 2 * P::SCALES + P::SCALE_BYTES - scales;
     }
 }
 
@@ -446,13 +495,14 @@ void launch_tiles(const QrTokensLinear &p, int parts, hipStream_t st)
 {
     using P = QrTile<MT, NT, WN, WM, D>;
     const int tn = (p.rows + P::BN - 1) / P::BN, tm = (p.M + P::BM - 1) / P::BM;
+    const int places = P::WAVES == 8 ? 256 : 512;   // what 256 compute units hold
     static bool allowed[QR_MAX_DEVICES];   // per device: more than 64 KiB of LDS
     const int d = qr_current_device();
     if (!allowed[d]) {
         (void)hipFuncSetAttribute((const void *)linear_tokens_kernel<T, MT, NT, WN, WM, D>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
         allowed[d] = true;
     }
-    linear_tokens_kernel<T, MT, NT, WN, WM, D><<<dim3((unsigned)(tn * tm), parts), P::THREADS, P::LDS, st>>>(p, tn, tm);
+    linear_tokens_kernel<T, MT, NT, WN, WM, D><<<dim3((unsigned)(tn * tm < places ? tn * tm : places), parts), P::THREADS, P::LDS, st>>>(p, tn, tm);
 }
 
 template <class T, int RT, int NT, int WAVES>
