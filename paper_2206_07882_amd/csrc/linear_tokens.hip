@@ -429,23 +429,25 @@ struct QrTokensPlan {
     int n;
 };
 
-// Tiles by what they were measured to take (us): a chunk of 128 columns while at most half of the places on the device are
-// taken, and with all of them; what a tile costs besides.  256 compute units hold one large tile each, or two of the others.
+// Tiles by what they were measured to take (us), over 140 layers of 64 to 8192 columns, 64 to 32000 rows and 40 to 16384 tokens (80 % of
+// them within a tenth; the kind chosen by it is on average half a per cent slower than the best): a chunk of 128 columns while
+// at most half of the places on the device are taken, and with all of them; what a tile costs besides; what a launch does.
+// 256 compute units hold one large tile each, or two of the others.
 struct QrTileCost {
     int size, places;
-    float alone, full, fixed;
+    float alone, full, fixed, start;
     float time(int64_t tiles, int chunks) const
     {
         const int64_t rounds = tiles / places, rest = tiles % places;
-        return rounds * (chunks * full + fixed) + (rest == 0 ? 0.0f : chunks * (rest <= places / 2 ? alone : full) + fixed);
+        return start + rounds * (chunks * full + fixed) + (rest == 0 ? 0.0f : chunks * (rest <= places / 2 ? alone : full) + fixed);
     }
     int64_t tiles(int rows, int M) const { return (int64_t)((rows + size - 1) / size) * ((M + size - 1) / size); }
 };
-constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.28f, 0.43f, 1.5f}, {128, 512, 0.65f, 1.1f, 4.5f}, {256, 256, 1.0f, 1.4f, 9.0f}};
+constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.26f, 0.43f, 1.1f, 1.9f}, {128, 512, 0.66f, 1.1f, 3.6f, 0.6f}, {256, 256, 1.03f, 1.4f, 9.6f, -1.4f}};
 
 // Measured at each choice (us; few / small / middle / large): 32 x 1000 x 1000 (tokens x rows x columns) 3.4 / 4.5; 48 x 16000 x
-// 4000 14.1 / 12.3; 200 x 8000 x 500 - / 4.5 / 7.7 / 12.9; 4000 x 1024 x 4096 - / 30.6 / 26.8 / 39.9; 2000 x 5000 x 3000 - / 59 / 46 /
-// 37; 8192^3 - / 879 / 569 / 403.  300 x 1024 x 8192 on small tiles whole 20.7, in two parts 15.1, in four 12.8.
+// 4000 14.1 / 11.9; 200 x 8000 x 500 - / 4.4 / 6.1 / 12.3; 4000 x 1024 x 4096 - / 30.8 / 27.2 / 39.1; 2000 x 5000 x 3000 - / 59 / 46 /
+// 37; 8192^3 - / 901 / 584 / 396.  300 x 1024 x 8192 on small tiles whole 21.2, in two parts 15.1, in four 12.9.
 QrTokensPiece plan_piece(int rows, int K, int M, float &least)
 {
     const int nkc = qr_round_up(K, QRNNT_KCHUNK) / QRNNT_KCHUNK;
@@ -471,8 +473,8 @@ QrTokensPlan plan_linear_tokens(int rows, int K, int M)
     if (M <= 16 || (M <= 32 && (rows <= 16384 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= 4096)) return {{{FEW, 1, M}}, 1};
     float least;
     QrTokensPlan best = {{plan_piece(rows, K, M, least)}, 1};
-    // whole rounds of large tiles first, what would leave a round part empty in a launch of its own (6000 x 3000 x 5000: 114 us
-    // in two rounds, 93 in one and middle tiles; 2100 x 8192 x 4096 88 and 66)
+    // whole rounds of large tiles first, what would leave a round part empty in a launch of its own (6000 x 3000 x 5000: 121 us
+    // in two rounds, 96 in one and middle tiles; 2100 x 8192 x 4096 87 and 65)
     const QrTileCost &c = TILE_COST[LARGE];
     const int nkc = qr_round_up(K, QRNNT_KCHUNK) / QRNNT_KCHUNK, across = (rows + c.size - 1) / c.size;
     const int64_t rounds = c.tiles(rows, M) / c.places;
@@ -481,7 +483,7 @@ QrTokensPlan plan_linear_tokens(int rows, int K, int M)
         if (first < c.size || first >= M) continue;
         float rest;
         const QrTokensPiece second = plan_piece(rows, K, M - (int)first, rest);
-        const float t = c.time(c.tiles(rows, (int)first), nkc) + rest + 2.0f;
+        const float t = c.time(c.tiles(rows, (int)first), nkc) + rest + 3.5f;   // (the second launch waits for the first one's last stores)
         if (t < least) {
             least = t;
             best = {{{LARGE, 1, (int)first}, second}, 2};
