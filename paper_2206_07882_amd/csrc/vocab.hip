@@ -159,14 +159,16 @@ __device__ __forceinline__ void write_ranks(const QrSelectArgs &a, int b, QrPick
 }
 
 // A thread's NV vectors of n logits: vector v of thread t of `threads` starts at element (v * threads + t) * V, wherever the row begins
-// in memory (sums have to come out the same for the same row); -inf behind the end.  Kept in their own type: as fp32 16-bit logits
-// would take twice the registers.
+// in memory (sums have to come out the same for the same row); -inf behind the end.
 template <class T, int NV>
 struct QrLogits {
-    static constexpr int V = QrVec<T>::N, PER = NV * V;
-    typename QrVec<T>::type raw[NV];
+    static constexpr int V = QrVec<T>::N, PER = NV * V, GROUP = 8, NG = PER / GROUP;
+    static_assert(PER % GROUP == 0, "whole groups");
+    float f[PER];
+    float best[NG];   // largest of 8 (NaN is passed over)
     __device__ __forceinline__ void load(const T *x, int n, int t, int threads)
     {
+        typename QrVec<T>::type raw[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * threads + t) * V;
@@ -177,48 +179,52 @@ struct QrLogits {
                 for (int i = 0; i < V; ++i) raw[v][i] = c + i < n ? x[c + i] : (T)-INFINITY;
             }
         }
-    }
-    __device__ __forceinline__ float operator[](int i) const { return (float)raw[i / V][i % V]; }
-    // Before a further pass: what the last one made of the logits is not kept.
-    __device__ __forceinline__ void anew()
-    {
-        if (sizeof(T) == 2)
 #pragma unroll
-            for (int v = 0; v < NV; ++v) asm volatile("" : "+v"(raw[v]));
-    }
-    __device__ __forceinline__ float largest() const   // (NaN is passed over)
-    {
-        float m = -INFINITY;
+        for (int i = 0; i < PER; ++i) f[i] = (float)raw[i / V][i % V];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) m = fmaxf(m, (*this)[i]);
+        for (int g = 0; g < NG; ++g) {
+            best[g] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) best[g] = fmaxf(best[g], f[g * GROUP + i]);
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return f[i]; }
+    __device__ __forceinline__ float largest() const
+    {
+        float m = best[0];
+#pragma unroll
+        for (int g = 1; g < NG; ++g) m = fmaxf(m, best[g]);
         return m;
     }
     __device__ __forceinline__ float sum_exp(float top) const
     {
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) s += qr_exp((*this)[i] - top);
+        for (int i = 0; i < PER; ++i) s += qr_exp(f[i] - top);
         return s;
     }
-    // take(logit, i) for those that are not below `least`.  A thread that has any most often has one, its largest: that one is found
+    // take(logit, i) for those that are not below `least`.  A group that has any most often has one, its largest: that one is found
     // without a branch for each.
     template <class Take>
-    __device__ __forceinline__ void hits(float largest, float least, Take &&take) const
+    __device__ __forceinline__ void hits(float least, Take &&take) const
     {
-        if (!(largest >= least)) return;
-        int n = 0, at = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const bool hit = (*this)[i] >= least;
-            n += hit ? 1 : 0;
-            at = hit ? i : at;
-        }
-        if (n == 1) {
-            take(largest, at);
-        } else {
+        for (int g = 0; g < NG; ++g) {
+            if (!(best[g] >= least)) continue;
+            int n = 0, at = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if ((*this)[i] >= least) take((*this)[i], i);
+            for (int i = g * GROUP; i < (g + 1) * GROUP; ++i) {
+                const bool hit = f[i] >= least;
+                n += hit ? 1 : 0;
+                at = hit ? i : at;
+            }
+            if (n == 1) {
+                take(best[g], at);
+            } else {
+#pragma unroll
+                for (int i = g * GROUP; i < (g + 1) * GROUP; ++i)
+                    if (f[i] >= least) take(f[i], i);
+            }
         }
     }
 };
@@ -288,15 +294,13 @@ __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs 
     top_key = qr_wave_reduce_u32<true>(top_key);
     const float top = top_key ? qr_key_float(top_key) : -INFINITY;
     if (a.log_softmax) {
-        f.anew();
         const double d = wave_sum((double)f.sum_exp(top_key ? top : 0.0f));
         if (lane == 0) sums[wave] = d;
     }
     const unsigned T_key = bound_of(g, top_key, a.K, a.K + a.K / 4);
     const float least = T_key > 0x00800000u ? qr_key_float(T_key) : -FLT_MAX;   // (keys up to there are those of -inf and below)
     auto cand = [&](float l, int i) { return qr_cand(qr_float_key(l + 0.0f), first + ((i / V) * NT + tid) * V + i % V); };
-    f.anew();
-    f.hits(largest, least, [&](float l, int i) {
+    f.hits(least, [&](float l, int i) {
         const int at = atomicAdd(&n_list, 1);
         if (at < LIST) list[at] = cand(l, i);
     });
@@ -326,7 +330,6 @@ __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs 
     }
     // many equal logits: rank by rank over what the threads hold
     QrCand last = ~0ull;
-    f.anew();
     for (int r = 0; r < a.K; ++r) {
         QrCand mine = 0;
 #pragma unroll
@@ -471,8 +474,7 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
                 const unsigned k = qr_wave_reduce_u32<true>(logit_key(largest));
                 const float top = k ? qr_key_float(k) : -INFINITY;
                 row.top = (double)top;
-                f.anew();
-                row.log_sum = log(wave_sum((double)f.sum_exp(top)));   // (of -inf alone: NaN)
+                        row.log_sum = log(wave_sum((double)f.sum_exp(top)));   // (of -inf alone: NaN)
             }
             if (largest > -INFINITY) {
                 const unsigned k = (unsigned)(row(largest) >> 32);
@@ -502,11 +504,10 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
         const QrRowValue row = rows[w];
         if (row.log_sum == row.log_sum) {
             if (a.W > 16) f.load(x + w * a.ld, a.V, lane, 64);
-            f.anew();
-            // the bound as a logit of this row, a little lower than it is; where it has none every logit passes
+                // the bound as a logit of this row, a little lower than it is; where it has none every logit passes
             const double at = Tk ? ((word_value((QrValue)Tk << 32) - row.score) + row.log_sum) + row.top : -INFINITY;
             const float least = at == at ? fmaxf((float)(at - 1e-6 * fabs(at)), -FLT_MAX) : -FLT_MAX;
-            f.hits(f.largest(), least, [&](float l, int i) {
+            f.hits(least, [&](float l, int i) {
                 const QrPick p = {row(l), qr_cand(qr_float_key(l + 0.0f), ((i / V) * 64 + lane) * V + i % V), w};
                 if ((unsigned)(p.v >> 32) >= Tk && p.v) push(list, p);
             });
