@@ -260,8 +260,10 @@ __device__ __forceinline__ unsigned quad_max(unsigned v)
 }
 
 // Long rows, first launch.  Grid: x = stretch, y (and z) = row; NT = 256 or 512 threads with NV vectors each.
-// Bound by the chain of its steps and the exponentials: of 28 us for 64 x 16 x 32000 bf16 logits reading them and their maximum take 10,
-// sums 4, bound 2, gathering and ranks 5, the second launch 5; other numbers of waves and logits to one change little.
+// Bound by the chain of its steps and by its arithmetic, of which the exponentials are most: of a workgroup's 8 us for 64 x 16 x 32000
+// bf16 logits (two workgroups one after the other at each place, 19 us in all, the second launch 6) loading takes 2 to 5, maximum,
+// sums, bound and ranks 1 each, gathering 1.6; other numbers of waves and logits to one change little, fetching a next
+// stretch ahead spills.
 template <class T, int NV, int NT>
 __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs a)
 {
@@ -276,7 +278,8 @@ __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs 
     const int first = blockIdx.x * a.part, n = a.V - first < a.part ? a.V - first : a.part;
     if (tid == 0) n_list = 0;
     QrLogits<T, NV> f;
-    f.load((const T *)a.logits + row * a.ld + first, n, tid, NT);
+    const T *x = (const T *)a.logits + row * a.ld + first;
+    f.load(x, n, tid, NT);
     const float largest = f.largest();   // (NaN is found in the sum)
     if (NT == 256) {
         group_best[tid] = logit_key(largest);
@@ -328,13 +331,14 @@ __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs 
         if (tid >= M && tid < a.K) out[tid] = 0ull;
         return;
     }
-    // many equal logits: rank by rank over what the threads hold
+    // many equal logits: rank by rank, from memory (kept in registers up to here they would spill in every call: 26 MB written
+    // for 64 x 16 x 32000 bf16, 28 us against 25)
     QrCand last = ~0ull;
     for (int r = 0; r < a.K; ++r) {
         QrCand mine = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const QrCand c = f[i] > -INFINITY ? cand(f[i], i) : 0ull;
+        for (int i = tid; i < n; i += NT) {
+            const float l = (float)x[i];
+            const QrCand c = l > -INFINITY ? qr_cand(qr_float_key(l + 0.0f), first + i) : 0ull;
             if (c < last && c > mine) mine = c;
         }
         for (int off = 32; off > 0; off >>= 1) {
@@ -535,8 +539,8 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
 }
 
 // How rows are cut: whole up to SHORT logits (one launch); stretches of up to 8192 logits for 256 threads, or of 16384 for 512 where
-// there are rows enough to fill the device (64 x 16 x 32000 bf16, n_out 16: 28 us, by 8192 28, by 32768 30; 16 x 16 x 32000 fp32, n_out
-// 32: 18, by 8192 26).
+// there are rows enough to fill the device (measured for 16 x 16 x 32000 fp32, n_out 32: 18 us, by 8192 26; by 32768 at 64 x 16 x 32000 bf16 a
+// tenth more).
 constexpr int SHORT = 2048;
 bool long_stretches(int64_t rows, int V) { return rows >= 256 && V > 8192; }
 void plan_select(int64_t rows, int V, int &n_parts, int &part)
