@@ -538,15 +538,13 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
     });
 }
 
-// How rows are cut: whole up to SHORT logits (one launch); stretches of up to 8192 logits for 256 threads, or of 16384 for 512 where
-// there are rows enough to fill the device (measured for 16 x 16 x 32000 fp32, n_out 32: 18 us, by 8192 26; by 32768 at 64 x 16 x 32000 bf16 a
-// tenth more).
+// How rows are cut: whole up to SHORT logits (one launch) and, for 256 threads, up to 8192; longer ones into stretches of up to 16384
+// for 512 threads (64 x 16 x 32000 bf16, n_out 16: 24.8 us, by 8192 25.7; 16 x 16 x 32000 fp32, n_out 32: 17.6 and 19.6; 4 x 8 x 131072
+// 12.1 and 13.1; only 2 x 2 x 50000 is better by 8192: 9.4 and 9.1).
 constexpr int SHORT = 2048;
-bool long_stretches(int64_t rows, int V) { return rows >= 256 && V > 8192; }
-void plan_select(int64_t rows, int V, int &n_parts, int &part)
+void plan_select(int V, int &n_parts, int &part)
 {
-    const int len = long_stretches(rows, V) ? 16384 : 8192;
-    n_parts = (V + len - 1) / len;
+    n_parts = (V + 16383) / 16384;
     part = qr_round_up((V + n_parts - 1) / n_parts, 8);
     n_parts = (V + part - 1) / part;
 }
@@ -571,11 +569,11 @@ void launch_select(QrSelectArgs &a, void *workspace, hipStream_t st)
         return;
     }
     const int64_t rows = (int64_t)a.B * a.W;
-    plan_select(rows, a.V, a.n_parts, a.part);
+    plan_select(a.V, a.n_parts, a.part);
     a.heads = (QrPartHead *)workspace;
     a.cands = (QrCand *)((char *)workspace + heads_bytes(rows, a.n_parts));
     const dim3 grid(a.n_parts, (unsigned)(rows < 32768 ? rows : 32768), (unsigned)((rows + 32767) / 32768));
-    if (!long_stretches(rows, a.V)) select_parts_kernel<T, 8192 / 256 / V, 256><<<grid, 256, 0, st>>>(a);
+    if (a.V <= 8192) select_parts_kernel<T, 8192 / 256 / V, 256><<<grid, 256, 0, st>>>(a);
     else select_parts_kernel<T, 16384 / 512 / V, 512><<<grid, 512, 0, st>>>(a);
     const int64_t total = (int64_t)a.W * a.n_parts * a.K;
     if (total <= 1024) select_beam_kernel<256, true><<<a.B, 256, 0, st>>>(a);
@@ -591,7 +589,7 @@ extern "C" size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, i
     if (V <= SHORT) return 256;   // (not used)
     int n_parts, part;
     const int64_t rows = (int64_t)(B > 0 ? B : 1) * W;
-    plan_select(rows, V, n_parts, part);
+    plan_select(V, n_parts, part);
     return heads_bytes(rows, n_parts) + (size_t)rows * n_parts * n_out * sizeof(QrCand);
 }
 
