@@ -43,7 +43,7 @@ __device__ __forceinline__ void finish(const QrTokensLinear &p, int m, int r0, v
 // Few tokens: the weights are what is read.  A workgroup has RT tiles of 16 rows x 16*NT tokens; its waves take the 128-column
 // chunks in turn (each weight fragment is fetched once, straight into registers) and join their sums through LDS, where wave i
 // finishes the row tiles i, i + WAVES, ...
-// Grid: x = blocks of 16*RT rows.
+// Grid: x = blocks of 16*RT rows.  Bound by the weights' way from memory: 16 x 32000 x 1024 fp32, 35 MB, 7.4 us (4.7 TB/s with the launch).
 template <class T, int RT, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void linear_tokens_few_kernel(const QrTokensLinear p)
 {
@@ -130,6 +130,10 @@ __device__ __forceinline__ void store_past(float *p, v4f v)
 // the activations of D chunks of 128 (1 KiB blocks of 8 tokens x 128 bytes, lane l of the loading wave fetching token l/8's
 // 16-byte piece (l%8) ^ (l/8): whole lines per load, operand reads spread over the banks).  Both arrive by direct loads to LDS up
 // to three steps ahead, and a wave reads the next step's first operands before its last matrix instructions of the present one.
+// Bound, large tiles, by the matrix units at the clock that the power leaves them (8192^3 bf16 396 us, 2.78 POP/s: they are busy
+// 73 % of the cycles and the clock falls from 2.4 to 1.7 GHz; the library's int8 product of that size reaches 2.06 POP/s) and where
+// columns are few by the stores (16384 x 8192 x 128 bf16, 287 MB, 55 us: 5.2 TB/s).  16000 x 2560 x 1280 fp32 takes 65 us: 38
+// of products and 31 of stores, half of which pass while the other compute units' tiles are multiplied.
 template <int MT, int NT, int WN, int WM, int D>
 struct QrTile {
     static constexpr int WAVES = WN * WM, THREADS = 64 * WAVES;
