@@ -147,3 +147,33 @@ def test_two_streams_at_once(gpu_lib):
     torch.cuda.synchronize()
     for k in range(2):
         assert all(torch.equal(o, want[k]) for o in outs[k])
+
+
+# Large tiles alone, in rounds, with small or middle ones behind them; middle and small ones in one round and in several; one, two,
+# three and more chunks of columns; edges in every dimension.
+WAYS = [(10941, 132, 40), (11403, 142, 200), (295, 10943, 520), (9991, 267, 40), (10302, 263, 200), (270, 10248, 257), (835, 11970, 40),
+        (10794, 1290, 200), (1291, 11271, 257), (9295, 1552, 520), (8899, 1313, 40), (10158, 773, 200), (10975, 727, 257), (729, 10918, 520),
+        (10960, 1448, 257), (2200, 9190, 520), (1412, 11042, 700), (11928, 2602, 700), (9927, 2823, 200), (2050, 11715, 257), (2693, 8875, 520),
+        (7215, 4494, 257), (5162, 6769, 520), (2954, 11036, 520), (4922, 9842, 520), (4608, 4096, 1920)]
+
+
+@pytest.mark.parametrize("M,N,K", WAYS)
+def test_every_way_of_larger_products(gpu_lib, M, N, K):
+    """Against 64 bits on the GPU; results in aligned rows, in rows at odd places, and with what lies beside them left as it was."""
+    q, g = gpu_lib, torch.Generator(DEV).manual_seed(M + N + K)
+    width = (K + 15) // 16 * 16
+    a = torch.randint(-127, 128, (M, width), dtype=torch.int8, device=DEV, generator=g)
+    w = torch.randint(-127, 128, (N, K), dtype=torch.int8, device=DEV, generator=g)
+    sa, sw = (torch.exp(torch.randn(n, device=DEV, generator=g)) / 100 for n in (M, N))
+    bias = torch.randn(N, device=DEV, generator=g)
+    p = torch.matmul(a[:, :K].double(), w.double().t().contiguous()) * sa.double()[:, None] * sw.double()[None, :]
+    m = q.pack_int8(w, q.LAYOUT_TILED, sw)
+    for dtype, pad_to, with_bias in ((torch.float32, 8, True), (torch.bfloat16, 8, False), (torch.float16, 1, True), (torch.bfloat16, 1, True)):
+        pitch = (N + 1 + 7) // 8 * 8 if pad_to == 8 else (N + 1) | 1
+        base = torch.full((M + 1, pitch), 3.0, dtype=dtype, device=DEV)
+        out = base[:M, :N]
+        q.linear_tokens(m, a, sa, bias=bias if with_bias else None, out=out)
+        y = p + bias.double() if with_bias else p
+        off = (out.double() - y).abs() - (2.01 * 2.0 ** -24 * p.abs() + (2.0 ** -24 + plain64.HALF_STEP[dtype]) * y.abs() * (1 + 2.0 ** -8) + 2.0 ** -25)
+        assert off.max().item() <= 0, (dtype, divmod(off.argmax().item(), N))
+        assert bool((base[M] == 3).all()) and bool((base[:, N:] == 3).all())
