@@ -372,13 +372,14 @@ __global__ __launch_bounds__(NT) void select_beam_kernel(const QrSelectArgs a)
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int64_t row0 = (int64_t)b * a.W;
     const int per = a.n_parts * a.K, total = a.W * per;
+    // Groups for the bound: a thread, or four neighbours, with every 256th candidate, each time 73 further on: the best ranks of the
+    // lists, which make up most of what is taken, are spread over the groups (n_out 64 of 64 hypotheses: 80 candidates pass the
+    // bound; with four ranks that follow one another to a group 380 would)
+    auto index = [&](int q) { const int block = NT == 256 ? q : q * 4 + (tid & 3); return ((NT == 256 ? tid : tid >> 2) - 73 * block & 255) + 256 * block; };
     QrCand held[4];
     if (HELD) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int i = tid + NT * q;
-            held[q] = a.cands[row0 * per + (i < total ? i : 0)];
-        }
+        for (int q = 0; q < 4; ++q) held[q] = a.cands[row0 * per + (index(q) < total ? index(q) : 0)];
     }
     if (tid == 0) list.n = 0;
     // four threads to a row
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(NT) void select_beam_kernel(const QrSelectArgs a)
     QrPick kept[4];
     if (HELD) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) kept[q] = tid + NT * q < total ? pick(tid + NT * q, held[q]) : QrPick{0ull, 0ull, 0};
+        for (int q = 0; q < 4; ++q) kept[q] = index(q) < total ? pick(index(q), held[q]) : QrPick{0ull, 0ull, 0};
     }
     auto each = [&](auto &&visit) {
         if (HELD) {
@@ -418,9 +419,10 @@ __global__ __launch_bounds__(NT) void select_beam_kernel(const QrSelectArgs a)
             for (int q = 0; q < 4; ++q)
                 if (kept[q].v) visit(kept[q]);
         } else {
-            #pragma unroll 4
-            for (int i = tid; i < total; i += NT) {
-                const QrPick p = pick(i, a.cands[row0 * per + i]);
+#pragma unroll 4
+            for (int q = 0; q * NT < total; ++q) {
+                const int i = index(q);
+                const QrPick p = i < total ? pick(i, a.cands[row0 * per + i]) : QrPick{0ull, 0ull, 0};
                 if (p.v) visit(p);
             }
         }
