@@ -1,7 +1,7 @@
 // Beam selection over large vocabularies, from logits: log-softmax, scores and the best extensions of a beam (Sec. 2: up
 // to W hypotheses are kept per iteration) in one pass over the logits.
 //
-// Short rows (a wave holds one in its registers): one launch, one workgroup per utterance.  Long rows: a hypothesis'
+// Short rows (a wave holds one in its registers): one launch, one workgroup per utterance.  Long rows, or wide beams of few utterances: a hypothesis'
 // candidates are ordered as its logits are, so a stretch of a row can give up all but its n_out largest logits before the
 // row's log-sum-exp is known.  First launch: one workgroup per stretch holds it in registers, finds its maximum, sum of
 // exponentials and n_out largest logits.  Second launch: one workgroup per utterance joins sums and lists.
@@ -540,10 +540,13 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
     });
 }
 
-// How rows are cut: whole up to SHORT logits (one launch) and, for 256 threads, up to 8192; longer ones into stretches of up to 16384
-// for 512 threads (64 x 16 x 32000 bf16, n_out 16: 24.8 us, by 8192 25.7; 16 x 16 x 32000 fp32, n_out 32: 17.6 and 19.6; 4 x 8 x 131072
-// 12.1 and 13.1; only 2 x 2 x 50000 is better by 8192: 9.4 and 9.1).
+// How rows are cut.  One launch for rows of up to 512 logits (16 x 32 x 300 fp32 10.0 us, two launches 13.3) and of up to 2048 unless
+// wide beams leave most of the device idle (16 x 16 x 2000 9.4 us, two launches 11.0; 64 x 64 x 2000 25.5 and 34; but 1 x 64 x 2000 21.9
+// and 15.6, 16 x 32 x 600 16.7 and 13.4).  Whole rows of up to 8192 to 256 threads, longer ones in stretches of up to 16384 to 512
+// (64 x 16 x 32000 bf16, n_out 16: 24.8 us, by 8192 25.7; 16 x 16 x 32000 fp32, n_out 32: 17.6 and 19.6; 4 x 8 x 131072 12.1
+// and 13.1; only 2 x 2 x 50000 is better by 8192: 9.4 and 9.1).
 constexpr int SHORT = 2048;
+bool one_launch(int64_t rows, int W, int V) { return V <= 512 || (V <= SHORT && (W <= 24 || rows > 1024)); }
 void plan_select(int V, int &n_parts, int &part)
 {
     n_parts = (V + 16383) / 16384;
@@ -562,15 +565,12 @@ template <class T>
 void launch_select(QrSelectArgs &a, void *workspace, hipStream_t st)
 {
     constexpr int V = QrVec<T>::N;
-    if (a.V <= 512) {
-        select_short_kernel<T, 512 / 64 / V><<<a.B, 1024, 0, st>>>(a);
-        return;
-    }
-    if (a.V <= SHORT) {
-        select_short_kernel<T, SHORT / 64 / V><<<a.B, 1024, 0, st>>>(a);
-        return;
-    }
     const int64_t rows = (int64_t)a.B * a.W;
+    if (one_launch(rows, a.W, a.V)) {
+        if (a.V <= 512) select_short_kernel<T, 512 / 64 / V><<<a.B, 1024, 0, st>>>(a);
+        else select_short_kernel<T, SHORT / 64 / V><<<a.B, 1024, 0, st>>>(a);
+        return;
+    }
     plan_select(a.V, a.n_parts, a.part);
     a.heads = (QrPartHead *)workspace;
     a.cands = (QrCand *)((char *)workspace + heads_bytes(rows, a.n_parts));
@@ -588,9 +588,9 @@ void launch_select(QrSelectArgs &a, void *workspace, hipStream_t st)
 extern "C" size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, int32_t n_out)
 {
     if (!select_sizes_ok(B, W, V, n_out)) return 0;
-    if (V <= SHORT) return 256;   // (not used)
-    int n_parts, part;
     const int64_t rows = (int64_t)(B > 0 ? B : 1) * W;
+    if (one_launch(rows, W, V)) return 256;   // (not used)
+    int n_parts, part;
     plan_select(V, n_parts, part);
     return heads_bytes(rows, n_parts) + (size_t)rows * n_parts * n_out * sizeof(QrCand);
 }

@@ -183,3 +183,21 @@ def test_no_utterances_and_what_the_workspace_held(gpu_lib):
             check_exact(run(q, score, logits, n, log_softmax=False, workspace=ws), v, n)
             # (run() moves the workspace to the device it is on already)
             assert bool((ws[need:] == fill).all())
+
+
+# Wide beams on both sides of the choice between one launch and two, lists that fit the second one's registers and that do not.
+WIDE = [(1, 64, 2000, 64), (16, 32, 600, 32), (33, 32, 600, 32), (3, 25, 513, 25), (41, 25, 1025, 7), (1, 64, 20000, 64), (2, 64, 3000, 64), (1, 25, 2048, 64),
+        (1, 3, 50001, 64), (2, 17, 16385, 33)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,W,V,n", WIDE)
+def test_wide_beams(gpu_lib, dtype, B, W, V, n):
+    score, logits = grid_case(B + W + V + n, B, W, V, dtype, spread=40)
+    finished = torch.from_numpy(np.random.RandomState(V).rand(B, W) < 0.2)
+    v = plain64.candidates(score.numpy(), logits.float().numpy(), False, finished.numpy(), 3)
+    check_exact(run(gpu_lib, score, logits, n, log_softmax=False, finished=finished, end_token=3), v, n)
+    g = torch.Generator().manual_seed(B + 2 * W + 3 * V + n)
+    logits = (3 * torch.randn((B * W, V), generator=g)).to(dtype)
+    v = plain64.candidates(score.numpy(), logits.float().numpy(), True)
+    check_near(run(gpu_lib, score, logits, n), v, n)
