@@ -473,8 +473,10 @@ QrTokensPiece plan_piece(int rows, int K, int M, float &least)
 
 QrTokensPlan plan_linear_tokens(int rows, int K, int M)
 {
-    // few tokens: beyond 16 their codes are fetched as often as the weights and more, so long or many rows go to tiles
-    if (M <= 16 || (M <= 32 && (rows <= 16384 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= 4096)) return {{{FEW, 1, M}}, 1};
+    // few tokens: beyond 16 their codes are fetched as often as the weights and more, so long or many rows go to tiles (tokens x rows x
+    // columns, few / small tiles: 17 x 8192 x 8192 12.4 / 15.1 us; 32 x 32000 x 1024 8.0 / 8.9; 32 x 16384 x 8192 28.8 / 24.9; 48 x 2048 x
+    // 2048 5.2 / 7.0; 64 x 2048 x 2048 5.8 / 7.0; 64 x 2048 x 4096 9.7 / 8.6)
+    if (M <= 16 || (M <= 32 && (rows <= 8192 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= (M <= 48 ? 4096 : 2048))) return {{{FEW, 1, M}}, 1};
     float least;
     QrTokensPlan best = {{plan_piece(rows, K, M, least)}, 1};
     // whole rounds of large tiles first, what would leave a round part empty in a launch of its own (6000 x 3000 x 5000: 121 us
