@@ -524,12 +524,12 @@ void launch_piece(const QrTokensLinear &p, const QrTokensPiece &piece, hipStream
 {
     switch (piece.kind) {
     case FEW:
-        // One row tile to a workgroup while that does not take more than two workgroups a compute unit; 8 waves where there are
+        // One row tile to a workgroup while that does not take more than about three workgroups a compute unit; 8 waves where there are
         // few of them (1 x 512 x 8192 3.7 us, with 4 waves 4.4; 16 x 8192 x 4096 7.3, with 4 waves 6.8).  Two row tiles beyond (16 x
-        // 32000 x 4096 24.6 us, one tile 29.5).
+        // 16384 x 8192 24.3 us, one tile 29.5; 1 x 12000 x 4096 8.9, one tile 8.6).
         if (p.M <= 16) {
             if (p.rows <= 4096) launch_few<T, 1, 1, 8>(p, st);
-            else if (p.rows <= 16384) launch_few<T, 1, 1, 4>(p, st);
+            else if (p.rows <= 12288) launch_few<T, 1, 1, 4>(p, st);
             else launch_few<T, 2, 1, 4>(p, st);
         } else if (p.M <= 32) {
             if (p.rows <= 4096) launch_few<T, 1, 2, 4>(p, st);
