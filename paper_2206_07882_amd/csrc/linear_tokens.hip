@@ -141,7 +141,9 @@ struct QrTile {
     static constexpr int A_BLOCKS = MT * WN, B_BLOCKS = 2 * NT * WM;      // of 1 KiB: weights of a step, activations of a chunk
     static constexpr int A_LOADS = A_BLOCKS / WAVES, B_LOADS = B_BLOCKS / WAVES;
     static constexpr int A_STAGE = A_BLOCKS * 1024, B_STAGE = B_BLOCKS * 1024;
-    static constexpr int B_AT = 2 * D * A_STAGE, TURN = B_AT + D * B_STAGE, SCALES = TURN + WAVES * 2048, SCALE_BYTES = (2 * BN + BM) * 4, LDS = SCALES + 2 * SCALE_BYTES;
+    // LDS: the ring, 2 KB for each wave's results, scales and bias of two tiles
+    static constexpr int B_AT = 2 * D * A_STAGE, TURN = B_AT + D * B_STAGE, SCALES = TURN + WAVES * 2048;
+    static constexpr int SCALE_BYTES = (2 * BN + BM) * 4, LDS = SCALES + 2 * SCALE_BYTES;
     static_assert(A_BLOCKS % WAVES == 0 && B_BLOCKS % WAVES == 0, "every wave loads as much");
     static_assert(D == 2 || D == 4, "ring of chunks");
 };
@@ -174,10 +176,14 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
     };
     const v4i *src_a[P::A_LOADS];
     const int8_t *src_b[P::B_LOADS];
-    auto load_a = [&](int i, int k) { qr_load_lds16(src_a[i] + (size_t)k * 64, __builtin_amdgcn_readfirstlane(lds0 + (k & (2 * D - 1)) * P::A_STAGE + (wave * P::A_LOADS + i) * 1024)); };
+    auto load_a = [&](int i, int k) {
+        const unsigned to = lds0 + (k & (2 * D - 1)) * P::A_STAGE + (wave * P::A_LOADS + i) * 1024;
+        qr_load_lds16(src_a[i] + (size_t)k * 64, __builtin_amdgcn_readfirstlane(to));
+    };
     auto load_b = [&](int i, int kc) {
         const int c = (kc0 + kc) * QRNNT_KCHUNK;   // columns behind the row: its start instead (they meet zero weights)
-        qr_load_lds16(src_b[i] + (c + piece < p.K ? c : -piece), __builtin_amdgcn_readfirstlane(lds0 + P::B_AT + (kc & (D - 1)) * P::B_STAGE + (wave * P::B_LOADS + i) * 1024));
+        const unsigned to = lds0 + P::B_AT + (kc & (D - 1)) * P::B_STAGE + (wave * P::B_LOADS + i) * 1024;
+        qr_load_lds16(src_b[i] + (c + piece < p.K ? c : -piece), __builtin_amdgcn_readfirstlane(to));
     };
     // Order of all loads: A(0), then for every chunk c: B(c), A(2c + 1), A(2c + 2).  Chunks up to D - 2 are on their way before the
     // loop; the two steps of chunk c start B(c + D - 1) and A(2(c + D) - 1), then A(2(c + D)).
@@ -399,7 +405,6 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
         scales = 2 * P::SCALES + P::SCALE_BYTES - scales;
     }
 }
-
 
 // Joins the sums of a product that was cut along its columns: one thread has four rows of a token.
 template <class T>

@@ -188,7 +188,6 @@ struct QrLogits {
             for (int i = 0; i < GROUP; ++i) best[g] = fmaxf(best[g], f[g * GROUP + i]);
         }
     }
-    __device__ __forceinline__ float operator[](int i) const { return f[i]; }
     __device__ __forceinline__ float largest() const
     {
         float m = best[0];
@@ -267,7 +266,7 @@ __device__ __forceinline__ unsigned quad_max(unsigned v)
 template <class T, int NV, int NT>
 __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs a)
 {
-    constexpr int V = QrVec<T>::N, PER = NV * V, NW = NT / 64;
+    constexpr int V = QrVec<T>::N, NW = NT / 64;
     __shared__ QrCand list[LIST], wave_best[NW];
     __shared__ unsigned group_best[256];
     __shared__ double sums[NW];
@@ -455,8 +454,8 @@ __global__ __launch_bounds__(NT) void select_beam_kernel(const QrSelectArgs a)
     write_ranks<NT>(a, b, list, each);
 }
 
-// Short rows: one launch, one workgroup of 16 waves an utterance, wave i takes the rows i, i + 16, ...; a row has at most 64 * PER
-// logits.
+// Short rows: one launch, one workgroup of 16 waves an utterance, wave i takes the rows i, i + 16, ...; a row has at most 64 * NV * V
+// logits.  Bound by its chain of steps, of 0.3 to 1 us each: 5.3 us for 1 x 4 x 1000 fp32, 9.8 for 64 x 16 x 1000 bf16.
 template <class T, int NV>
 __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a)
 {
