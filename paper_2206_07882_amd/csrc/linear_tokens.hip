@@ -340,12 +340,14 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
             constexpr int E = 16 / sizeof(T), MG = 8 / (int)sizeof(T);   // elements of 16 bytes; row tiles whose 128 bytes of a token turn at a time
             typedef T vec_e __attribute__((ext_vector_type(E)));
             typedef T vec_4 __attribute__((ext_vector_type(4)));
-            // Rows of whole 16-byte pieces are not kept in the L2 (whose lines the operands are in, and which a launch ends with
-            // writing back): large tiles store past it (16384 x 8192 x 512 bf16 95 us, kept or through it 106 and 102), the others
-            // through it (1024 x 2048 x 2048 fp32 9.1, past it 9.4, kept 10.1).  Pieces at any other address share lines and
-            // their 32-byte sectors with their neighbours, which only the L2 can join: 11206 x 9405 x 136 bf16 87 us kept in the
-            // L2, 160 past it, 144 through it.
-            const bool pieces = (((uintptr_t)p.y | ((uintptr_t)p.ld_y * sizeof(T))) & 15) == 0;
+            // Rows of whole lines are not kept in the L2 (whose lines the operands are in, and which a launch ends with writing back):
+            // large tiles store past it (16384 x 8192 x 512 bf16 95 us, kept or through it 106 and 102), the others through it
+            // (1024 x 2048 x 2048 fp32 9.1, past it 9.4, kept 10.1).  Where rows begin inside a line, two stores share it, which
+            // only the L2 can join: 11206 x 9400 x 136 bf16 82 us kept, 131 past it; 6000 x 6004 x 200 fp32 44 and 81; 11206 x
+            // 9405 x 136 87 and 160.  Small results stay in the caches behind it all the same: 3000 x 1004 x 1000 fp32, 12 MB,
+            // 11.1 kept and 10.0 through; 4200 x 4104 x 300 bf16, 34 MB, 17.4 and 19.7.
+            const uintptr_t odd = (uintptr_t)p.y | ((uintptr_t)p.ld_y * sizeof(T));
+            const bool pieces = (odd & 127) == 0 || ((odd & 15) == 0 && p.M * p.ld_y * (int64_t)sizeof(T) <= 16 << 20);
             v4f sw[MT], bs[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
