@@ -152,8 +152,13 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
     if (PER) {
         // all loads of the row first: a vector that lies inside the row as it is, what hangs over its end element by element
         float r[P][V], w[P][V];
+        const int t_wave = __builtin_amdgcn_readfirstlane(t & ~63);
+        // None of the wave's vectors is in the row (uniform): not computed.  (fp32 without a norm has so little to compute that the
+        // branches between its loads cost more: 16384 x 1100 16.2 us, with them 17.9; bf16 with residual, 608 columns 27.1 and 25.0.)
+        auto idle = [&](int p) { return (NORM || sizeof(T) == 2) && (p * TPR + t_wave) * V >= cols; };
 #pragma unroll
         for (int p = 0; p < P; ++p) {
+            if (idle(p)) continue;
             const int c = (p * TPR + t) * V, n = cols - c;
             const bool whole = n >= V;
             if (cols >= V) {   // uniform
@@ -173,6 +178,7 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
         }
 #pragma unroll
         for (int p = 0; p < P; ++p) {
+            if (idle(p)) continue;
             const int c = (p * TPR + t) * V;
             if (!(NORM && weight)) ones(w[p]);
             form(c, u[p], r[p]);
@@ -277,18 +283,27 @@ template <class T, bool NORM>
 void launch_tokens(const QrTokenArgs &a, hipStream_t st)
 {
     constexpr int V = QrVec<T>::N;
-    // A row to as few threads as its registers allow (us, at the rows of 4 to 16 thousand tokens; a copy of as many bytes): 4096 bf16 with
-    // residual 84 (90), 1280 fp32 19.5 with 64 threads, 20.5 with 256 (19.7), 2000 fp16 with residual 14.8 with 128, 17.7 with 256 (10.8),
-    // 8192 bf16 with residual 34.9 with 512, 37.2 with 256 (33.1), 10000 bf16 27.0 with 256, 32.5 with 1024 (17.3).
+    // A row to as few threads as its registers allow, and vectors as even as can be: what a wave has beyond the row it skips, but a
+    // thread's part of it it computes (us at 4 to 16 thousand rows; a copy of as many bytes): 4096 bf16 with residual 84 (90), 1280 fp32
+    // 19.7 by 64 x 5, 20.4 by 128 x 3 (19.7), 2300 bf16 with residual 74 by 64 x 5, 70 by 128 x 3 (51), 2000 fp16 with residual 14.8 by
+    // 128 x 2, 17.7 by 256 (10.8), 4104 bf16 with residual 100 by 256 x 3, 113 by 512 x 2 (91), 8192 bf16 with residual 34.9 by 512,
+    // 37.2 by 256 (33.1), 12000 bf16 with residual 128 by 512 x 3, 165 by 1024 x 2 (132).
     const int nv = (a.cols + V - 1) / V;
 #define QR_TOKENS(tpr, per) launch_rows<T, NORM, tpr, per>(a, st)
+    if constexpr (!NORM && V == 4) {
+        if (nv > 256 && nv <= 320) {
+            QR_TOKENS(64, 5);
+            return;
+        }
+    }
     if (nv <= 64) QR_TOKENS(64, 1);
     else if (nv <= 128) QR_TOKENS(64, 2);
     else if (nv <= 256) QR_TOKENS(128, 2);
-    else if (nv <= 320) QR_TOKENS(64, 5);
+    else if (nv <= 384) QR_TOKENS(128, 3);
     else if (nv <= 512) QR_TOKENS(256, 2);
+    else if (nv <= 768) QR_TOKENS(256, 3);
     else if (nv <= 1024) QR_TOKENS(512, 2);
-    else if (nv <= 1280) QR_TOKENS(256, 5);
+    else if (nv <= 1536) QR_TOKENS(512, 3);
     else if (nv <= 2048) QR_TOKENS(1024, 2);
     else if (nv <= 4096) QR_TOKENS(1024, 4);
     else QR_TOKENS(1024, 0);
