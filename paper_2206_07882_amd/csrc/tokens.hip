@@ -33,13 +33,22 @@ struct QrRowSums {
         key = o.key > key ? o.key : key;
         if (WIDE) peak = fmax(peak, o.peak);
     }
+    // Over LANES neighbouring lanes (the row's, or the wave's).
+    template <int LANES>
     __device__ __forceinline__ void reduce_wave(bool sums)
     {
         if (sums)
-            for (int off = 32; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
-        key = qr_wave_reduce_u32<true>(key);
+            for (int off = LANES / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off);
+        if (LANES == 64) {
+            key = qr_wave_reduce_u32<true>(key);
+        } else {
+            for (int off = LANES / 2; off > 0; off >>= 1) {
+                const unsigned o = __shfl_xor(key, off);
+                key = o > key ? o : key;
+            }
+        }
         if (WIDE)
-            for (int off = 32; off > 0; off >>= 1) peak = fmax(peak, __shfl_xor(peak, off));
+            for (int off = LANES / 2; off > 0; off >>= 1) peak = fmax(peak, __shfl_xor(peak, off));
     }
 };
 
@@ -47,11 +56,13 @@ struct QrRowSums {
 template <int TPR>
 __device__ __forceinline__ void reduce_row64(double &sum, double &peak, bool &bad, double *lds)
 {
-    for (int off = 32; off > 0; off >>= 1) {
+    int any_bad = bad ? 1 : 0;
+    for (int off = (TPR < 64 ? TPR : 64) / 2; off > 0; off >>= 1) {
         sum += __shfl_xor(sum, off);
         peak = fmax(peak, __shfl_xor(peak, off));
+        any_bad |= __shfl_xor(any_bad, off);
     }
-    bad = __any(bad);
+    bad = any_bad != 0;
     if (TPR > 64) {
         constexpr int NW = TPR / 64;
         const int wave = threadIdx.x >> 6;
@@ -101,17 +112,17 @@ __device__ __forceinline__ void odd_row(const T *h, const T *weight, int cols, f
 
 // Bound by memory: 16384 x 4096 bf16 with residual, 470 MB, in 84 us is 5.6 TB/s (a copy of 1 GiB on this card: 5.2); one row of
 // 4096 takes 4 us, the length of its chain.
-// TPR threads to a row (64: four rows to a workgroup), PER vectors of 16 bytes to a thread; PER = 0: rows of any length, read
+// TPR threads to a row (up to 64: workgroups of 256 have several), PER vectors of 16 bytes to a thread; PER = 0: rows of any length, read
 // a second time for the codes.
 template <class T, bool NORM, int TPR, int PER>
 __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrTokenArgs a)
 {
-    constexpr int V = QrVec<T>::N, RPB = TPR < 128 ? 256 / TPR : 1, NW = TPR / 64;
+    constexpr int V = QrVec<T>::N, RPB = TPR < 128 ? 256 / TPR : 1, NW = TPR < 64 ? 1 : TPR / 64;
     constexpr bool WIDE = NORM && sizeof(T) == 4;   // products of two fp32 values do not fit fp32
     __shared__ QrRowSums<WIDE> red[NW > 1 ? NW : 1];
     __shared__ double red64[3 * NW];
     const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    if (row >= a.rows) return;   // (whole waves; where rows share a workgroup nothing waits for others)
+    if (row >= a.rows) return;   // (where rows share a workgroup nothing waits for others)
     const int t = threadIdx.x % TPR, cols = a.cols;
     const T *x = (const T *)a.x + row * a.ld_x, *res = (const T *)a.residual, *weight = (const T *)a.weight;
     T *sum = (T *)a.sum;
@@ -199,7 +210,7 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
         }
         s.ss = (float)ss;
     }
-    s.reduce_wave(NORM);
+    s.template reduce_wave<(TPR < 64 ? TPR : 64)>(NORM);
     if (NW > 1) {
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
         __syncthreads();
@@ -288,6 +299,7 @@ void launch_tokens(const QrTokenArgs &a, hipStream_t st)
     // 19.7 by 64 x 5, 20.4 by 128 x 3 (19.7), 2300 bf16 with residual 74 by 64 x 5, 70 by 128 x 3 (51), 2000 fp16 with residual 14.8 by
     // 128 x 2, 17.7 by 256 (10.8), 4104 bf16 with residual 100 by 256 x 3, 113 by 512 x 2 (91), 8192 bf16 with residual 34.9 by 512,
     // 37.2 by 256 (33.1), 12000 bf16 with residual 128 by 512 x 3, 165 by 1024 x 2 (132).
+    // Rows of few vectors share a wave: 500000 x 128 bf16 with residual 92 by 16, 344 by 64 (86); 16384 x 256 11.2 by 32, 17.3 by 64.
     const int nv = (a.cols + V - 1) / V;
 #define QR_TOKENS(tpr, per) launch_rows<T, NORM, tpr, per>(a, st)
     if constexpr (!NORM && V == 4) {
@@ -296,7 +308,9 @@ void launch_tokens(const QrTokenArgs &a, hipStream_t st)
             return;
         }
     }
-    if (nv <= 64) QR_TOKENS(64, 1);
+    if (nv <= 16) QR_TOKENS(16, 1);
+    else if (nv <= 32) QR_TOKENS(32, 1);
+    else if (nv <= 64) QR_TOKENS(64, 1);
     else if (nv <= 128) QR_TOKENS(64, 2);
     else if (nv <= 256) QR_TOKENS(128, 2);
     else if (nv <= 384) QR_TOKENS(128, 3);

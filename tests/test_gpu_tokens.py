@@ -152,9 +152,10 @@ def test_many_rows(gpu_lib):
     check(codes[-50:], scale[-50:], plain64.token_codes(tail.double().numpy()), 24, torch.float32, False)
 
 
-def test_more_rows_than_a_grid_has_threads_for(gpu_lib):
-    """2^26 + 70 rows of 64 threads each are more than 2^32 threads."""
-    q, rows = gpu_lib, (1 << 26) + 70
+@pytest.mark.parametrize("rows", [(1 << 26) + 70, (1 << 27) + 70])
+def test_more_rows_than_a_launch_takes(gpu_lib, rows):
+    """Rows of 16 threads: 2^31 threads, 2^27 rows, to a launch; the last ones, and those of the second launch, as all others."""
+    q = gpu_lib
     x = torch.randn((rows, 1), device=DEV, dtype=torch.float16, generator=torch.Generator(DEV).manual_seed(1))
     codes, scale = q.quantize_tokens(x)
     at = torch.cat([torch.arange(5), torch.arange(1 << 25, (1 << 25) + 5), torch.arange(rows - 140, rows)]).to(DEV)
@@ -176,3 +177,25 @@ def test_long_rows_of_equal_values(gpu_lib, value):
     # 4 + 1 + 6 + 16 + 2 roundings halved by the root, 4 behind it; the count of columns itself is rounded to fp32: half of one
     assert abs(float(scale[0]) - want) <= ((4 + 1 + 6 + 16 + 2) / 2 + 4 + 0.5) * 2.0 ** -24 * want
     assert bool((codes[0, :cols] == 127).all()) and not bool(codes[0, cols:].any())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [1, 9, 60, 64, 65, 100, 127, 128, 129, 250, 256])
+def test_short_rows_of_every_kind_side_by_side(gpu_lib, dtype, cols):
+    """Several rows to a wave: rows that are ordinary, all zero, not finite, tiny or huge next to one another, a last wave that is
+    not full."""
+    q, rows = gpu_lib, 77
+    x = randn(cols, rows, cols).double()
+    big = 3e38 if dtype != torch.float16 else 6e4
+    x[3::8] = 0.0
+    x[4::8, cols // 2] = float("inf")
+    x[5::8, cols - 1] = float("nan")
+    x[6::8] *= 1e-30 if dtype != torch.float16 else 1e-6
+    x[7::8] = x[7::8].sign() * big
+    x = x.to(dtype)
+    codes, scale = q.quantize_tokens(x.to(DEV))
+    values = x.double().numpy()
+    check(codes, scale, plain64.token_codes(np.where(np.isfinite(values), values, np.nan)), cols, dtype, False)
+    w = (1 + 0.3 * randn(7, cols)).to(dtype)
+    codes, scale, _ = q.rms_norm_quant(x.to(DEV), w.to(DEV), 1e-5)
+    check(codes, scale, plain64.rms_norm_quant(x, w, 1e-5, None)[:2], cols, dtype, True)
