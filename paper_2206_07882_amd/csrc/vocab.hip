@@ -509,9 +509,13 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
         const QrRowValue row = rows[w];
         if (row.log_sum == row.log_sum) {
             if (a.W > 16) f.load(x + w * a.ld, a.V, lane, 64);
-                // the bound as a logit of this row, a little lower than it is; where it has none every logit passes
-            const double at = Tk ? ((word_value((QrValue)Tk << 32) - row.score) + row.log_sum) + row.top : -INFINITY;
-            const float least = at == at ? fmaxf((float)(at - 1e-6 * fabs(at)), -FLT_MAX) : -FLT_MAX;
+            // the bound as a logit of this row, and a little lower, by 1e-6 of it (its rounding to fp32) and by what the sums to the value and
+            // back are rounded by, a few halves of 2^-52 of the largest number in them (where they cancel that is all there is: 1 - 1e-20 is 1);
+            // where it has none every logit passes.  What passes is held against the bound itself.
+            const double bound = word_value((QrValue)Tk << 32);
+            const double at = Tk ? ((bound - row.score) + row.log_sum) + row.top : -INFINITY;
+            const double less = 1e-6 * fabs(at) + 0x1p-48 * (fabs(bound) + fabs(row.score) + fabs(row.log_sum) + fabs(row.top));
+            const float least = at == at ? fmaxf((float)(at - less), -FLT_MAX) : -FLT_MAX;
             f.hits(least, [&](float l, int i) {
                 const QrPick p = {row(l), qr_cand(qr_float_key(l + 0.0f), ((i / V) * 64 + lane) * V + i % V), w};
                 if ((unsigned)(p.v >> 32) >= Tk && p.v) push(list, p);
