@@ -84,6 +84,22 @@ __device__ __forceinline__ void reduce_row64(double &sum, double &peak, bool &ba
     }
 }
 
+// rne(127 u / peak).  WIDE: u and peak are products of two fp32 values, whose 127-fold (55 bits) fp64 does not hold; where the quotient is next
+// to the border of two codes the sign of 254 u - (2 j + 1) peak decides, each product as its rounded value and the rest of it.  (Otherwise u
+// and peak have at most 24 bits, and what is not at a border is further from it than 2^-32 of the quotient.)
+template <bool WIDE>
+__device__ __forceinline__ int code_of(double u, double peak)
+{
+    const double q = 127.0 * u / peak;
+    int k = (int)rint(q);
+    if (WIDE && fabs(fabs(q - k) - 0.5) < 0x1p-40) {
+        const double j = floor(q), a = 254.0 * u, m = 2.0 * j + 1.0, b = m * peak;
+        const double d = (a - b) + (fma(254.0, u, -a) - fma(m, peak, -b));
+        k = (int)j + (d > 0.0 || (d == 0.0 && ((int)j & 1)) ? 1 : 0);
+    }
+    return k;
+}
+
 // A row whose values fp32 does not carry well: all zero, not finite, squares or products that overflow or vanish.  All
 // of it in fp64, from the stored h.
 template <class T, bool NORM, int TPR>
@@ -103,7 +119,7 @@ __device__ __forceinline__ void odd_row(const T *h, const T *weight, int cols, f
     reduce_row64<TPR>(sum, peak, bad, lds);
     const bool none = bad || peak == 0.0;
     for (int c0 = t * V; c0 < cols; c0 += TPR * V)
-        for (int i = 0; i < V && c0 + i < cols; ++i) q[c0 + i] = none ? 0 : (int8_t)(int)rint(127.0 * value(c0 + i) / peak);
+        for (int i = 0; i < V && c0 + i < cols; ++i) q[c0 + i] = none ? 0 : (int8_t)code_of<NORM && sizeof(T) == 4>(value(c0 + i), peak);
     if (t == 0) {
         const double root = NORM ? sqrt(sum / cols + (double)eps) : 1.0;
         *scale = bad ? NAN : (peak == 0.0 ? 1.0f : (float)(peak / root / 127.0));
@@ -227,8 +243,8 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
         return;
     }
     const float inv = 127.0f / peak;
-    // u * inv is off by at most 3 roundings of 127 (2.3e-5): where it is nearer than 2^-14 to the border of two codes the
-    // quotient itself decides
+    // u * inv is off by at most 4 roundings of 127 (3.1e-5; of u and peak where they are products of fp32 values, of inv, of this product):
+    // where it is nearer than 2^-14 (6.1e-5) to the border of two codes the quotient itself decides
     auto codes = [&](int c, const float (&v)[V]) {
         int k[V];
         bool near = false;
@@ -244,7 +260,7 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
             for (int i = 0; i < V; ++i) {
                 double e = (double)v[i];
                 if (WIDE && c + i < cols) e = (double)(float)h_at[c + i] * (weight ? (double)(float)weight[c + i] : 1.0);
-                k[i] = (int)rint(127.0 * e / pk);
+                k[i] = code_of<WIDE>(e, pk);
             }
         }
 #pragma unroll

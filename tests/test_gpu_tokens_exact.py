@@ -1,0 +1,49 @@
+"""Rows of fp32 with a weight for which 64 bits do not decide: products of two fp32 values have 48 bits, 127 times them 55, and
+a quotient may lie so near the border of two codes that fp64 rounds onto it.  The expected codes come from whole numbers."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+# value, its weight, the row's largest value, its weight: 127 * value * weight / (largest * weight) is within 2^-53 of a half
+NEAR = [(13584009, 8509953, 12290083, 9518320), (11023329, 13666381, 12793516, 15659458), (15642983, 9019847, 15225983, 16012155),
+        (15642983, 9019847, 15225983, 13764835), (13227203, 13173249, 14272204, 12867274), (14618029, 8953173, 11915842, 11871536),
+        (10582359, 10850585, 11730093, 10316939), (9958251, 13467876, 14051179, 15641249), (11146650, 11784417, 14200113, 15560281),
+        (10299142, 12322864, 13548638, 16409025), (10299142, 12322864, 13548638, 10574705), (14706544, 8708158, 10176483, 15746241),
+        (9934616, 13880719, 13732198, 12817509), (13163666, 15079352, 13965955, 16636535), (9649961, 13171371, 13289237, 16304367),
+        (12936874, 9737182, 11304771, 11842317), (11145924, 14358381, 15563013, 15455209), (8892439, 16257012, 15127853, 9827003)]
+
+
+def code(value, largest):
+    """rne(127 value / largest) of whole numbers."""
+    two, rest = divmod(254 * abs(value), largest)   # in half codes
+    k = two // 2
+    up = two % 2 and (rest or k % 2)
+    return (1 if value > 0 else -1) * (k + (1 if up else 0))
+
+
+def case(pad, scale, sign):
+    """A row for each entry, zeros but for two columns of its own, and one with an exact half: (x, weight, codes)."""
+    rows = NEAR + [(15, 1 << 20, 254, 1 << 20)]   # 127 * 15 / 254 = 7.5
+    cols = 2 * len(rows) + pad
+    x, w, want = torch.zeros((len(rows), cols)), torch.ones(cols), np.zeros((len(rows), cols), np.int8)
+    for r, (h, hw, p, pw) in enumerate(rows):
+        at = cols - 2 * len(rows) + 2 * r
+        x[r, at], w[at], x[r, at + 1], w[at + 1] = sign * h, hw, p, pw
+        want[r, at], want[r, at + 1] = code(sign * h * hw, p * pw), 127
+    return x * scale, w * scale, want
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -23, 1.0, 2.0 ** -50, 2.0 ** 40])   # the latter two in the way of rows out of the ordinary
+@pytest.mark.parametrize("pad", [0, 3, 300, 5000, 20000])
+def test_codes_that_64_bits_do_not_decide(gpu_lib, pad, scale):
+    for sign in (1, -1):
+        x, w, want = case(pad, scale, sign)
+        codes, _, _ = gpu_lib.rms_norm_quant(x.to(DEV), w.to(DEV), 0.0)
+        np.testing.assert_array_equal(codes.cpu().numpy()[:, :x.shape[1]], want)
+
+
+def test_the_expected_codes_are_not_those_of_64_bits():
+    for h, hw, p, pw in NEAR:
+        assert int(np.rint(127.0 * float(h * hw) / float(p * pw))) != code(h * hw, p * pw)
