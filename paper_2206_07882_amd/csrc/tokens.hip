@@ -285,7 +285,10 @@ __global__ __launch_bounds__(TPR < 128 ? 256 : TPR) void tokens_kernel(const QrT
             codes(c, u[0]);
         }
     }
-    if (t == 0) a.scale[row] = NORM ? (peak * (1.0f / sqrtf(s.ss / (float)cols + a.eps))) / 127.0f : peak / 127.0f;
+    if (t == 0) {
+        const float r = NORM ? 1.0f / sqrtf(s.ss / (float)cols + a.eps) : 1.0f, y = peak * r;   // the largest value of the normalised row
+        a.scale[row] = y < INFINITY ? y / 127.0f : (peak / 127.0f) * r;   // (it may pass fp32 where its 127th part does not)
+    }
 }
 
 template <class T, bool NORM, int TPR, int PER>

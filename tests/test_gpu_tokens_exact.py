@@ -47,3 +47,17 @@ def test_codes_that_64_bits_do_not_decide(gpu_lib, pad, scale):
 def test_the_expected_codes_are_not_those_of_64_bits():
     for h, hw, p, pw in NEAR:
         assert int(np.rint(127.0 * float(h * hw) / float(p * pw))) != code(h * hw, p * pw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [4, 200, 5000])
+def test_scales_of_rows_whose_largest_value_passes_fp32(gpu_lib, dtype, cols):
+    """One value of 2^-30 among zeros times 2^127: normalised it is 2^127 sqrt(cols), and a 127th of it fits fp32."""
+    x = torch.zeros((2, cols))
+    x[0, 1] = x[1, cols - 1] = 2.0 ** -30
+    w = torch.full((cols,), 2.0 ** 127)
+    codes, scale, _ = gpu_lib.rms_norm_quant(x.to(dtype).to(DEV), w.to(dtype).to(DEV), 0.0)
+    want = 2.0 ** 127 * np.sqrt(cols) / 127.0
+    # quotient, mean, its root and reciprocal, product: 5 roundings, the mean's halved by the root
+    assert (np.abs(scale.cpu().numpy().astype(np.float64) - want) <= 5 * 2.0 ** -24 * want).all()
+    assert codes[0, 1] == 127 and codes[1, cols - 1] == 127 and int(codes.float().sum()) == 254
