@@ -21,6 +21,14 @@ static inline size_t qr_matrix_bytes(int64_t rows, int64_t cols, int64_t ld, siz
 {
     return (size_t)((rows - 1) * ld + cols) * size;
 }
+// Whether two matrices of rows have a byte in common (sizes, rows and pitches in bytes); columns of one matrix have none.
+static inline bool qr_rows_overlap(const void *p, size_t pn, int64_t p_row, int64_t p_pitch, const void *q, size_t qn, int64_t q_row, int64_t q_pitch)
+{
+    if (!qr_overlap(p, pn, q, qn)) return false;
+    if (p_pitch != q_pitch) return true;
+    const int64_t pitch = p_pitch, d = (((intptr_t)q - (intptr_t)p) % pitch + pitch) % pitch;
+    return d < p_row || d + q_row > pitch;
+}
 
 template <class T>
 struct QrVec {

@@ -95,15 +95,6 @@ void launch_reorder(const QrReorderArgs &a, hipStream_t st)
     reorder_kernel<PIECE, NR, IN_PLACE><<<a.end[a.n - 1], 256, 0, st>>>(a);
 }
 
-// Whether two arrays have a byte in common; columns of one matrix have none.
-bool rows_overlap(const void *p, size_t pn, int64_t p_row, int64_t p_pitch, const void *q, size_t qn, int64_t q_row, int64_t q_pitch)
-{
-    if (!qr_overlap(p, pn, q, qn)) return false;
-    if (p_pitch != q_pitch) return true;
-    const int64_t pitch = p_pitch, d = (((intptr_t)q - (intptr_t)p) % pitch + pitch) % pitch;
-    return d < p_row || d + q_row > pitch;
-}
-
 }  // namespace
 
 extern "C" qrnnt_status qrnnt_reorder_states(const qrnnt_state_rows *states, int32_t n_states, const int32_t *parent, int32_t B,
@@ -133,9 +124,9 @@ extern "C" qrnnt_status qrnnt_reorder_states(const qrnnt_state_rows *states, int
         const bool in_place = s.src == s.dst && s.src_pitch == s.dst_pitch && W == W_out;
         for (int j = 0; j < n_states; ++j) {
             const qrnnt_state_rows &o = states[j];
-            QR_REQUIRE((j == k && in_place) || !rows_overlap(s.dst, dst_bytes(k), s.row_bytes, s.dst_pitch, o.src, src_bytes(j), o.row_bytes, o.src_pitch),
+            QR_REQUIRE((j == k && in_place) || !qr_rows_overlap(s.dst, dst_bytes(k), s.row_bytes, s.dst_pitch, o.src, src_bytes(j), o.row_bytes, o.src_pitch),
                        QRNNT_ERR_RANGE);
-            QR_REQUIRE(j == k || !rows_overlap(s.dst, dst_bytes(k), s.row_bytes, s.dst_pitch, o.dst, dst_bytes(j), o.row_bytes, o.dst_pitch),
+            QR_REQUIRE(j == k || !qr_rows_overlap(s.dst, dst_bytes(k), s.row_bytes, s.dst_pitch, o.dst, dst_bytes(j), o.row_bytes, o.dst_pitch),
                        QRNNT_ERR_RANGE);
         }
         QR_REQUIRE(!qr_overlap(s.dst, dst_bytes(k), parent, (size_t)B * W_out * 4), QRNNT_ERR_RANGE);

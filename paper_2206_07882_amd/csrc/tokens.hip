@@ -383,10 +383,11 @@ extern "C" qrnnt_status qrnnt_rms_norm_quant(const void *x, const void *residual
     QR_REQUIRE(qr_aligned(x, e) && qr_aligned(residual, e) && qr_aligned(weight, e) && qr_aligned(sum_out, e) && qr_aligned(q, 16) && qr_aligned(scale, 4),
                QRNNT_ERR_ALIGN);
     if (residual != nullptr) {
-        const size_t bytes = qr_matrix_bytes(rows, cols, ld_sum, e);
-        QR_REQUIRE((sum_out == x && ld_sum == ld_x) || !qr_overlap(sum_out, bytes, x, qr_matrix_bytes(rows, cols, ld_x, e)), QRNNT_ERR_RANGE);
-        QR_REQUIRE((sum_out == residual && ld_sum == ld_residual) ||
-                       !qr_overlap(sum_out, bytes, residual, qr_matrix_bytes(rows, cols, ld_residual, e)), QRNNT_ERR_RANGE);
+        const auto apart = [&](const void *in, int64_t ld) {
+            return (sum_out == in && ld_sum == ld) || !qr_rows_overlap(sum_out, qr_matrix_bytes(rows, cols, ld_sum, e), cols * e, ld_sum * e,
+                                                                       in, qr_matrix_bytes(rows, cols, ld, e), cols * e, ld * e);
+        };
+        QR_REQUIRE(apart(x, ld_x) && apart(residual, ld_residual), QRNNT_ERR_RANGE);
     }
     QrTokenArgs a = {};
     a.x = x;  a.residual = residual;  a.weight = weight;  a.sum = sum_out;  a.rows = rows;  a.cols = cols;

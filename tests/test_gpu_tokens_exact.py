@@ -61,3 +61,20 @@ def test_scales_of_rows_whose_largest_value_passes_fp32(gpu_lib, dtype, cols):
     # quotient, mean, its root and reciprocal, product: 5 roundings, the mean's halved by the root
     assert (np.abs(scale.cpu().numpy().astype(np.float64) - want) <= 5 * 2.0 ** -24 * want).all()
     assert codes[0, 1] == 127 and codes[1, cols - 1] == 127 and int(codes.float().sum()) == 254
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_the_sum_beside_its_inputs_in_one_matrix(gpu_lib, dtype):
+    """x, residual and sum as columns of one matrix: their rows lie between one another and share no byte."""
+    q, rows, cols = gpu_lib, 9, 75
+    big = torch.randn((rows, 3 * cols), generator=torch.Generator().manual_seed(1)).to(dtype).to(DEV)
+    x, res = big[:, :cols], big[:, 2 * cols:]
+    want = q.rms_norm_quant(x.contiguous(), None, 1e-5, residual=res.contiguous())
+    before = big.clone()
+    got = q.rms_norm_quant(x, None, 1e-5, residual=res, sum_out=big[:, cols:2 * cols])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(x, before[:, :cols]) and torch.equal(res, before[:, 2 * cols:])
+    with pytest.raises(RuntimeError):   # a column of x among the sum's
+        q.rms_norm_quant(x, None, 1e-5, residual=res, sum_out=big[:, cols - 1:2 * cols - 1])
+    with pytest.raises(RuntimeError):
+        q.rms_norm_quant(x, None, 1e-5, residual=res, sum_out=big[:, cols + 1:2 * cols + 1])
