@@ -278,6 +278,13 @@ def _dtype(t: torch.dtype) -> int:
     return code
 
 
+def _int32(value, what: str):
+    """The value as it is: ctypes would drop the upper bits of a larger one."""
+    if not -_INT_MAX - 1 <= value <= _INT_MAX:
+        raise ValueError(f"{what} {value} does not fit 32 bits")
+    return value
+
+
 def _here(first: torch.Tensor, *others):
     """The tensors a call works on have to be on the current device, on whose current stream it runs."""
     device = torch._C._cuda_getDevice() if first.is_cuda else -1
@@ -373,7 +380,7 @@ def rms_norm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: 
 
 def linear_tokens_workspace(w: QMat, M: int) -> int:
     cw = w.c()
-    return int(load().qrnnt_linear_tokens_workspace(C.byref(cw), M))
+    return int(load().qrnnt_linear_tokens_workspace(C.byref(cw), _int32(M, "M")))
 
 
 def linear_tokens(w: QMat, codes: torch.Tensor, scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -616,7 +623,7 @@ def beam_step(score: torch.Tensor, fused: torch.Tensor, blank: int = 0, force_bl
 
 
 def beam_select_workspace(B: int, W: int, V: int, n_out: int) -> int:
-    return int(load().qrnnt_beam_select_workspace(B, W, V, n_out))
+    return int(load().qrnnt_beam_select_workspace(_int32(B, "B"), _int32(W, "W"), _int32(V, "V"), _int32(n_out, "n_out")))
 
 
 def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] = None, log_softmax: bool = True,
@@ -653,7 +660,7 @@ def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] 
     ns = torch.empty((B, K), dtype=torch.float32, device=dev)
     done = None if end_token is None else torch.empty((B, K), dtype=torch.bool, device=dev)
     _call("qrnnt_beam_select", _vector(score, torch.float32, rows), pl, _dtype(logits.dtype), ld, 1 if log_softmax else 0,
-          pf, -1 if end_token is None else end_token, B, W, V, K, par.data_ptr(), tok.data_ptr(), ns.data_ptr(),
+          pf, -1 if end_token is None else _int32(end_token, "end_token"), B, W, V, K, par.data_ptr(), tok.data_ptr(), ns.data_ptr(),
           None if done is None else done.data_ptr(), _addr(workspace), workspace.nbytes, _stream_handle())
     return par, tok, ns, done
 
