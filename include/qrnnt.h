@@ -408,8 +408,9 @@ qrnnt_status qrnnt_beam_step(const float *score, const float *fused, int32_t B, 
  * NULL; finished_out [device] uint8 [B,n_out] or NULL: 1 where the parent was finished or the token is end_token (no
  * token: -1), 0 elsewhere and for unfilled ranks.  W <= 64, n_out <= 64, B <= 2^21, V <= 2^30, W*V < 2^31.  No output may overlap an
  * input.
- * workspace [device]: qrnnt_beam_select_workspace bytes (0 on bad sizes), 256-byte aligned; calls that may run at the
- * same time need workspaces of their own.  B = 0 does nothing. */
+ * workspace [device]: qrnnt_beam_select_workspace bytes (0 on bad sizes), 256-byte aligned; the size for B, W, V and n_out does
+ * for every call with none of them larger.  Calls that may run at the same time need workspaces of their own.  B = 0 does
+ * nothing. */
 size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, int32_t n_out);
 qrnnt_status qrnnt_beam_select(const float *score, const void *logits, int32_t dtype, int64_t ld, int32_t log_softmax,
                                const uint8_t *finished, int32_t end_token, int32_t B, int32_t W, int32_t V,

@@ -548,11 +548,12 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
 // and 15.6, 16 x 32 x 600 16.7 and 13.4).  Whole rows of up to 8192 to 256 threads, longer ones in stretches of up to 16384 to 512
 // (64 x 16 x 32000 bf16, n_out 16: 24.8 us, by 8192 25.7; 16 x 16 x 32000 fp32, n_out 32: 17.6 and 19.6; 4 x 8 x 131072 12.1
 // and 13.1; only 2 x 2 x 50000 is better by 8192: 9.4 and 9.1).
-constexpr int SHORT = 2048;
-bool one_launch(int64_t rows, int W, int V) { return V <= 512 || (V <= SHORT && (W <= 24 || rows > 1024)); }
+constexpr int SHORT = 2048, STRETCH = 16384, FEW_ROWS = 1024;
+bool always_one_launch(int W, int V) { return V <= 512 || (V <= SHORT && W <= 24); }   // for any number of rows
+bool one_launch(int64_t rows, int W, int V) { return always_one_launch(W, V) || (V <= SHORT && rows > FEW_ROWS); }
 void plan_select(int V, int &n_parts, int &part)
 {
-    n_parts = (V + 16383) / 16384;
+    n_parts = (V + STRETCH - 1) / STRETCH;
     part = qr_round_up((V + n_parts - 1) / n_parts, 8);
     n_parts = (V + part - 1) / part;
 }
@@ -591,10 +592,11 @@ void launch_select(QrSelectArgs &a, void *workspace, hipStream_t st)
 extern "C" size_t qrnnt_beam_select_workspace(int32_t B, int32_t W, int32_t V, int32_t n_out)
 {
     if (!select_sizes_ok(B, W, V, n_out)) return 0;
-    const int64_t rows = (int64_t)(B > 0 ? B : 1) * W;
-    if (one_launch(rows, W, V)) return 256;   // (not used)
-    int n_parts, part;
-    plan_select(V, n_parts, part);
+    // what the largest call within these sizes takes: a smaller batch may go in two launches where this one goes in one
+    int64_t rows = (int64_t)(B > 0 ? B : 1) * W;
+    if (always_one_launch(W, V)) return 256;   // (not used)
+    if (V <= SHORT && rows > FEW_ROWS) rows = FEW_ROWS;
+    const int n_parts = (V + STRETCH - 1) / STRETCH;
     return heads_bytes(rows, n_parts) + (size_t)rows * n_parts * n_out * sizeof(QrCand);
 }
 
