@@ -217,8 +217,9 @@ qrnnt_status qrnnt_linear_quant(const qrnnt_qmat *w, const float *bias, float a_
  * of 16), 16-byte aligned; the bytes behind column cols may hold anything.  a_scale [device] fp32 [M].  bias [device]
  * fp32 [rows] or NULL.  y [device] [M, rows] of y_dtype (QRNNT_F32, _F16, _BF16; rounded once from fp32) with row
  * pitch ld_y elements >= rows.  workspace [device]: qrnnt_linear_tokens_workspace bytes, 256-byte aligned, or NULL
- * where that is 0: products of few rows and a long sum are cut along the sum.  Calls that may run at the same time
- * need workspaces of their own.  M = 0 does nothing. */
+ * where that is 0: products of few rows and a long sum are cut along the sum.  The size for M does for every call with the
+ * same weights and fewer tokens.  Calls that may run at the same time need workspaces of their own.  No output may overlap
+ * an input.  M = 0 does nothing. */
 size_t qrnnt_linear_tokens_workspace(const qrnnt_qmat *w, int32_t M);
 qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const int8_t *a, int32_t ld_a,
                                  const float *a_scale, int32_t M, void *y, int32_t y_dtype, int64_t ld_y,

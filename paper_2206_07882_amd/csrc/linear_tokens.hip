@@ -456,6 +456,11 @@ struct QrTileCost {
 };
 constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.26f, 0.43f, 1.1f, 1.9f}, {128, 512, 0.66f, 1.1f, 3.6f, 0.6f}, {256, 256, 1.03f, 1.4f, 9.6f, -1.4f}};
 
+// A sum of few columns is not cut (up to 1920 a launch more costs what eight parts save), nor one whose parts' sums, read and written, pass
+// 512 tokens x 128 rows for each chunk of it (the costs above choose 57 thousand at most): so what a call may need is known without its plan.
+int most_parts(int nkc) { return nkc < 16 ? 1 : nkc < 32 ? nkc / 4 : 8; }
+int64_t most_sums(int nkc) { return (int64_t)nkc << 16; }
+
 // Measured at each choice (us; few / small / middle / large): 32 x 1000 x 1000 (tokens x rows x columns) 3.4 / 4.5; 48 x 16000 x
 // 4000 14.1 / 11.9; 200 x 8000 x 500 - / 4.4 / 6.1 / 12.3; 4000 x 1024 x 4096 - / 30.8 / 27.2 / 39.1; 2000 x 5000 x 3000 - / 59 / 46 /
 // 37; 8192^3 - / 901 / 584 / 396.  300 x 1024 x 8192 on small tiles whole 21.2, in two parts 15.1, in four 12.9.
@@ -466,7 +471,8 @@ QrTokensPiece plan_piece(int rows, int K, int M, float &least)
     least = INFINITY;
     for (int kind = SMALL; kind <= LARGE; ++kind) {
         const QrTileCost &c = TILE_COST[kind];
-        for (int parts = 1; parts <= (kind == SMALL ? 8 : 1) && (parts == 1 || nkc / parts >= 4); ++parts) {
+        for (int parts = 1; parts <= (kind == SMALL ? most_parts(nkc) : 1); ++parts) {
+            if (parts > 1 && (int64_t)parts * M * qr_round_up(rows, 4) > most_sums(nkc)) break;
             const float join = parts == 1 ? 0.0f : 3.0f + (float)parts * M * rows * 8 / 4e6f;   // a launch, and the sums written and read at 4 TB/s
             const float t = c.time(c.tiles(rows, M) * parts, (nkc + parts - 1) / parts) + join;
             if (t < least) {
@@ -478,12 +484,17 @@ QrTokensPiece plan_piece(int rows, int K, int M, float &least)
     return best;
 }
 
+// Few tokens: beyond 16 their codes are fetched as often as the weights and more, so long or many rows go to tiles (tokens x rows x
+// columns, few / small tiles: 17 x 8192 x 8192 12.4 / 15.1 us; 32 x 32000 x 1024 8.0 / 8.9; 32 x 16384 x 8192 28.8 / 24.9; 48 x 2048 x
+// 2048 5.2 / 7.0; 64 x 2048 x 2048 5.8 / 7.0; 64 x 2048 x 4096 9.7 / 8.6)
+bool few_tokens(int rows, int K, int M)
+{
+    return M <= 16 || (M <= 32 && (rows <= 8192 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= (M <= 48 ? 4096 : 2048));
+}
+
 QrTokensPlan plan_linear_tokens(int rows, int K, int M)
 {
-    // few tokens: beyond 16 their codes are fetched as often as the weights and more, so long or many rows go to tiles (tokens x rows x
-    // columns, few / small tiles: 17 x 8192 x 8192 12.4 / 15.1 us; 32 x 32000 x 1024 8.0 / 8.9; 32 x 16384 x 8192 28.8 / 24.9; 48 x 2048 x
-    // 2048 5.2 / 7.0; 64 x 2048 x 2048 5.8 / 7.0; 64 x 2048 x 4096 9.7 / 8.6)
-    if (M <= 16 || (M <= 32 && (rows <= 8192 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= (M <= 48 ? 4096 : 2048))) return {{{FEW, 1, M}}, 1};
+    if (few_tokens(rows, K, M)) return {{{FEW, 1, M}}, 1};
     float least;
     QrTokensPlan best = {{plan_piece(rows, K, M, least)}, 1};
     // whole rounds of large tiles first, what would leave a round part empty in a launch of its own (6000 x 3000 x 5000: 121 us
@@ -577,9 +588,11 @@ bool tokens_weights_ok(const qrnnt_qmat *w) { return w != nullptr && w->rows > 0
 extern "C" size_t qrnnt_linear_tokens_workspace(const qrnnt_qmat *w, int32_t M)
 {
     if (!tokens_weights_ok(w) || M <= 0 || M > 1 << 28) return 0;
-    const QrTokensPlan plan = plan_linear_tokens(w->rows, w->cols, M);
-    const QrTokensPiece &last = plan.piece[plan.n - 1];   // (large tiles in front of it are not cut)
-    return last.parts > 1 ? (size_t)last.parts * last.M * qr_round_up(w->rows, 4) * 4 : 0;
+    // what the largest call of up to M tokens takes: fewer tokens may be cut where these are not
+    const int nkc = qr_round_up(w->cols, QRNNT_KCHUNK) / QRNNT_KCHUNK, parts = most_parts(nkc);
+    if (parts == 1 || few_tokens(w->rows, w->cols, M)) return 0;
+    const int64_t sums = (int64_t)parts * M * qr_round_up(w->rows, 4);
+    return (size_t)(sums < most_sums(nkc) ? sums : most_sums(nkc)) * 4;
 }
 
 extern "C" qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const int8_t *a, int32_t ld_a,

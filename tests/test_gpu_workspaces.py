@@ -23,3 +23,23 @@ def test_a_search_whose_batch_shrinks(gpu_lib, W, V, n, batches):
         got, want = q.beam_select(*args, workspace=ws[:need]), q.beam_select(*args)
         assert all(torch.equal(a, b) for a, b in zip(got[:3], want[:3]))
         assert bool((ws[need:] == 99).all())
+
+
+@pytest.mark.parametrize("N,K,tokens", [(4096, 4096, (700, 400, 77, 65, 64, 40, 20, 1)), (1024, 8192, (2000, 1024, 512, 300, 65, 33, 3)),
+                                        (8192, 8192, (300, 65, 64, 33, 17)), (130, 131071, (600, 100, 33)), (1000, 1283, (3000, 77, 5)),
+                                        (2600, 2500, (7215, 4494, 1412, 130))])
+def test_a_layer_whose_tokens_become_fewer(gpu_lib, N, K, tokens):
+    q, width = gpu_lib, (K + 15) // 16 * 16
+    m = q.pack_int8(torch.randint(-127, 128, (N, K), dtype=torch.int8, device=DEV, generator=gen(1)), q.LAYOUT_TILED,
+                    torch.rand(N, device=DEV, generator=gen(2)))
+    a = torch.randint(-127, 128, (tokens[0], width), dtype=torch.int8, device=DEV, generator=gen(3))
+    scale = torch.rand(tokens[0], device=DEV, generator=gen(4))
+    need = q.linear_tokens_workspace(m, tokens[0])
+    ws = torch.full((need + 4096,), 99, dtype=torch.uint8, device=DEV)
+    whole = None
+    for M in tokens:
+        y = q.linear_tokens(m, a[:M], scale[:M], workspace=ws[:need])
+        assert bool((ws[need:] == 99).all())
+        whole = y if whole is None else whole
+        assert torch.equal(y, whole[:M])   # (sums of whole numbers: the same in every way)
+        assert torch.equal(y, q.linear_tokens(m, a[:M], scale[:M]))

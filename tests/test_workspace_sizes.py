@@ -1,5 +1,6 @@
 """A workspace for the largest call does for the smaller ones: its size never falls as a call grows, also where a larger call is
 computed in another way that needs none."""
+import ctypes as C
 import random
 
 import pytest
@@ -30,3 +31,25 @@ def test_beam_select_over_every_size():
             if sizes[1] * sizes[2] < 1 << 31:
                 got.append(qrnnt.beam_select_workspace(*sizes))
         assert all(got) and rising(got), sizes
+
+
+def linear(rows, cols, M):
+    w = qrnnt.CQMat(0x1000, 0x2000, rows, cols, qrnnt.LAYOUT_TILED, 8)
+    return qrnnt.load().qrnnt_linear_tokens_workspace(C.byref(w), M)
+
+
+@pytest.mark.parametrize("rows,cols", [(1024, 4096), (8192, 8192), (4096, 4096), (1024, 8192), (64, 131071), (32000, 1024), (1000, 1283), (5000, 2048)])
+def test_linear_tokens_over_tokens(rows, cols):
+    sizes = [linear(rows, cols, M) for M in list(range(1, 1200)) + list(range(1200, 60000, 97)) + [1 << 20, 1 << 28]]
+    assert rising(sizes) and sizes[0] == 0
+    assert all(size <= 512 * 128 * 4 * ((cols + 127) // 128) for size in sizes)
+
+
+def test_linear_tokens_over_every_size():
+    rng = random.Random(2)
+    for _ in range(2000):
+        sizes = [int(16 * 2000 ** rng.random()), int(40 * 200 ** rng.random()), int(17 * 2000 ** rng.random())]
+        got = []
+        for f in (0.3, 0.5, 0.9, 0.99, 1, 1.01, 1.1, 2, 10):
+            got.append(linear(sizes[0], sizes[1], max(1, int(sizes[2] * f))))
+        assert rising(got), sizes
