@@ -1,5 +1,6 @@
 // 8-bit linear layers whose activations have a scale for each row: y[m,r] = a_scale[m] * row_scale[r] * sum + bias[r]
 // with exact int32 sums on the matrix units.
+#include <atomic>
 #include <type_traits>
 
 #include "elem.h"
@@ -522,12 +523,11 @@ void launch_tiles(const QrTokensLinear &p, int parts, hipStream_t st)
     using P = QrTile<MT, NT, WN, WM, D>;
     const int tn = (p.rows + P::BN - 1) / P::BN, tm = (p.M + P::BM - 1) / P::BM;
     const int places = P::WAVES == 8 ? 256 : 512;   // what 256 compute units hold
-    static bool allowed[QR_MAX_DEVICES];   // per device: more than 64 KiB of LDS
+    static std::atomic<bool> allowed[QR_MAX_DEVICES];   // per device: more than 64 KiB of LDS
     const int d = qr_current_device();
-    if (!allowed[d]) {
-        (void)hipFuncSetAttribute((const void *)linear_tokens_kernel<T, MT, NT, WN, WM, D>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
-        allowed[d] = true;
-    }
+    if (!allowed[d].load(std::memory_order_relaxed) &&
+        hipFuncSetAttribute((const void *)linear_tokens_kernel<T, MT, NT, WN, WM, D>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS) == hipSuccess)
+        allowed[d].store(true, std::memory_order_relaxed);   // (where it failed the launch says so, and the next call asks again)
     linear_tokens_kernel<T, MT, NT, WN, WM, D><<<dim3((unsigned)(tn * tm < places ? tn * tm : places), parts), P::THREADS, P::LDS, st>>>(p, tn, tm);
 }
 

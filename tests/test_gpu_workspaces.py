@@ -1,5 +1,7 @@
 """One workspace, made for the largest call, for all smaller ones: the bits of calls with a workspace of their own, and nothing
 written behind it."""
+from concurrent.futures import ThreadPoolExecutor
+
 import pytest
 import torch
 
@@ -43,3 +45,29 @@ def test_a_layer_whose_tokens_become_fewer(gpu_lib, N, K, tokens):
         whole = y if whole is None else whole
         assert torch.equal(y, whole[:M])   # (sums of whole numbers: the same in every way)
         assert torch.equal(y, q.linear_tokens(m, a[:M], scale[:M]))
+
+
+def test_first_calls_of_several_threads(gpu_lib):
+    """Every size of tile in every type, from four threads at once, each on a stream and with a workspace of its own."""
+    q, K = gpu_lib, 2048
+    sizes = [(70, 500), (700, 1000), (3000, 4200)]
+    ins = []
+    for M, N in sizes:
+        m = q.pack_int8(torch.randint(-127, 128, (N, K), dtype=torch.int8, device=DEV, generator=gen(N)), q.LAYOUT_TILED)
+        a = torch.randint(-127, 128, (M, K), dtype=torch.int8, device=DEV, generator=gen(M))
+        ins.append((m, a, torch.rand(M, device=DEV, generator=gen(5))))
+    torch.cuda.synchronize()
+
+    def work():
+        stream, out = torch.cuda.Stream(), []
+        with torch.cuda.stream(stream):
+            for i in ins:
+                out += [q.linear_tokens(*i, dtype=t) for t in (torch.float32, torch.float16, torch.bfloat16)]
+        stream.synchronize()
+        return out
+
+    with ThreadPoolExecutor(4) as pool:
+        got = [f.result() for f in [pool.submit(work) for _ in range(4)]]
+    want = work()
+    for out in got:
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
