@@ -126,8 +126,9 @@ __device__ __forceinline__ void odd_row(const T *h, const T *weight, int cols, f
     }
 }
 
-// Bound by memory: 16384 x 4096 bf16 with residual, 470 MB, in 84 us is 5.6 TB/s (a copy of 1 GiB on this card: 5.2); one row of
-// 4096 takes 4 us, the length of its chain.
+// Bound by memory: 16384 x 4096 bf16 with residual, 470 MB, in 83 us where calls follow one another is 5.6 TB/s (a copy of 1 GiB on this
+// card: 5.2), and 92 in the trace of a program that multiplies codes and scales in between; fp32, 872 MB, 146.  One row of 4096 takes 4
+// us, the length of its chain.
 // TPR threads to a row (up to 64: workgroups of 256 have several), PER vectors of 16 bytes to a thread; PER = 0: rows of any length, read
 // a second time for the codes.
 template <class T, bool NORM, int TPR, int PER>
@@ -314,7 +315,7 @@ void launch_tokens(const QrTokenArgs &a, hipStream_t st)
 {
     constexpr int V = QrVec<T>::N;
     // A row to as few threads as its registers allow, and vectors as even as can be: what a wave has beyond the row it skips, but a
-    // thread's part of it it computes (us at 4 to 16 thousand rows; a copy of as many bytes): 4096 bf16 with residual 84 (90), 1280 fp32
+    // thread's part of it it computes (us at 4 to 16 thousand rows; a copy of as many bytes): 4096 bf16 with residual 83 (90), 1280 fp32
     // 19.7 by 64 x 5, 20.4 by 128 x 3 (19.7), 2300 bf16 with residual 74 by 64 x 5, 70 by 128 x 3 (51), 2000 fp16 with residual 14.8 by
     // 128 x 2, 17.7 by 256 (10.8), 4104 bf16 with residual 100 by 256 x 3, 113 by 512 x 2 (91), 8192 bf16 with residual 34.9 by 512,
     // 37.2 by 256 (33.1), 12000 bf16 with residual 128 by 512 x 3, 165 by 1024 x 2 (132).

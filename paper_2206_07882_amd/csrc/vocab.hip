@@ -261,10 +261,9 @@ __device__ __forceinline__ unsigned quad_max(unsigned v)
 }
 
 // Long rows, first launch.  Grid: x = stretch, y (and z) = row; NT = 256 or 512 threads with NV vectors each.
-// Bound by the chain of its steps and by its arithmetic, of which the exponentials are most: of a workgroup's 8 us for 64 x 16 x 32000
-// bf16 logits (two workgroups one after the other at each place, 19 us in all, the second launch 6) loading takes 2 to 5, maximum,
-// sums, bound and ranks 1 each, gathering 1.6; other numbers of waves and logits to one change little, fetching a next
-// stretch ahead spills.
+// Bound by the chain of its steps: of a workgroup's 8 us for 64 x 16 x 32000 bf16 logits (two workgroups one after the other at each
+// place, 18 us in all, the second launch 6; vector units busy 41 % or a little more) loading takes 2 to 5, maximum, sums, bound and
+// ranks 1 each, gathering 1.6.  Other numbers of waves and logits to one change little, fetching a next stretch ahead spills.
 template <class T, int NV, int NT>
 __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs a)
 {
