@@ -185,8 +185,9 @@ qrnnt_status qrnnt_quantize_tokens(const void *x, int32_t dtype, int64_t rows, i
  *   y = h / sqrt(mean_k h^2 + eps) * weight;   scale[r] = max|y| / 127;   q = rne(127 y / max|y|).
  * The root divides all of a row alike, so the codes are those of h * weight and only the scale carries it.  weight
  * [device] [cols] of `dtype`, or NULL for 1.  All matrices are [rows, cols] of `dtype` with pitches of their own;
- * sum_out may be x or residual itself (same pitch), and may not overlap them otherwise.  eps >= 0.  q, scale and the
- * rows that are zero or not finite as in qrnnt_quantize_tokens. */
+ * sum_out may be x or residual itself (same pitch, where there is more than one row), and may not overlap them
+ * otherwise; columns of one matrix do not.  eps >= 0.  q, scale and the rows that are zero or not finite as in
+ * qrnnt_quantize_tokens. */
 qrnnt_status qrnnt_rms_norm_quant(const void *x, const void *residual, const void *weight, int32_t dtype, int64_t rows,
                                   int32_t cols, int64_t ld_x, int64_t ld_residual, float eps, void *sum_out,
                                   int64_t ld_sum, int8_t *q, int32_t ld_q, float *scale, void *stream);

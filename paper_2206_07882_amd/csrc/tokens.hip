@@ -385,7 +385,7 @@ extern "C" qrnnt_status qrnnt_rms_norm_quant(const void *x, const void *residual
                QRNNT_ERR_ALIGN);
     if (residual != nullptr) {
         const auto apart = [&](const void *in, int64_t ld) {
-            return (sum_out == in && ld_sum == ld) || !qr_rows_overlap(sum_out, qr_matrix_bytes(rows, cols, ld_sum, e), cols * e, ld_sum * e,
+            return (sum_out == in && (ld_sum == ld || rows == 1)) || !qr_rows_overlap(sum_out, qr_matrix_bytes(rows, cols, ld_sum, e), cols * e, ld_sum * e,
                                                                        in, qr_matrix_bytes(rows, cols, ld, e), cols * e, ld * e);
         };
         QR_REQUIRE(apart(x, ld_x) && apart(residual, ld_residual), QRNNT_ERR_RANGE);

@@ -78,3 +78,19 @@ def test_the_sum_beside_its_inputs_in_one_matrix(gpu_lib, dtype):
         q.rms_norm_quant(x, None, 1e-5, residual=res, sum_out=big[:, cols - 1:2 * cols - 1])
     with pytest.raises(RuntimeError):
         q.rms_norm_quant(x, None, 1e-5, residual=res, sum_out=big[:, cols + 1:2 * cols + 1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_one_row_in_place_by_views_of_different_pitch(gpu_lib, dtype):
+    """A single row has no pitch: two views of it are the same row."""
+    q, cols = gpu_lib, 75
+    big = torch.randn((6, 100), generator=torch.Generator().manual_seed(2)).to(dtype).to(DEV)
+    res = torch.randn((1, cols), generator=torch.Generator().manual_seed(3)).to(dtype).to(DEV)
+    for a, b in ((big[3:4, :cols], big[3, :cols].unsqueeze(0)), (big[4, :cols].unsqueeze(0), big[4:5, :cols])):
+        want, before = q.rms_norm_quant(a.clone(), None, 1e-5, residual=res), big.clone()
+        assert a.stride(0) != b.stride(0)
+        got = q.rms_norm_quant(a, None, 1e-5, residual=res, sum_out=b)
+        assert all(torch.equal(x, y) for x, y in zip(got, want)) and torch.equal(a, want[2])
+        assert torch.equal(big[:3], before[:3]) and torch.equal(big[5:], before[5:]) and torch.equal(big[:, cols:], before[:, cols:])
+    with pytest.raises(RuntimeError):
+        q.rms_norm_quant(big[3:4, :cols], None, 1e-5, residual=res, sum_out=big[3:4, 1:cols + 1])
