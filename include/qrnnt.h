@@ -226,6 +226,62 @@ qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const i
                                  const float *a_scale, int32_t M, void *y, int32_t y_dtype, int64_t ld_y,
                                  void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- microscaled 4-bit floats: a scale for each block of 32 columns, and the linear layer of them ----
+ *
+ * Weights and activations as 4-bit floats (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, codes 0 to 7 and 8 to 15)
+ * with a power of two for each block of 32 neighbouring columns of a row (E8M0: the byte e stands for 2^(e-127), 255 for
+ * NaN), which one loud value costs no more than its own block's resolution.  value[r,k] = E2M1(code[r,k]) * 2^(e[r,k/32]-127).
+ * A matrix of codes has two to a byte, the even column in bits 0-3, rows at a pitch of ld bytes (a multiple of 16, at least
+ * qrnnt_mx4_pitch(cols) = 16 ceil(cols/32)); its scales are bytes at a pitch of ld_scale (a multiple of 8, at least
+ * qrnnt_mx4_scale_pitch(cols) = ceil(cols/32) rounded up to 8).  Codes start on 16-byte boundaries, scales on 8-byte ones.
+ * Both pitches are 0 for a number of columns below 1 or above 2^30.  QRNNT_ERR_UNSUPPORTED: more than 2^31 - 1 rows or 2^30
+ * columns to quantize, 2^28 rows or tokens or QRNNT_MX4_MAX_COLS columns of a linear layer, matrices of more than 2^60 elements. */
+#define QRNNT_MX4_MAX_COLS (1 << 20)
+int32_t qrnnt_mx4_pitch(int32_t cols);
+int32_t qrnnt_mx4_scale_pitch(int32_t cols);
+
+/* Per block with a = max|x|: e = max(floor(log2 a) - 2 + 127, 0), code = x / 2^(e-127) rounded to the nearest of E2M1, ties to
+ * the even code, magnitudes above 6 to 6 (a lies between 4 and 8 steps).  Exact but for that rounding.  A block of zeros gets
+ * scale byte 127, one that holds a value that is not finite gets scale byte 255 and codes 0.  x [device] [rows, cols] of `dtype`
+ * (QRNNT_F32, _F16, _BF16) with row pitch ld_x elements, rows at any element.  q, scale [device]: the codes behind column cols
+ * of the last block are written as zero, the scales behind the last block up to qrnnt_mx4_scale_pitch(cols) as 127; bytes behind
+ * those are left as they are.  No output may overlap an input.  rows = 0 does nothing. */
+qrnnt_status qrnnt_quantize_mx4(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t ld_x, uint8_t *q,
+                                int32_t ld_q, uint8_t *scale, int32_t ld_scale, void *stream);
+
+/* The values that codes and scales stand for: x [device] [rows, cols] of `dtype`, row pitch ld_x elements.  fp32 and bf16 hold them
+ * all (up to scale byte 252, the largest that the quantizer writes), fp16 rounds those that it does not hold.  rows = 0 does
+ * nothing. */
+qrnnt_status qrnnt_dequantize_mx4(const uint8_t *q, int32_t ld_q, const uint8_t *scale, int32_t ld_scale, int64_t rows,
+                                  int32_t cols, void *x, int32_t dtype, int64_t ld_x, void *stream);
+
+/* Weights, laid out once for qrnnt_linear_mx4 from codes and scales (as qrnnt_quantize_mx4 writes them, or from a model that is
+ * in this form already; here scales may start anywhere and ld_scale be any number from ceil(cols/32)).  packed_out [device]:
+ * qrnnt_pack_mx4_bytes bytes (0 on bad or unsupported sizes), 16-byte aligned, fully written. */
+size_t qrnnt_pack_mx4_bytes(int32_t rows, int32_t cols);
+qrnnt_status qrnnt_pack_mx4(const uint8_t *q, int32_t ld_q, const uint8_t *scale, int32_t ld_scale, int32_t rows,
+                            int32_t cols, void *packed_out, void *stream);
+
+/* One packed matrix. */
+typedef struct {
+    const void *packed;      /* [device] written by qrnnt_pack_mx4, 16-byte aligned */
+    int32_t rows, cols;      /* logical size */
+} qrnnt_mx4;
+
+/* y[m,r] = sum_k value_w[r,k] * value_a[m,k] + bias[r], summed in fp32 and rounded once to y_dtype.  Products are exact; a matrix
+ * instruction adds 128 of them to a sum at a time, which rounds by at most 2^-23 of the largest magnitude in it.  The order of the
+ * sums depends on the sizes of the call, not on its data.  A row of a or w with a NaN scale gives NaN.
+ * a, a_scale [device]: M rows as qrnnt_quantize_mx4 writes them.  The codes behind column cols and the bytes behind the row may hold
+ * anything, the scales from ceil(cols/32) up to qrnnt_mx4_scale_pitch(cols) anything but 255.  bias [device] fp32 [rows] or
+ * NULL.  y [device] [M, rows] of y_dtype with row pitch ld_y elements >= rows.  workspace [device]:
+ * qrnnt_linear_mx4_workspace bytes, 256-byte aligned, or NULL where that is 0.  The size for M does for every call with the
+ * same weights and fewer tokens.  Calls that may run at the same time need workspaces of their own.  No output may overlap
+ * an input.  M = 0 does nothing. */
+size_t qrnnt_linear_mx4_workspace(const qrnnt_mx4 *w, int32_t M);
+qrnnt_status qrnnt_linear_mx4(const qrnnt_mx4 *w, const float *bias, const uint8_t *a, int32_t ld_a, const uint8_t *a_scale,
+                              int32_t ld_scale, int32_t M, void *y, int32_t y_dtype, int64_t ld_y, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
 /* ---- LSTM: one step for a set of hypotheses (Sec. 3.2, Sec. 3.4) ---- */
 
 /* For n in [0,N): input row x_codes[x_row ? x_row[n] : n] (length I, row pitch qrnnt_act_pitch(I)), previous
@@ -421,6 +477,28 @@ qrnnt_status qrnnt_beam_select(const float *score, const void *logits, int32_t d
                                const uint8_t *finished, int32_t end_token, int32_t B, int32_t W, int32_t V,
                                int32_t n_out, int32_t *parent_out, int32_t *token_out, float *score_out,
                                uint8_t *finished_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Scores of given tokens, from logits (rescoring of hypotheses by a language model: log P of Eq. 1 for the tokens they hold).  With
+ * lse = log sum_k exp(logits[r,k]) and p_k = exp(logits[r,k] - lse), per row r
+ *   logp_out[r]    = logits[r, token[r]] - lse
+ *   entropy_out[r] = -sum_k p_k log p_k
+ *   top_token_out, top_logp_out [rows, n_top]: the n_top tokens with the largest logits, largest first, equal ones lowest first,
+ *   and their logits - lse.
+ * A logit of -inf is a token that cannot be: p = 0, never among the best.  Ranks without a token get token -1 and -inf.  A row whose
+ * logits are all -inf gives logp -inf, entropy 0 and no tokens; one with a logit that is NaN or +inf gives NaN, NaN and no
+ * tokens.  token[r] < 0 (padding) gives logp 0, whatever the row holds; token[r] >= V gives NaN.
+ * The order is exact.  Exponentials are summed in fp32 32 at a time, then in fp64: lse is off by at most (25 + 2 ln V) 2^-23, the
+ * entropy by at most 2 (9 + ln V)(25 + 2 ln V) 2^-23; on top of that each result is rounded to fp32.
+ * logits [device] [rows, V] of `dtype`, row pitch ld elements, rows at any element.  token [device] int32 [rows], or NULL where
+ * logp_out is NULL.  Any of logp_out, entropy_out [device] fp32 [rows] may be NULL; top_token_out int32 and top_logp_out fp32
+ * [device] may be NULL where n_top is 0.  n_top <= 64, rows <= 2^25, V <= 2^30.  No output may overlap an input.  workspace [device]:
+ * qrnnt_token_scores_workspace bytes (0 on bad sizes), 256-byte aligned: long rows that are few are cut into parts; the size for
+ * rows, V and n_top does for every call with none of them larger.  Calls that may run at the same time need workspaces of
+ * their own.  rows = 0 does nothing. */
+size_t qrnnt_token_scores_workspace(int32_t rows, int32_t V, int32_t n_top);
+qrnnt_status qrnnt_token_scores(const void *logits, int32_t dtype, int64_t ld, const int32_t *token, int32_t rows, int32_t V,
+                                int32_t n_top, float *logp_out, float *entropy_out, int32_t *top_token_out,
+                                float *top_logp_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Reordering of the states that belong to hypotheses (codes, cells, histories, caches) after a selection, all of them in
  * one launch: for every array, row b*W_out + j of dst becomes row b*W + parent[b,j] of src, byte for byte.  Rows with

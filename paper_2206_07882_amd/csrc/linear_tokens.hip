@@ -113,19 +113,6 @@ __global__ __launch_bounds__(64 * WAVES) void linear_tokens_few_kernel(const QrT
     }
 }
 
-// One float a lane straight to LDS.
-__device__ __forceinline__ void qr_load_lds4(const void *gptr, unsigned lds_addr)
-{
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr), "s"(lds_addr) : "memory");
-}
-
-// Past the caches.  In asm: the compiler makes one ordinary store of a nontemporal and an ordinary one in two branches.
-// (s_nop 1: two wait states before the data registers of a wide store may be rewritten.)
-__device__ __forceinline__ void store_past(float *p, v4f v)
-{
-    asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" ::"v"(p), "v"(v) : "memory");
-}
-
 // Many tokens: the matrix units are what is kept busy.  A workgroup of WN x WM waves has BN = 16*MT*WN weight rows x
 // BM = 16*NT*WM tokens.  LDS holds the weights of 2D steps of 64 columns (1 KiB blocks as the blob has them: operand order) and
 // the activations of D chunks of 128 (1 KiB blocks of 8 tokens x 128 bytes, lane l of the loading wave fetching token l/8's
@@ -369,7 +356,7 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_tokens_kernel(const QrTok
                     if (tm0 + t < p.M) {
                         if (r0 + r + E <= p.rows) {
                             if (!pieces) *(typename QrVec<T>::any *)y = out[i];
-                            else if (MT * WN >= 16) store_past((float *)y, __builtin_bit_cast(v4f, out[i]));
+                            else if (MT * WN >= 16) qr_store_past((float *)y, __builtin_bit_cast(v4f, out[i]));
                             else qr_store_through((float *)y, __builtin_bit_cast(v4f, out[i]));
                         } else {
 #pragma unroll

@@ -53,6 +53,12 @@ __device__ __forceinline__ void qr_load_lds16(const void *gptr, unsigned lds_add
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gptr), "s"(lds_addr) : "memory");
 }
 
+// Four bytes a lane.
+__device__ __forceinline__ void qr_load_lds4(const void *gptr, unsigned lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr), "s"(lds_addr) : "memory");
+}
+
 template <int N>
 __device__ __forceinline__ void qr_wait_vmcnt()
 {

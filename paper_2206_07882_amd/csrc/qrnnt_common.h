@@ -132,6 +132,13 @@ __device__ __forceinline__ void qr_store_through(int8_t *p, unsigned v)   // 4 c
     asm volatile("global_store_dword %0, %1, off sc1" ::"v"(p), "v"(v) : "memory");
 }
 
+// Past the caches.  In asm: the compiler makes one ordinary store of a nontemporal and an ordinary one in two branches.
+// (s_nop 1: two wait states before the data registers of a wide store may be rewritten.)
+__device__ __forceinline__ void qr_store_past(float *p, v4f v)
+{
+    asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" ::"v"(p), "v"(v) : "memory");
+}
+
 // Wave-wide max / min of a 32-bit unsigned value on the DPP path (row scans, then
 // the two cross-row broadcasts of gfx9), result broadcast through lane 63.
 template <bool IS_MAX>

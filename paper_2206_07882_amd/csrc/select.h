@@ -126,3 +126,66 @@ __device__ __forceinline__ void qr_rank(const QrCand *list, int M, int W, int ti
     }
 }
 
+// A bound from below of the K-th largest of 256 groups' keys, four to a lane: the K-th largest itself, or a little less (as soon as
+// no more than `enough` groups pass); 0 if fewer than K groups have one.  top: the largest.  By bits of the distance from it, which
+// begin where the groups' distances do: the first bits of the keys themselves tell little apart.
+__device__ __forceinline__ unsigned qr_bound_of(const unsigned (&g)[4], unsigned top, int K, int enough)
+{
+    unsigned d[4], far = 0u;
+    int some = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        d[i] = g[i] ? top - g[i] : ~0u;
+        far = g[i] && d[i] > far ? d[i] : far;
+        some += (int)__popcll(__ballot(g[i] != 0u));
+    }
+    if (some < K) return 0u;   // uniform
+    far = qr_wave_reduce_u32<true>(far);
+    const int bits = 32 - __builtin_clz(far | 1u);
+    unsigned D = bits == 32 ? ~0u : (1u << bits) - 1u;   // (no trial is ~0, the distance of what is none)
+    for (int bit = bits - 1; bit >= 0; --bit) {
+        const unsigned trial = D & ~(1u << bit);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += (int)__popcll(__ballot(d[i] <= trial));
+        if (n >= K) {
+            D = trial;   // uniform
+            if (n <= enough) break;
+        }
+    }
+    return D < top ? top - D : 1u;
+}
+
+// Key of a logit; 0 for -inf and NaN, which are never taken.
+__device__ __forceinline__ unsigned qr_logit_key(float f) { return f > -INFINITY ? qr_float_key(f + 0.0f) : 0u; }
+
+// Sum over the wave, on the DPP path (row scans, then the two cross-row broadcasts of gfx9), in all lanes.
+__device__ __forceinline__ double qr_wave_sum(double d)
+{
+#define QR_DPP_ADD(ctrl, rmask)                                                                                          \
+    {                                                                                                                    \
+        const unsigned long long u = (unsigned long long)__double_as_longlong(d);                                        \
+        const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, rmask, 0xf, false);          \
+        const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, rmask, 0xf, false);  \
+        d += __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));                                       \
+    }
+    QR_DPP_ADD(0x111, 0xf)   // row_shr:1
+    QR_DPP_ADD(0x112, 0xf)   // row_shr:2
+    QR_DPP_ADD(0x114, 0xf)   // row_shr:4
+    QR_DPP_ADD(0x118, 0xf)   // row_shr:8
+    QR_DPP_ADD(0x142, 0xa)   // row_bcast:15 into rows 1 and 3
+    QR_DPP_ADD(0x143, 0xc)   // row_bcast:31 into rows 2 and 3
+#undef QR_DPP_ADD
+    const unsigned long long u = (unsigned long long)__double_as_longlong(d);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, 63), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), 63);
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+
+// Largest of four neighbouring lanes.
+__device__ __forceinline__ unsigned qr_quad_max(unsigned v)
+{
+    unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true);
+    v = o > v ? o : v;
+    o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true);
+    return o > v ? o : v;
+}

@@ -42,36 +42,6 @@ struct QrSelectArgs {
 __device__ __forceinline__ bool is_finished(const QrSelectArgs &a, int64_t row) { return a.finished && a.finished[row]; }
 __device__ __forceinline__ bool reads_logits(const QrSelectArgs &a, int64_t row) { return a.score[row] > -INFINITY && !is_finished(a, row); }
 
-// A bound from below of the K-th largest of 256 groups' keys, four to a lane: the K-th largest itself, or a little less (as soon as
-// no more than `enough` groups pass); 0 if fewer than K groups have one.  top: the largest.  By bits of the distance from it, which
-// begin where the groups' distances do: the first bits of the keys themselves tell little apart.
-__device__ __forceinline__ unsigned bound_of(const unsigned (&g)[4], unsigned top, int K, int enough)
-{
-    unsigned d[4], far = 0u;
-    int some = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        d[i] = g[i] ? top - g[i] : ~0u;
-        far = g[i] && d[i] > far ? d[i] : far;
-        some += (int)__popcll(__ballot(g[i] != 0u));
-    }
-    if (some < K) return 0u;   // uniform
-    far = qr_wave_reduce_u32<true>(far);
-    const int bits = 32 - __builtin_clz(far | 1u);
-    unsigned D = bits == 32 ? ~0u - 1u : (1u << bits) - 1u;
-    for (int bit = bits - 1; bit >= 0; --bit) {
-        const unsigned trial = D & ~(1u << bit);
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) n += (int)__popcll(__ballot(d[i] <= trial));
-        if (n >= K) {
-            D = trial;   // uniform
-            if (n <= enough) break;
-        }
-    }
-    return D < top ? top - D : 1u;
-}
-
 // A value as a word: larger double <=> larger word; 0 for what is never taken.
 typedef unsigned long long QrValue;
 __device__ __forceinline__ QrValue value_word(double v)
@@ -229,37 +199,6 @@ struct QrLogits {
         }
     }
 };
-__device__ __forceinline__ unsigned logit_key(float f) { return f > -INFINITY ? qr_float_key(f + 0.0f) : 0u; }   // (0 for NaN, too)
-// Sum over the wave, on the DPP path (row scans, then the two cross-row broadcasts of gfx9), in all lanes.
-__device__ __forceinline__ double wave_sum(double d)
-{
-#define QR_DPP_ADD(ctrl, rmask)                                                                                          \
-    {                                                                                                                    \
-        const unsigned long long u = (unsigned long long)__double_as_longlong(d);                                        \
-        const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, rmask, 0xf, false);          \
-        const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, rmask, 0xf, false);  \
-        d += __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));                                       \
-    }
-    QR_DPP_ADD(0x111, 0xf)   // row_shr:1
-    QR_DPP_ADD(0x112, 0xf)   // row_shr:2
-    QR_DPP_ADD(0x114, 0xf)   // row_shr:4
-    QR_DPP_ADD(0x118, 0xf)   // row_shr:8
-    QR_DPP_ADD(0x142, 0xa)   // row_bcast:15 into rows 1 and 3
-    QR_DPP_ADD(0x143, 0xc)   // row_bcast:31 into rows 2 and 3
-#undef QR_DPP_ADD
-    const unsigned long long u = (unsigned long long)__double_as_longlong(d);
-    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, 63), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), 63);
-    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
-}
-// Largest of four neighbouring lanes.
-__device__ __forceinline__ unsigned quad_max(unsigned v)
-{
-    unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true);
-    v = o > v ? o : v;
-    o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true);
-    return o > v ? o : v;
-}
-
 // Long rows, first launch.  Grid: x = stretch, y (and z) = row; NT = 256 or 512 threads with NV vectors each.
 // Bound by the chain of its steps: of a workgroup's 8 us for 64 x 16 x 32000 bf16 logits (two workgroups one after the other at each
 // place, 18 us in all, the second launch 6; vector units busy 41 % or a little more) loading takes 2 to 5, maximum, sums, bound and
@@ -282,9 +221,9 @@ __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs 
     f.load(x, n, tid, NT);
     const float largest = f.largest();   // (NaN is found in the sum)
     if (NT == 256) {
-        group_best[tid] = logit_key(largest);
+        group_best[tid] = qr_logit_key(largest);
     } else {
-        const unsigned k = logit_key(largest), o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)k, 0xB1, 0xf, 0xf, true);   // its neighbour's
+        const unsigned k = qr_logit_key(largest), o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)k, 0xB1, 0xf, 0xf, true);   // its neighbour's
         if ((tid & 1) == 0) group_best[tid >> 1] = o > k ? o : k;
     }
     __syncthreads();
@@ -297,10 +236,10 @@ __global__ __launch_bounds__(NT, 8) void select_parts_kernel(const QrSelectArgs 
     top_key = qr_wave_reduce_u32<true>(top_key);
     const float top = top_key ? qr_key_float(top_key) : -INFINITY;
     if (a.log_softmax) {
-        const double d = wave_sum((double)f.sum_exp(top_key ? top : 0.0f));
+        const double d = qr_wave_sum((double)f.sum_exp(top_key ? top : 0.0f));
         if (lane == 0) sums[wave] = d;
     }
-    const unsigned T_key = bound_of(g, top_key, a.K, a.K + a.K / 4);
+    const unsigned T_key = qr_bound_of(g, top_key, a.K, a.K + a.K / 4);
     const float least = T_key > 0x00800000u ? qr_key_float(T_key) : -FLT_MAX;   // (keys up to there are those of -inf and below)
     auto cand = [&](float l, int i) { return qr_cand(qr_float_key(l + 0.0f), first + ((i / V) * NT + tid) * V + i % V); };
     f.hits(least, [&](float l, int i) {
@@ -436,7 +375,7 @@ __global__ __launch_bounds__(NT) void select_beam_kernel(const QrSelectArgs a)
     if (NT == 256) {
         group_best[tid] = top;
     } else {
-        const unsigned k = quad_max(top);
+        const unsigned k = qr_quad_max(top);
         if ((tid & 3) == 0) group_best[tid >> 2] = k;
     }
     __syncthreads();
@@ -446,7 +385,7 @@ __global__ __launch_bounds__(NT) void select_beam_kernel(const QrSelectArgs a)
         g[i] = group_best[i * 64 + lane];
         most = g[i] > most ? g[i] : most;
     }
-    const unsigned T = bound_of(g, qr_wave_reduce_u32<true>(most), a.K, a.K + a.K / 4);
+    const unsigned T = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.K, a.K + a.K / 4);
     if (top >= T)
         each([&](const QrPick &p) {
             if ((unsigned)(p.v >> 32) >= T) push(list, p);
@@ -477,10 +416,10 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
             const float largest = f.largest();
             row.log_sum = 0.0;
             if (a.log_softmax) {
-                const unsigned k = qr_wave_reduce_u32<true>(logit_key(largest));
+                const unsigned k = qr_wave_reduce_u32<true>(qr_logit_key(largest));
                 const float top = k ? qr_key_float(k) : -INFINITY;
                 row.top = (double)top;
-                row.log_sum = log(wave_sum((double)f.sum_exp(top)));   // (of -inf alone: NaN)
+                row.log_sum = log(qr_wave_sum((double)f.sum_exp(top)));   // (of -inf alone: NaN)
             }
             if (largest > -INFINITY) {
                 const unsigned k = (unsigned)(row(largest) >> 32);
@@ -495,7 +434,7 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
     if (a.W <= 4) {   // groups: lanes of 4 waves, or quads of 16
         if (wave < 4) group_best[tid] = best;
     } else {
-        best = quad_max(best);
+        best = qr_quad_max(best);
         if ((lane & 3) == 0) group_best[tid >> 2] = best;
     }
     __syncthreads();
@@ -505,7 +444,7 @@ __global__ __launch_bounds__(1024) void select_short_kernel(const QrSelectArgs a
         g[i] = group_best[i * 64 + lane];
         most = g[i] > most ? g[i] : most;
     }
-    const unsigned Tk = bound_of(g, qr_wave_reduce_u32<true>(most), a.K, a.K + a.K / 4);
+    const unsigned Tk = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.K, a.K + a.K / 4);
     for (int w = wave; w < a.W; w += 16) {
         const QrRowValue row = rows[w];
         if (row.log_sum == row.log_sum) {

@@ -60,7 +60,9 @@ class CModel(C.Structure):
 EXPORTS = ["qrnnt_status_str", "qrnnt_abi_version", "qrnnt_pack_int4_bytes", "qrnnt_pack_int4", "qrnnt_unpack_int4",
            "qrnnt_pack_int8_bytes", "qrnnt_pack_int8", "qrnnt_quantize_act8", "qrnnt_act_pitch", "qrnnt_quantize_act_rows",
            "qrnnt_quantize_act", "qrnnt_quantize_tokens", "qrnnt_rms_norm_quant", "qrnnt_linear", "qrnnt_linear_quant",
-           "qrnnt_linear_tokens_workspace", "qrnnt_linear_tokens", "qrnnt_lstm_step", "qrnnt_lstm_layer_workspace", "qrnnt_lstm_layer",
+           "qrnnt_linear_tokens_workspace", "qrnnt_linear_tokens", "qrnnt_mx4_pitch", "qrnnt_mx4_scale_pitch",
+           "qrnnt_quantize_mx4", "qrnnt_dequantize_mx4", "qrnnt_pack_mx4_bytes", "qrnnt_pack_mx4", "qrnnt_linear_mx4_workspace",
+           "qrnnt_linear_mx4", "qrnnt_token_scores_workspace", "qrnnt_token_scores", "qrnnt_lstm_step", "qrnnt_lstm_layer_workspace", "qrnnt_lstm_layer",
            "qrnnt_input_projection", "qrnnt_input_table", "qrnnt_lstm_step_group", "qrnnt_lstm_step_group_listed",
            "qrnnt_bilstm_layer_workspace", "qrnnt_bilstm_layer", "qrnnt_lstm_layer_static",
            "qrnnt_joint_fuse", "qrnnt_beam_step", "qrnnt_beam_select_workspace", "qrnnt_beam_select", "qrnnt_reorder_states",
@@ -110,6 +112,18 @@ def load():
         lib.qrnnt_linear_tokens_workspace.restype = size
         lib.qrnnt_linear_tokens_workspace.argtypes = [vp, i32]
         lib.qrnnt_linear_tokens.argtypes = [vp, vp, vp, i32, vp, i32, vp, i32, i64, vp, size, vp]
+        lib.qrnnt_mx4_pitch.argtypes = lib.qrnnt_mx4_scale_pitch.argtypes = [i32]
+        lib.qrnnt_quantize_mx4.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, i32, vp]
+        lib.qrnnt_dequantize_mx4.argtypes = [vp, i32, vp, i32, i64, i32, vp, i32, i64, vp]
+        lib.qrnnt_pack_mx4_bytes.restype = size
+        lib.qrnnt_pack_mx4_bytes.argtypes = [i32, i32]
+        lib.qrnnt_pack_mx4.argtypes = [vp, i32, vp, i32, i32, i32, vp, vp]
+        lib.qrnnt_linear_mx4_workspace.restype = size
+        lib.qrnnt_linear_mx4_workspace.argtypes = [vp, i32]
+        lib.qrnnt_linear_mx4.argtypes = [vp, vp, vp, i32, vp, i32, i32, vp, i32, i64, vp, size, vp]
+        lib.qrnnt_token_scores_workspace.restype = size
+        lib.qrnnt_token_scores_workspace.argtypes = [i32, i32, i32]
+        lib.qrnnt_token_scores.argtypes = [vp, i32, i64, vp, i32, i32, i32, vp, vp, vp, vp, vp, size, vp]
         lib.qrnnt_beam_select_workspace.restype = size
         lib.qrnnt_beam_select_workspace.argtypes = [i32, i32, i32, i32]
         lib.qrnnt_beam_select.argtypes = [vp, vp, i32, i64, i32, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, size, vp]
@@ -309,7 +323,7 @@ def _matrix(t: torch.Tensor, dtype, rows: int, cols: int):
         if rows > 1:
             raise ValueError("rows must not overlap")
         pitch = cols
-    if rows > _INT_MAX or cols > _INT_MAX or pitch > _INT_MAX and dtype is torch.int8:   # (ctypes would drop the upper bits)
+    if rows > _INT_MAX or cols > _INT_MAX or pitch > _INT_MAX and dtype in (torch.int8, torch.uint8):   # (ctypes would drop the upper bits)
         raise ValueError(f"a matrix of {rows} x {cols}, pitch {pitch}, is too large")
     return t.data_ptr(), pitch
 
@@ -407,6 +421,117 @@ def linear_tokens(w: QMat, codes: torch.Tensor, scale: torch.Tensor, bias: Optio
     n_ws = 0 if workspace is None else workspace.nbytes
     _call("qrnnt_linear_tokens", C.byref(cw), _vector(bias, torch.float32, w.rows), pa, ld_a, _vector(scale, torch.float32, M), M,
           py, kind, ld_y, _addr(workspace) if n_ws else None, n_ws, _stream_handle())
+    return out
+
+
+class CMx4(C.Structure):
+    _fields_ = [("packed", C.c_void_p), ("rows", C.c_int32), ("cols", C.c_int32)]
+
+
+class Mx4Mat:
+    """Weights in microscaled 4-bit floats, packed for linear_mx4."""
+
+    def __init__(self, packed: torch.Tensor, rows: int, cols: int):
+        self.packed, self.rows, self.cols = packed, rows, cols
+
+    def c(self) -> CMx4:
+        return CMx4(self.packed.data_ptr(), self.rows, self.cols)
+
+
+def mx4_pitch(cols: int) -> int:
+    """Bytes of a row of codes."""
+    return load().qrnnt_mx4_pitch(_int32(cols, "cols"))
+
+
+def mx4_scale_pitch(cols: int) -> int:
+    """Bytes of a row of block scales."""
+    return load().qrnnt_mx4_scale_pitch(_int32(cols, "cols"))
+
+
+def _mx4(codes: torch.Tensor, scale: torch.Tensor, rows: int, cols: int):
+    """(address and pitch of the codes, address and pitch of the scales) of [rows, cols] values."""
+    width, n_scale = (cols + 31) // 32 * 16, (cols + 255) // 256 * 8
+    pq, ld_q = _matrix(codes, torch.uint8, rows, codes.shape[-1])
+    ps, ld_s = _matrix(scale, torch.uint8, rows, scale.shape[-1])
+    if codes.shape[1] < width or scale.shape[1] < n_scale:
+        raise ValueError(f"rows of {cols} columns take {width} bytes of codes and {n_scale} scales, got {codes.shape[1]} and {scale.shape[1]}")
+    return pq, width if rows <= 1 else ld_q, ps, n_scale if rows <= 1 else ld_s
+
+
+def quantize_mx4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """[rows, cols] of float32, float16 or bfloat16 (rows may lie apart) -> uint8 codes [rows, mx4_pitch(cols)] (two columns to
+    a byte) and uint8 scales [rows, mx4_scale_pitch(cols)]: 4-bit floats with a power of two for each block of 32 columns
+    (qrnnt_quantize_mx4)."""
+    _here(x, codes, scale)
+    dtype = x.dtype
+    rows, cols = x.shape
+    px, ld = _matrix(x, dtype, rows, cols)
+    if codes is None:
+        codes = torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=x.device)
+    if scale is None:
+        scale = torch.empty((rows, (cols + 255) // 256 * 8), dtype=torch.uint8, device=x.device)
+    pq, ld_q, ps, ld_s = _mx4(codes, scale, rows, cols)
+    _call("qrnnt_quantize_mx4", px, _dtype(dtype), rows, cols, ld, pq, ld_q, ps, ld_s, _stream_handle())
+    return codes, scale
+
+
+def dequantize_mx4(codes: torch.Tensor, scale: torch.Tensor, cols: int, dtype: torch.dtype = torch.float32,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values [rows, cols] that codes and scales stand for (qrnnt_dequantize_mx4)."""
+    _here(codes, scale, out)
+    rows = codes.shape[0]
+    pq, ld_q, ps, ld_s = _mx4(codes, scale, rows, _int32(cols, "cols"))
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    px, ld = _matrix(out, out.dtype, rows, cols)
+    _call("qrnnt_dequantize_mx4", pq, ld_q, ps, ld_s, rows, cols, px, _dtype(out.dtype), ld, _stream_handle())
+    return out
+
+
+def pack_mx4(codes: torch.Tensor, scale: torch.Tensor, cols: int) -> Mx4Mat:
+    """Weights for linear_mx4 from codes and scales as quantize_mx4 returns them (qrnnt_pack_mx4)."""
+    _here(codes, scale)
+    rows = codes.shape[0]
+    blocks = (_int32(cols, "cols") + 31) // 32
+    pq, ld_q = _matrix(codes, torch.uint8, rows, codes.shape[-1])
+    ps, ld_s = _matrix(scale, torch.uint8, rows, scale.shape[-1])
+    if codes.shape[1] < 16 * blocks or scale.shape[1] < blocks:
+        raise ValueError(f"rows of {cols} columns take {16 * blocks} bytes of codes and {blocks} scales, got {codes.shape[1]} and {scale.shape[1]}")
+    need = load().qrnnt_pack_mx4_bytes(rows, cols)
+    if need == 0:
+        _check(7 if rows > 0 and cols > 0 else 2, "qrnnt_pack_mx4_bytes")
+    packed = torch.empty(need, dtype=torch.uint8, device=codes.device)
+    _call("qrnnt_pack_mx4", pq, 16 * blocks if rows == 1 else ld_q, ps, ld_s, rows, cols, packed.data_ptr(), _stream_handle())
+    return Mx4Mat(packed, rows, cols)
+
+
+def linear_mx4_workspace(w: Mx4Mat, M: int) -> int:
+    cw = w.c()
+    return int(load().qrnnt_linear_mx4_workspace(C.byref(cw), _int32(M, "M")))
+
+
+def linear_mx4(w: Mx4Mat, codes: torch.Tensor, scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+               dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Linear layer of microscaled 4-bit floats: w from pack_mx4, codes and scales as quantize_mx4 returns them
+    (qrnnt_linear_mx4).  out may be a matrix whose rows lie apart."""
+    _here(codes, scale, bias, workspace, w.packed, out)
+    M = codes.shape[0]
+    pa, ld_a, ps, ld_s = _mx4(codes, scale, M, w.cols)
+    if out is None:
+        kind = _dtype(dtype)
+        out = torch.empty((M, w.rows), dtype=dtype, device=codes.device)
+        py, ld_y = out.data_ptr(), w.rows
+    else:
+        kind = _dtype(out.dtype)
+        py, ld_y = _matrix(out, out.dtype, M, w.rows)
+    cw = w.c()
+    if workspace is None:
+        need = load().qrnnt_linear_mx4_workspace(C.byref(cw), M)
+        workspace = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
+    n_ws = 0 if workspace is None else workspace.nbytes
+    _call("qrnnt_linear_mx4", C.byref(cw), _vector(bias, torch.float32, w.rows), pa, ld_a, ps, ld_s, M, py, kind, ld_y,
+          _addr(workspace) if n_ws else None, n_ws, _stream_handle())
     return out
 
 
@@ -663,6 +788,37 @@ def beam_select(score: torch.Tensor, logits: torch.Tensor, n_out: Optional[int] 
           pf, -1 if end_token is None else _int32(end_token, "end_token"), B, W, V, K, par.data_ptr(), tok.data_ptr(), ns.data_ptr(),
           None if done is None else done.data_ptr(), _addr(workspace), workspace.nbytes, _stream_handle())
     return par, tok, ns, done
+
+
+def token_scores_workspace(rows: int, V: int, n_top: int) -> int:
+    return int(load().qrnnt_token_scores_workspace(_int32(rows, "rows"), _int32(V, "V"), _int32(n_top, "n_top")))
+
+
+def token_scores(logits: torch.Tensor, token: Optional[torch.Tensor] = None, n_top: int = 0, entropy: bool = True,
+                 workspace: Optional[torch.Tensor] = None):
+    """Log probability of token[r] (int32; negative: padding, 0) in row r of logits [rows, V] (float32, float16 or bfloat16; rows may
+    lie apart), the row's entropy, its n_top best tokens and their log probabilities: (logp [rows] or None without token,
+    entropy [rows] or None, tokens [rows, n_top], logp of those), the last two None without n_top (qrnnt_token_scores)."""
+    _here(logits, token, workspace)
+    rows, V = logits.shape
+    pl, ld = _matrix(logits, logits.dtype, rows, V)
+    kind = _dtype(logits.dtype)
+    pt = _vector(token, torch.int32, rows)
+    if workspace is None:
+        need = token_scores_workspace(rows, V, n_top)
+        if need == 0:
+            _check(7 if rows >= 0 and V > 0 and n_top >= 0 else 2, "qrnnt_token_scores_workspace")
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    elif n_top < 0 or n_top > 64:
+        _check(2 if n_top < 0 else 7, "qrnnt_token_scores")
+    make = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
+    logp = None if token is None else make(rows)
+    ent = make(rows) if entropy else None
+    tokens, values = (make(rows, n_top, dtype=torch.int32), make(rows, n_top)) if n_top else (None, None)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    _call("qrnnt_token_scores", pl, kind, ld, pt, rows, V, n_top, ptr(logp), ptr(ent), ptr(tokens), ptr(values), _addr(workspace),
+          workspace.nbytes, _stream_handle())
+    return logp, ent, tokens, values
 
 
 class CStateRows(C.Structure):
