@@ -1,15 +1,17 @@
 // Scores of given tokens, from logits: log probability of a row's token, entropy of the row, its best alternatives, in one pass
 // over the logits.
 //
-// With S = sum exp(x - m), U = sum exp(x - m)(x - m) for any m:  lse = m + log S,  logp = (x[token] - m) - log S,
-// entropy = log S - U / S.  Each lane keeps an m, S and U of what it has read (S and U in fp64) and joins them with the others' once, at
-// the end of the row.  m is a logit that is at most LATE below the largest so far: sums move to another m seldom, and what they lose
-// in moving (an exponential's rounding) weighs at most exp(-LATE) of them.
+// With S = sum 2^(x L - r), U = sum 2^(x L - r)(x L - r), L = log2(e), for any r:  log P(x) = ln 2 (x L - r) - log S,
+// entropy = log S - ln 2 U / S.  A wave takes the largest logit of the first that it reads for r, a product, a sum, an exponential and
+// two more sums a logit then do; where a logit passes r by far (2^40) sums move to a larger one.  Lanes add up at the end of the row.
+// Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read again, with x - max
+// formed first.
 //
-// The best alternatives: a wave knows a bound that n logits of the row reach; what reaches it goes to a list in LDS, out of which the
-// n best are kept, and their smallest raises the bound, as often as the list fills.  The first bound is that of the groups of
-// the wave's first logits.
+// The best alternatives: the n-th largest of groups of the logits that are read first bounds the n-th best from below.  What reaches the
+// bound goes to a list in LDS, of which the n best are kept where it fills, and their smallest becomes the bound; at the end a
+// candidate's rank is how many are better.
 #include <float.h>
+#include <type_traits>
 
 #include "elem.h"
 #include "kernels.h"
@@ -17,12 +19,24 @@
 
 namespace {
 
-constexpr int MAX_TOP = 64, CAP = 256;   // ranks; candidates in a wave's list
+constexpr int MAX_TOP = 64, CAP = 256, LIST = 1024;   // ranks; candidates in a wave's and in a workgroup's list
 constexpr int MAX_PARTS = 16;
+constexpr float LOG2E = 1.4426950408889634f, FAR = -300.0f;   // 2^FAR is 0 in fp32
+constexpr float MOST = 0x1p100f;                              // r stays within
+constexpr double LN2 = 0.69314718055994530942;
 
-struct QrScoresHead {
-    float top, pad;
-    double s, u;
+// A part's sums.
+struct QrScoresSum {
+    double r, s, u;
+    // to an r that is not below
+    __device__ __forceinline__ void move(double to)
+    {
+        const double d = fmax(r - to, (double)FAR), c = (double)__builtin_amdgcn_exp2f((float)d);
+        u = c * (u + d * s);
+        s *= c;
+        r = to;
+    }
+    __device__ __forceinline__ bool good() const { return s > 0.0 && s < INFINITY; }
 };
 
 struct QrScoresArgs {
@@ -34,303 +48,513 @@ struct QrScoresArgs {
     float *logp, *entropy;
     int32_t *top_token;
     float *top_logp;
-    QrScoresHead *heads;     // [rows][n_parts]
+    QrScoresSum *heads;      // [rows][n_parts]
     QrCand *cands;           // [rows][n_parts][n], 0: none
 };
 
-constexpr float LOG2E = 1.4426950408889634f, FAR = -200.0f, LATE = 4.0f;   // exp(FAR) is 0 in fp32
-
-// Sums relative to `top`, which starts at the lowest finite value: a row of nothing but -inf has S = 0.  NaN and +inf make S NaN.
-struct QrScoresSum {
-    float top = -FLT_MAX;
-    double s = 0.0, u = 0.0;
-    __device__ __forceinline__ QrScoresHead head() const { return {top, 0.0f, s, u}; }
-    __device__ __forceinline__ void set(const QrScoresHead &h)
+// A row's token and its logit, fetched before the row is read.
+struct QrScoresToken {
+    int t = -1;
+    float x = 0.0f;
+    template <class T>
+    __device__ __forceinline__ void load(const QrScoresArgs &a, int64_t row)
     {
-        top = h.top;
-        s = h.s;
-        u = h.u;
-    }
-    // moves the sums to a top that is not below theirs
-    __device__ __forceinline__ void move(float to)
-    {
-        const float d = fmaxf(top - to, FAR);
-        const double c = (double)__builtin_amdgcn_exp2f(LOG2E * d);
-        u = c * (u + (double)d * s);
-        s *= c;
-        top = to;
-    }
-    __device__ __forceinline__ void join_wave()
-    {
-        move(qr_key_float(qr_wave_reduce_u32<true>(qr_float_key(top))));
-        s = qr_wave_sum(s);
-        u = qr_wave_sum(u);
+        if (!a.logp) return;
+        t = a.token[row];
+        x = (float)((const T *)a.logits)[row * a.ld + (t >= 0 && t < a.V ? t : 0)];
     }
 };
 
-// Value of a row's logits from its sums.
+// Values of a row's logits from its sums.
 struct QrScoresRow {
-    double top, log_s, entropy;
+    double r, log_s, entropy;
     bool none, bad;   // no token can be; a logit is NaN or +inf
     __device__ __forceinline__ explicit QrScoresRow(const QrScoresSum &a)
     {
-        top = (double)a.top;
+        r = a.r;
         none = a.s == 0.0;
         bad = !(a.s == a.s);
         log_s = log(a.s);
-        entropy = none ? 0.0 : log_s - a.u / a.s;
+        entropy = none ? 0.0 : log_s - LN2 * (a.u / a.s);
     }
-    __device__ __forceinline__ float logp(float logit) const { return none ? -INFINITY : (float)(((double)logit - top) - log_s); }
+    __device__ __forceinline__ float logp(float logit) const { return none ? -INFINITY : (float)(LN2 * ((double)logit * (double)LOG2E - r) - log_s); }
+    __device__ __forceinline__ void write(const QrScoresArgs &a, int64_t row, const QrScoresToken &t) const
+    {
+        if (a.logp) a.logp[row] = t.t < 0 ? 0.0f : t.t >= a.V ? NAN : logp(t.x);
+        if (a.entropy) a.entropy[row] = (float)entropy;
+    }
+    __device__ __forceinline__ void write_rank(const QrScoresArgs &a, int64_t row, int rank, QrCand c) const
+    {
+        const bool some = c != 0ull && !bad;
+        a.top_token[row * a.n + rank] = some ? qr_cand_index(c) : -1;
+        a.top_logp[row * a.n + rank] = some ? logp(qr_cand_value(c)) : -INFINITY;
+    }
 };
-
-template <class T>
-__device__ __forceinline__ void write_row(const QrScoresArgs &a, int64_t row, const QrScoresRow &r)
-{
-    if (a.logp) {
-        const int t = a.token[row];
-        a.logp[row] = t < 0 ? 0.0f : t >= a.V ? NAN : r.logp((float)((const T *)a.logits)[row * a.ld + t]);
-    }
-    if (a.entropy) a.entropy[row] = (float)r.entropy;
-}
-__device__ __forceinline__ void write_rank(const QrScoresArgs &a, int64_t row, int rank, QrCand c, const QrScoresRow &r)
-{
-    const bool some = c != 0ull && !r.bad;
-    a.top_token[row * a.n + rank] = some ? qr_cand_index(c) : -1;
-    a.top_logp[row * a.n + rank] = some ? r.logp(qr_cand_value(c)) : -INFINITY;
-}
 
 // Four vectors of a lane out of 256 that follow one another; -inf behind the end.
 template <class T>
 struct QrChunk {
     static constexpr int V = QrVec<T>::N, LEN = 256 * V, PER = 4 * V;
-    typename QrVec<T>::type raw[4];
+    v4i raw[4];
     __device__ __forceinline__ void load(const T *x, int n, int lane)
     {
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int c = (v * 64 + lane) * V;
             if (c + V <= n) {
-                raw[v] = *(const typename QrVec<T>::any *)(x + c);
+                raw[v] = __builtin_bit_cast(v4i, *(const typename QrVec<T>::any *)(x + c));
             } else {
+                typename QrVec<T>::type u;
 #pragma unroll
-                for (int i = 0; i < V; ++i) raw[v][i] = c + i < n ? x[c + i] : (T)-INFINITY;
+                for (int i = 0; i < V; ++i) u[i] = c + i < n ? x[c + i] : (T)-INFINITY;
+                raw[v] = __builtin_bit_cast(v4i, u);
             }
         }
     }
-    __device__ __forceinline__ float at(int i) const { return (float)raw[i / V][i % V]; }
-};
-
-// A wave's list of candidates, in LDS; n and the bound are uniform.
-struct QrTopList {
-    QrCand *list;
-    int count = 0;
-    unsigned key = 0u;   // what is asked of a further candidate: a key not below this
-    __device__ __forceinline__ float least() const { return key > 0x00800000u ? qr_key_float(key) : -FLT_MAX; }   // (keys up to there are those of -inf and below)
-
-    // Keeps the n best, or up to `enough` while that needs no look at indices; returns the key that n of them reach (0: there are fewer).
-    // (The bound is the n-th largest key itself unless no more than `enough` reach it: what is left is never more than that.)
-    __device__ __forceinline__ unsigned keep_best(int n, int enough, int lane)
+    __device__ __forceinline__ float at(int i) const
     {
-        QrCand e[CAP / 64];
-        unsigned g[CAP / 64], top = 0u;
+        const unsigned w = (unsigned)raw[i / V][i % V * (int)sizeof(T) / 4];
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+        if constexpr (std::is_same<T, __bf16>::value) return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w >> 16 : w));
+    }
+    // What follows widens the logits again: kept in fp32 from one use to the next they would take other waves' registers.
+    __device__ __forceinline__ void fresh()
+    {
 #pragma unroll
-        for (int j = 0; j < CAP / 64; ++j) {
-            e[j] = lane + 64 * j < count ? list[lane + 64 * j] : 0ull;
-            g[j] = (unsigned)(e[j] >> 32);
-            top = g[j] > top ? g[j] : top;
-        }
-        const unsigned T = qr_bound_of(g, qr_wave_reduce_u32<true>(top), n, enough);
-        if (T == 0u) return 0u;
-        int above = 0, equal = 0;
-#pragma unroll
-        for (int j = 0; j < CAP / 64; ++j) {
-            above += (int)__popcll(__ballot(g[j] > T));
-            equal += (int)__popcll(__ballot(g[j] == T));
-        }
-        unsigned low = 0u;   // of the equal ones: the words (complements of the indices) from here on
-        if (above + equal > enough) {
-            for (int bit = 31; bit >= 0; --bit) {
-                const unsigned trial = low | (1u << bit);
-                int some = 0;
-#pragma unroll
-                for (int j = 0; j < CAP / 64; ++j) some += (int)__popcll(__ballot(g[j] == T && (unsigned)e[j] >= trial));
-                if (above + some >= n) low = trial;
-            }
-        }
-        int at = 0;
-#pragma unroll
-        for (int j = 0; j < CAP / 64; ++j) {
-            const bool stays = g[j] > T || (g[j] == T && (unsigned)e[j] >= low);
-            const unsigned long long m = __ballot(stays);
-            if (stays) list[at + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u))] = e[j];
-            at += (int)__popcll(m);
-        }
-        count = at;
-        __builtin_amdgcn_wave_barrier();
-        return T;
+        for (int v = 0; v < 4; ++v) asm volatile("" : "+v"(raw[v]));
     }
 };
 
-// Grid: x = part of a row, y (and z) = row, or four rows where a wave has one of its own (WPR 1).  WPR waves to a row.
-template <class T, int WPR, bool TOP>
-__global__ __launch_bounds__(WPR < 4 ? 256 : 64 * WPR) void scores_kernel(const QrScoresArgs a)
+typedef __attribute__((address_space(3))) QrCand *QrLdsList;   // (for functions that are not inlined)
+
+__device__ __forceinline__ int lanes_below(unsigned long long m) { return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u)); }
+__device__ __forceinline__ float least_of(unsigned key) { return key > 0x00800000u ? qr_key_float(key) : -FLT_MAX; }   // (keys up to there are those of -inf and below)
+__device__ __forceinline__ float wave_max(float v) { return qr_key_float(qr_wave_reduce_u32<true>(qr_float_key(v))); }   // (v is not NaN)
+__device__ __forceinline__ float limited(float r) { return fminf(fmaxf(r, -MOST), MOST); }
+
+// A wave keeps the n best of a list in LDS, or up to `enough` while that needs no look at indices; returns the key that n of them reach
+// (0: there are fewer).  (The bound is the n-th largest key itself unless no more than `enough` reach it: what is left is never more than that.)
+template <int ROOM, class List>
+__device__ __forceinline__ unsigned keep_best(List list, int &count, int n, int enough, int lane)
 {
-    constexpr int WAVES = WPR < 4 ? 4 : WPR, V = QrVec<T>::N, PER = QrChunk<T>::PER, LEN = QrChunk<T>::LEN;
-    __shared__ QrCand lists[TOP ? WAVES : 1][TOP ? CAP : 1];
-    __shared__ unsigned shared_key;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
-    if (WPR == 1) row = row * 4 + wave;
-    const bool real = row < a.rows;   // uniform in a wave; of a workgroup with one row uniform at all
-    if (!real) return;
-    const int first = blockIdx.x * a.part, n = a.V - first < a.part ? a.V - first : a.part;
-    const T *x = (const T *)a.logits + row * a.ld + first;
-    QrTopList top;
-    top.list = lists[TOP ? wave : 0];
-    if (TOP && WPR > 1) {
-        if (tid == 0) shared_key = 0u;
-        __syncthreads();
+    QrCand e[ROOM / 64];
+    unsigned g[ROOM / 64], top = 0u;
+#pragma unroll
+    for (int j = 0; j < ROOM / 64; ++j) {
+        e[j] = lane + 64 * j < count ? list[lane + 64 * j] : 0ull;
+        g[j] = (unsigned)(e[j] >> 32);
+        top = g[j] > top ? g[j] : top;
     }
-    QrScoresSum sum;
-    QrChunk<T> now, next;
-    const int at0 = (WPR == 1 ? 0 : wave) * LEN;
-    if (at0 < n) now.load(x + at0, n - at0, lane);
-    for (int at = at0; at < n; at += WPR * LEN) {
-        const bool more = n - at > WPR * LEN;
-        if (more) next.load(x + at + WPR * LEN, n - at - WPR * LEN, lane);
-        float best[4];
+    const unsigned T = qr_bound_of(g, qr_wave_reduce_u32<true>(top), n, enough);
+    if (T == 0u) return 0u;
+    int above = 0, equal = 0;
+#pragma unroll
+    for (int j = 0; j < ROOM / 64; ++j) {
+        above += (int)__popcll(__ballot(g[j] > T));
+        equal += (int)__popcll(__ballot(g[j] == T));
+    }
+    unsigned low = 0u;   // of the equal ones: the words (complements of the indices) from here on
+    if (above + equal > enough) {
+        for (int bit = 31; bit >= 0; --bit) {
+            const unsigned trial = low | (1u << bit);
+            int some = 0;
+#pragma unroll
+            for (int j = 0; j < ROOM / 64; ++j) some += (int)__popcll(__ballot(g[j] == T && (unsigned)e[j] >= trial));
+            if (above + some >= n) low = trial;
+        }
+    }
+    int at = 0;
+#pragma unroll
+    for (int j = 0; j < ROOM / 64; ++j) {
+        const bool stays = g[j] > T || (g[j] == T && (unsigned)e[j] >= low);
+        const unsigned long long m = __ballot(stays);
+        if (stays) list[at + lanes_below(m)] = e[j];
+        at += (int)__popcll(m);
+    }
+    count = at;
+    __builtin_amdgcn_wave_barrier();
+    return T;
+}
+
+// A wave's sums and best logits, as it goes through a row.  All but the lanes' sums is uniform.
+template <class T>
+struct QrScoresWave {
+    static constexpr int V = QrVec<T>::N, PER = QrChunk<T>::PER;
+    QrChunk<T> now;
+    float best[4], largest;   // of each vector, of all four (not NaN)
+    float r = -MOST;
+    double s = 0.0, u = 0.0;
+
+    __device__ __forceinline__ void find_best()
+    {
+        now.fresh();
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             best[v] = now.at(v * V);
 #pragma unroll
             for (int i = 1; i < V; ++i) best[v] = fmaxf(best[v], now.at(v * V + i));
         }
-        const float largest = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
-        const bool late = largest > sum.top + LATE;
-        if (__ballot(late)) sum.move(late ? largest : sum.top);
-        float s = 0.0f, u = 0.0f;
+        largest = fmaxf(-INFINITY, fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])));
+    }
+    __device__ __forceinline__ void start() { r = limited(LOG2E * wave_max(largest)); }
+    __device__ __forceinline__ void add_chunk(float &cs, float &cu)
+    {
+        cs = cu = 0.0f;
+        now.fresh();
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const float d = now.at(i) - sum.top, e = __builtin_amdgcn_exp2f(LOG2E * d);
-            s += e;
-            u = fmaf(e, fmaxf(d, FAR), u);
+            const float d = fmaf(now.at(i), LOG2E, -r), e = __builtin_amdgcn_exp2f(d);
+            cs += e;
+            cu = fmaf(e, fmaxf(d, FAR), cu);
         }
-        sum.s += (double)s;
-        sum.u += (double)u;
-        if (TOP) {
-            if (at == at0) {
-                unsigned g[4], most = 0u;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    g[v] = qr_logit_key(best[v]);
-                    most = g[v] > most ? g[v] : most;
-                }
-                top.key = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, a.n + a.n / 4);
-                if (WPR > 1 && lane == 0) atomicMax(&shared_key, top.key);
-            }
-            if (WPR > 1) {
-                const unsigned k = __builtin_amdgcn_readfirstlane(*(volatile unsigned *)&shared_key);
-                top.key = k > top.key ? k : top.key;
-            }
-            float least = top.least();
-            if (__ballot(largest >= least)) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    if (!__ballot(best[v] >= least)) continue;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float f = now.at(v * V + i);
-                        unsigned long long m = __ballot(f >= least);
-                        if (!m) continue;
-                        if (top.count + (int)__popcll(m) > CAP) {
-                            // (n of the list reach the key, but what is left of these logits may lie in front of them)
-                            const unsigned k = top.keep_best(a.n, a.n + a.n / 4, lane);
-                            top.key = k > top.key ? k : top.key;
-                            least = top.least();
-                            m = __ballot(f >= least);
-                        }
-                        const int to = top.count + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u));
-                        if (f >= least) top.list[to] = qr_cand(qr_float_key(f + 0.0f), first + at + (v * 64 + lane) * V + i);
-                        top.count += (int)__popcll(m);
-                    }
-                }
-                __builtin_amdgcn_wave_barrier();
-                if (top.count >= 2 * a.n + 16) {
-                    const unsigned k = top.keep_best(a.n, a.n + a.n / 4, lane);
-                    if (WPR > 1 && lane == 0) atomicMax(&shared_key, k);
-                    // what this wave has not read yet lies behind: to be among the best it has to be larger
-                    top.key = k + 1u > top.key ? k + 1u : top.key;
-                }
-            }
-        }
-        if (more) now = next;
     }
-    sum.join_wave();
-    if (TOP && top.count > a.n) top.keep_best(a.n, a.n, lane);
-    QrCand mine = TOP && lane < top.count ? top.list[lane] : 0ull;
-    if (WPR == 1) {
-        const QrScoresRow r(sum);
-        if (lane == 0) write_row<T>(a, row, r);
-        if (TOP) {
-            int rank = 0;
-            for (int j = 0; j < top.count; ++j) rank += top.list[j] > mine ? 1 : 0;
-            if (lane < a.n) write_rank(a, row, lane < top.count ? rank : lane, mine, r);
+    template <bool FOUND>
+    __device__ __forceinline__ void add()
+    {
+        float cs, cu;
+        add_chunk(cs, cu);
+        if (__ballot(!(cs < 0x1p40f))) {
+            if (!FOUND) find_best();
+            const float to = limited(LOG2E * wave_max(largest));
+            if (to > r) {
+                QrScoresSum moved = {(double)r, s, u};
+                moved.move((double)to);
+                r = to;
+                s = moved.s;
+                u = moved.u;
+                add_chunk(cs, cu);
+            }
         }
-        return;
+        s += (double)cs;
+        u += (double)cu;
     }
-    // the waves' sums and lists
-    __shared__ QrScoresHead sums[WAVES];
-    __shared__ unsigned group_best[256];
-    __shared__ QrCand all[TOP ? 64 * WAVES : 1];
-    __shared__ int n_all;
-    if (lane == 0) sums[wave] = sum.head();
+    __device__ __forceinline__ QrScoresSum sum() const { return {(double)r, qr_wave_sum(s), qr_wave_sum(u)}; }
+    // Which of a lane's logits are not below `least`, as bits.
+    __device__ __forceinline__ unsigned from(float least)
+    {
+        unsigned mask = 0u;
+        now.fresh();
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (!__ballot(best[v] >= least)) continue;
+#pragma unroll
+            for (int i = 0; i < V; ++i) mask |= now.at(v * V + i) >= least ? 1u << (v * V + i) : 0u;
+        }
+        return mask;
+    }
+    // The logit of the lowest bit of `mask` and its place in the chunk at x; all: the bits before any was taken.  The only one of a
+    // vector is the vector's largest; where there are more (seldom) they are read again, which takes less code than a way for each register.
+    __device__ __forceinline__ float pop(unsigned &mask, unsigned all, const T *x, int lane, int &place) const
+    {
+        const int b = __builtin_ctz(mask), v = b / V;
+        mask &= mask - 1u;
+        place = (v * 64 + lane) * V + b % V;
+        const float b0 = best[0], b1 = best[1], b2 = best[2], b3 = best[3];   // (values: a choice of places would put them into memory)
+        float f = v == 0 ? b0 : v == 1 ? b1 : v == 2 ? b2 : b3;
+        if (__popc(all & (((1u << V) - 1u) << (v * V))) > 1) f = (float)x[place];
+        return f;
+    }
+    // take(logit, place in the chunk at x) for the logits from `least` on.
+    template <class Take>
+    __device__ __forceinline__ void hits(float least, const T *x, int lane, Take &&take)
+    {
+        if (!__ballot(largest >= least)) return;
+        const unsigned all = from(least);
+        for (unsigned mask = all; mask != 0u;) {
+            int i;
+            const float f = pop(mask, all, x, lane, i);
+            take(f, i);
+        }
+    }
+    // The same into a wave's list, which never overflows: where it is full its n best are kept.  first: index of the chunk's first logit.
+    template <class List>
+    __device__ __forceinline__ void hits_to(List list, int &count, unsigned &key, int n, const T *x, int first, int lane)
+    {
+        float least = least_of(key);
+        if (!__ballot(largest >= least)) return;
+        const unsigned all = from(least);
+        for (unsigned mask = all; __ballot(mask != 0u);) {   // uniform
+            int i = 0;
+            float f = -INFINITY;
+            if (mask != 0u) f = pop(mask, all, x, lane, i);
+            unsigned long long m = __ballot(f >= least);
+            if (count + (int)__popcll(m) > CAP) {
+                // (n of the list reach the key, but what is left of these logits may lie in front of them)
+                const unsigned k = keep_best<CAP>(list, count, n, n + n / 4, lane);
+                key = k > key ? k : key;
+                least = least_of(key);
+                m = __ballot(f >= least);
+            }
+            if (f >= least) list[count + lanes_below(m)] = qr_cand(qr_float_key(f + 0.0f), first + i);
+            count += (int)__popcll(m);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (count >= 2 * n + 32) {
+            // what this wave has not read yet lies behind: to be among the best it has to be larger
+            const unsigned k = keep_best<CAP>(list, count, n, n + n / 4, lane) + 1u;
+            key = k > key ? k : key;
+        }
+    }
+};
+
+// The bound that groups of a wave's logits give.  Few ranks: a lane's are a group.
+template <class T>
+__device__ __forceinline__ unsigned first_bound(const QrScoresWave<T> &w, int n)
+{
+    if (n <= 16) {
+        const unsigned g[1] = {qr_logit_key(w.largest)};
+        return qr_bound_of(g, qr_wave_reduce_u32<true>(g[0]), n, n + n / 4);
+    }
+    unsigned g[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) g[v] = qr_logit_key(w.best[v]);
+    return qr_bound_of(g, qr_wave_reduce_u32<true>(qr_logit_key(w.largest)), n, n + n / 4);
+}
+
+// Sums of a row's part that are good for any logits: relative to its largest one.  WPR waves of a workgroup, `most` in LDS.
+template <class T, int WPR>
+__device__ __attribute__((noinline)) QrScoresSum sums_of_any(const T *x, int n, int wave, int lane, float *most)
+{
+    float m = -INFINITY;
+    bool nan = false;
+    for (int c = wave * 64 + lane; c < n; c += WPR * 64) {
+        const float f = (float)x[c];
+        m = fmaxf(m, f);
+        nan = nan || !(f < INFINITY);
+    }
+    m = wave_max(m);
+    nan = __ballot(nan) != 0ull;
+    if (WPR > 1) {
+        if (lane == 0) most[wave] = nan ? INFINITY : m;
+        __syncthreads();
+        for (int w = 0; w < WPR; ++w) m = fmaxf(m, most[w]);
+        nan = !(m < INFINITY);
+    }
+    if (nan) return {0.0, NAN, NAN};
+    if (m == -INFINITY) return {0.0, 0.0, 0.0};
+    QrScoresSum sum = {(double)m * (double)LOG2E, 0.0, 0.0};
+    for (int c = wave * 64 + lane; c < n; c += WPR * 64) {
+        const float d = LOG2E * ((float)x[c] - m), e = __builtin_amdgcn_exp2f(d);
+        sum.s += (double)e;
+        sum.u += (double)(e * fmaxf(d, FAR));
+    }
+    return {sum.r, qr_wave_sum(sum.s), qr_wave_sum(sum.u)};
+}
+
+// A wave to a row: many rows, or short ones.  Grid: y (and z) = four rows.
+template <class T, bool TOP>
+__global__ __launch_bounds__(256, TOP ? 6 : 8) void scores_wave_kernel(const QrScoresArgs a)
+{
+    constexpr int LEN = QrChunk<T>::LEN;
+    __shared__ QrCand lists[TOP ? 4 : 1][TOP ? CAP : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t row = (blockIdx.y + (int64_t)blockIdx.z * 32768) * 4 + wave;
+    if (row >= a.rows) return;
+    const int n = a.V;
+    const T *x = (const T *)a.logits + row * a.ld;
+    QrScoresWave<T> w;
+    w.now.load(x, n, lane);
+    QrScoresToken token;
+    token.load<T>(a, row);
+    QrCand *list = lists[TOP ? wave : 0];
+    int count = 0;
+    unsigned key = 0u;
+    for (int at = 0;; at += LEN) {
+        const bool more = n - at > LEN;
+        QrChunk<T> next;
+        if (more) next.load(x + at + LEN, n - at - LEN, lane);
+        if (TOP || at == 0) w.find_best();
+        if (at == 0) w.start();
+        w.template add<TOP>();
+        if (TOP) {
+            if (at == 0) key = first_bound(w, a.n);
+            w.hits_to(list, count, key, a.n, x + at, at, lane);
+        }
+        if (!more) break;
+        w.now = next;
+    }
+    QrScoresSum sum = w.sum();
+    if (!sum.good()) sum = sums_of_any<T, 1>(x, n, 0, lane, nullptr);
+    const QrScoresRow values(sum);
+    if (lane == 0) values.write(a, row, token);
     if (TOP) {
-        if (tid == 0) n_all = 0;
-        const unsigned k = (unsigned)(mine >> 32);
-        if (WAVES == 4) {
+        if (count > 128) keep_best<CAP>(list, count, a.n, a.n, lane);
+        const QrCand c0 = lane < count ? list[lane] : 0ull, c1 = lane + 64 < count ? list[lane + 64] : 0ull;
+        int r0 = 0, r1 = 0;
+#pragma unroll 4
+        for (int j = 0; j < count; ++j) {
+            const QrCand o = list[j];
+            r0 += o > c0 ? 1 : 0;
+            r1 += o > c1 ? 1 : 0;
+        }
+        if (c0 != 0ull && r0 < a.n) values.write_rank(a, row, r0, c0);
+        if (c1 != 0ull && r1 < a.n) values.write_rank(a, row, r1, c1);
+        if (lane >= count && lane < a.n) values.write_rank(a, row, lane, 0ull);
+    }
+}
+
+// What a list of the workgroup does not hold, because very many logits are equal or they rise: every wave finds the n best of what it
+// reads by itself; one to a lane.
+template <class T, int NW>
+__device__ __attribute__((noinline)) QrCand best_of_any(const T *x, int len, int first, int n, int wave, int lane, QrLdsList list)
+{
+    QrScoresWave<T> w;
+    int count = 0;
+    unsigned key = 0u;
+    for (int at = wave * QrChunk<T>::LEN; at < len; at += NW * QrChunk<T>::LEN) {
+        w.now.load(x + at, len - at, lane);
+        w.find_best();
+        w.hits_to(list, count, key, n, x + at, first + at, lane);
+    }
+    if (count > n) keep_best<CAP>(list, count, n, n, lane);
+    return lane < count ? list[lane] : 0ull;
+}
+
+// A workgroup of NW waves to a row or a part of one.  Grid: x = part of a row, y (and z) = row.
+template <class T, int NW, bool TOP>
+__global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScoresArgs a)
+{
+    constexpr int LEN = QrChunk<T>::LEN, BLOCK = NW * LEN;
+    __shared__ QrCand lists[TOP ? NW : 1][TOP ? CAP : 1];   // (of waves by themselves, where the list overflows)
+    __shared__ QrCand list[TOP ? LIST : 1], ranked[TOP ? MAX_TOP : 1];
+    __shared__ unsigned group_best[256], shared_key;
+    __shared__ QrScoresSum sums[NW];
+    __shared__ float most_of[NW];
+    __shared__ int n_list;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
+    if (row >= a.rows) return;   // uniform
+    const int first = blockIdx.x * a.part, n = a.V - first < a.part ? a.V - first : a.part;
+    const T *x = (const T *)a.logits + row * a.ld + first;
+    QrScoresWave<T> w;
+    w.now.load(x + wave * LEN, n - wave * LEN, lane);   // (nothing behind the end is read)
+    QrScoresToken token;
+    if (a.n_parts == 1 && wave == 0) token.load<T>(a, row);
+    if (TOP) {
+        if (tid == 0) n_list = 0;
+        if (tid < MAX_TOP) ranked[tid] = 0ull;
+    }
+    // every thread has a key: a bound from below of the n-th best, by the best keys of groups of threads.  The work is wave 0's, the
+    // barrier behind it the caller's.
+    auto find_bound = [&](unsigned k) {
+        if (NW == 4) {
             group_best[tid] = k;
         } else {
             const unsigned four = qr_quad_max(k);
             if ((lane & 3) == 0) group_best[tid >> 2] = four;
         }
-    }
-    __syncthreads();
-    sum = QrScoresSum();
-    if (lane < WAVES) sum.set(sums[lane]);
-    sum.join_wave();
-    const int64_t part = row * a.n_parts + blockIdx.x;
-    if (TOP) {
-        unsigned g[4], most = 0u;
+        __syncthreads();
+        if (wave == 0) {
+            unsigned g[4], one[1] = {0u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            g[i] = group_best[i * 64 + lane];
-            most = g[i] > most ? g[i] : most;
+            for (int i = 0; i < 4; ++i) {
+                g[i] = group_best[i * 64 + lane];
+                one[0] = g[i] > one[0] ? g[i] : one[0];
+            }
+            const unsigned top = qr_wave_reduce_u32<true>(one[0]);
+            const unsigned bound = a.n <= 16 ? qr_bound_of(one, top, a.n, a.n + a.n / 4) : qr_bound_of(g, top, a.n, a.n + a.n / 4);
+            if (lane == 0) shared_key = bound;
         }
-        const unsigned bound = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, a.n + a.n / 4);
-        if (mine != 0ull && (unsigned)(mine >> 32) >= bound) all[atomicAdd(&n_all, 1)] = mine;
+    };
+    auto push = [&](QrCand c) {
+        const int to = atomicAdd(&n_list, 1);
+        if (to < LIST) list[to] = c;
+    };
+    bool over = false;   // the list
+    for (int at = 0;; at += BLOCK) {
+        const bool more = n - at > BLOCK;
+        const int mine = at + wave * LEN;
+        QrChunk<T> next;
+        if (more) next.load(x + mine + BLOCK, n - mine - BLOCK, lane);
+        if (TOP || at == 0) w.find_best();
+        if (at == 0) w.start();
+        if (TOP && at == 0) find_bound(qr_logit_key(w.largest));   // (the other waves add up in the meantime)
+        w.template add<TOP>();
+        if (TOP && !over) {
+            __syncthreads();
+            w.hits(least_of(shared_key), x + mine, lane, [&](float f, int i) { push(qr_cand(qr_float_key(f + 0.0f), first + mine + i)); });
+            if (more) {
+                __syncthreads();
+                const int count = n_list;
+                over = count > LIST;
+                if (count > LIST / 2 && !over) {   // uniform: what the list holds raises the bound and goes where it is below
+                    constexpr int EACH = LIST / (64 * NW);
+                    QrCand c[EACH];
+                    unsigned k = 0u;
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) {
+                        c[i] = tid + i * 64 * NW < count ? list[tid + i * 64 * NW] : 0ull;
+                        k = (unsigned)(c[i] >> 32) > k ? (unsigned)(c[i] >> 32) : k;
+                    }
+                    find_bound(k);
+                    if (tid == 0) n_list = 0;
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i)
+                        if (c[i] != 0ull && (unsigned)(c[i] >> 32) >= shared_key) push(c[i]);
+                }
+            }
+        }
+        if (!more) break;
+        w.now = next;
+    }
+    const QrScoresSum own = w.sum();
+    if (lane == 0) sums[wave] = own;
+    __syncthreads();
+    int M = 0;
+    if (TOP) {
+        M = n_list;
+        if (M > LIST) {   // uniform
+            list[tid] = best_of_any<T, NW>(x, n, first, a.n, wave, lane, (QrLdsList)lists[wave]);
+            M = 64 * NW;
+            __syncthreads();
+        }
+    }
+    const double s_of = lane < NW ? sums[lane].s : 0.0;
+    if (__ballot(!(s_of < INFINITY)) || !__ballot(s_of > 0.0)) {   // uniform
+        __syncthreads();
+        const QrScoresSum any = sums_of_any<T, NW>(x, n, wave, lane, most_of);
+        if (lane == 0) sums[wave] = any;
         __syncthreads();
     }
-    const QrScoresRow r(sum);
-    if (tid == 0) {
-        if (a.n_parts > 1) a.heads[part] = sum.head();
-        else write_row<T>(a, row, r);
-    }
-    if (TOP) {
-        const int M = n_all;
-        auto put = [&](int rank, QrCand c) {
-            if (a.n_parts > 1) a.cands[part * a.n + rank] = c;
-            else write_rank(a, row, rank, c, r);
-        };
-        for (int i0 = 0; i0 < M; i0 += 16 * WAVES) {   // uniform; four threads count for one candidate
-            const int i = i0 + (tid >> 2);
-            const QrCand c = all[i < M ? i : 0];
+    QrScoresSum sum = {0.0, 0.0, 0.0};
+    if (wave == 0) {   // joins the sums, the others rank
+        sum = lane < NW ? sums[lane] : QrScoresSum{-1e300, 0.0, 0.0};
+        double to = sum.r;
+#pragma unroll
+        for (int off = 1; off < NW; off <<= 1) to = fmax(to, __shfl_xor(to, off));
+        to = __shfl(to, 0);
+        sum.move(to);
+        sum.s = qr_wave_sum(sum.s);
+        sum.u = qr_wave_sum(sum.u);
+    } else if (TOP) {
+        for (int i0 = 0; i0 < M; i0 += 16 * (NW - 1)) {   // uniform; four threads count for one candidate
+            const int i = i0 + ((tid - 64) >> 2);
+            const QrCand c = list[i < M ? i : 0];
             int rank = 0;
-            for (int j = tid & 3; j < M; j += 4) rank += all[j] > c ? 1 : 0;
+#pragma unroll 8
+            for (int j = tid & 3; j < M; j += 4) rank += list[j] > c ? 1 : 0;
             rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
             rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
-            if ((tid & 3) == 0 && i < M && rank < a.n) put(rank, c);
+            if ((tid & 3) == 0 && i < M && c != 0ull && rank < a.n) ranked[rank] = c;
         }
-        if (tid >= M && tid < a.n) put(tid, 0ull);
+    }
+    const int64_t part = row * a.n_parts + blockIdx.x;
+    if (a.n_parts > 1) {
+        if (tid == 0) a.heads[part] = sum;
+        if (TOP) {
+            __syncthreads();
+            if (tid < a.n) a.cands[part * a.n + tid] = ranked[tid];
+        }
+        return;
+    }
+    if (!TOP && wave > 0) return;
+    const QrScoresRow values(sum);
+    if (tid == 0) values.write(a, row, token);
+    if (TOP) {
+        __syncthreads();
+        if (tid < a.n) values.write_rank(a, row, tid, ranked[tid]);
     }
 }
 
@@ -344,13 +568,20 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
     QrCand mine = tid < a.n_parts * a.n ? a.cands[row * a.n_parts * a.n + tid] : 0ull;
-    QrScoresSum sum;
-    if (lane < a.n_parts) sum.set(a.heads[row * a.n_parts + lane]);
-    sum.join_wave();
-    const QrScoresRow r(sum);
+    QrScoresToken token;
+    token.load<T>(a, row);
+    // (the r of a part that holds no finite logit, 0, may be above the others': it counts only where there is something to it)
+    QrScoresSum sum = lane < a.n_parts ? a.heads[row * a.n_parts + lane] : QrScoresSum{0.0, 0.0, 0.0};
+    const bool some = sum.s != 0.0;
+    double to = some ? sum.r : -1e300;
+    for (int off = 1; off < MAX_PARTS; off <<= 1) to = fmax(to, __shfl_xor(to, off));
+    to = __shfl(to, 0);
+    if (some) sum.move(to);
+    sum = {to, qr_wave_sum(sum.s), qr_wave_sum(sum.u)};
+    const QrScoresRow values(sum);
     if (tid == 0) {
         n_all = 0;
-        write_row<T>(a, row, r);
+        values.write(a, row, token);
     }
     if (a.n == 0) return;
     const unsigned four = qr_quad_max((unsigned)(mine >> 32));
@@ -370,12 +601,13 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
         const int i = i0 + (tid >> 2);
         const QrCand c = all[i < M ? i : 0];
         int rank = 0;
+#pragma unroll 8
         for (int j = tid & 3; j < M; j += 4) rank += all[j] > c ? 1 : 0;
         rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
         rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
-        if ((tid & 3) == 0 && i < M && rank < a.n) write_rank(a, row, rank, c, r);
+        if ((tid & 3) == 0 && i < M && rank < a.n) values.write_rank(a, row, rank, c);
     }
-    if (tid >= M && tid < a.n) write_rank(a, row, tid, 0ull, r);
+    if (tid >= M && tid < a.n) values.write_rank(a, row, tid, 0ull);
 }
 
 // Waves to a row, and parts of it.
@@ -404,9 +636,9 @@ void launch_scores(const QrScoresArgs &a, int waves, hipStream_t st)
 {
     const int64_t n = waves == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;
     const dim3 grid(a.n_parts, (unsigned)(n < 32768 ? n : 32768), (unsigned)((n + 32767) / 32768));
-    if (waves == 1) scores_kernel<T, 1, TOP><<<grid, 256, 0, st>>>(a);
-    else if (waves == 4) scores_kernel<T, 4, TOP><<<grid, 256, 0, st>>>(a);
-    else scores_kernel<T, 16, TOP><<<grid, 1024, 0, st>>>(a);
+    if (waves == 1) scores_wave_kernel<T, TOP><<<grid, 256, 0, st>>>(a);
+    else if (waves == 4) scores_group_kernel<T, 4, TOP><<<grid, 256, 0, st>>>(a);
+    else scores_group_kernel<T, 16, TOP><<<grid, 1024, 0, st>>>(a);
     if (a.n_parts > 1) scores_join_kernel<T><<<a.rows, 64 * MAX_PARTS, 0, st>>>(a);
 }
 
@@ -415,7 +647,7 @@ void launch_scores(const QrScoresArgs &a, int waves, hipStream_t st)
 extern "C" size_t qrnnt_token_scores_workspace(int32_t rows, int32_t V, int32_t n_top)
 {
     if (!scores_sizes_ok(rows, V, n_top)) return 0;
-    return (size_t)most_parts(rows, V) * (sizeof(QrScoresHead) + n_top * sizeof(QrCand)) + 256;
+    return (size_t)most_parts(rows, V) * (sizeof(QrScoresSum) + n_top * sizeof(QrCand)) + 256;
 }
 
 extern "C" qrnnt_status qrnnt_token_scores(const void *logits, int32_t dtype, int64_t ld, const int32_t *token, int32_t rows, int32_t V,
@@ -435,8 +667,8 @@ extern "C" qrnnt_status qrnnt_token_scores(const void *logits, int32_t dtype, in
     a.logp = logp_out;  a.entropy = entropy_out;  a.top_token = top_token_out;  a.top_logp = top_logp_out;
     int waves;
     plan_scores(rows, V, waves, a.n_parts, a.part);
-    a.heads = (QrScoresHead *)workspace;
-    a.cands = (QrCand *)((char *)workspace + (size_t)rows * a.n_parts * sizeof(QrScoresHead));
+    a.heads = (QrScoresSum *)workspace;
+    a.cands = (QrCand *)((char *)workspace + (size_t)rows * a.n_parts * sizeof(QrScoresSum));
     auto launch = [&](auto zero) {
         using T = decltype(zero);
         if (n_top) launch_scores<T, true>(a, waves, (hipStream_t)stream);

@@ -126,15 +126,16 @@ __device__ __forceinline__ void qr_rank(const QrCand *list, int M, int W, int ti
     }
 }
 
-// A bound from below of the K-th largest of 256 groups' keys, four to a lane: the K-th largest itself, or a little less (as soon as
+// A bound from below of the K-th largest of 64 * NG groups' keys, NG to a lane: the K-th largest itself, or a little less (as soon as
 // no more than `enough` groups pass); 0 if fewer than K groups have one.  top: the largest.  By bits of the distance from it, which
 // begin where the groups' distances do: the first bits of the keys themselves tell little apart.
-__device__ __forceinline__ unsigned qr_bound_of(const unsigned (&g)[4], unsigned top, int K, int enough)
+template <int NG>
+__device__ __forceinline__ unsigned qr_bound_of(const unsigned (&g)[NG], unsigned top, int K, int enough)
 {
-    unsigned d[4], far = 0u;
+    unsigned d[NG], far = 0u;
     int some = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NG; ++i) {
         d[i] = g[i] ? top - g[i] : ~0u;
         far = g[i] && d[i] > far ? d[i] : far;
         some += (int)__popcll(__ballot(g[i] != 0u));
@@ -147,7 +148,7 @@ __device__ __forceinline__ unsigned qr_bound_of(const unsigned (&g)[4], unsigned
         const unsigned trial = D & ~(1u << bit);
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) n += (int)__popcll(__ballot(d[i] <= trial));
+        for (int i = 0; i < NG; ++i) n += (int)__popcll(__ballot(d[i] <= trial));
         if (n >= K) {
             D = trial;   // uniform
             if (n <= enough) break;
