@@ -343,8 +343,9 @@ __device__ __attribute__((noinline)) QrScoresSum sums_of_any(const T *x, int n, 
 }
 
 // A wave to a row: many rows, or short ones.  Grid: y (and z) = four rows.
+// Bound by memory where rows are long (16384 x 32000 bf16, 1.05 GB: 190 us, 5.5 TB/s; with eight waves to a SIMD instead of four 198).
 template <class T, bool TOP>
-__global__ __launch_bounds__(256, TOP ? 6 : 8) void scores_wave_kernel(const QrScoresArgs a)
+__global__ __launch_bounds__(256, TOP ? 8 : 4) void scores_wave_kernel(const QrScoresArgs a)
 {
     constexpr int LEN = QrChunk<T>::LEN;
     __shared__ QrCand lists[TOP ? 4 : 1][TOP ? CAP : 1];
@@ -440,6 +441,9 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
     auto find_bound = [&](unsigned k) {
         if (NW == 4) {
             group_best[tid] = k;
+        } else if (NW == 8) {
+            const unsigned o = (unsigned)__builtin_amdgcn_update_dpp(0, (int)k, 0xB1, 0xf, 0xf, true);   // the neighbour's
+            if ((lane & 1) == 0) group_best[tid >> 1] = o > k ? o : k;
         } else {
             const unsigned four = qr_quad_max(k);
             if ((lane & 3) == 0) group_best[tid >> 2] = four;
@@ -610,15 +614,21 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
     if (tid >= M && tid < a.n) values.write_rank(a, row, tid, 0ull);
 }
 
-// Waves to a row, and parts of it.
-constexpr int FEW_ROWS = 256, STRETCH = 16384;
-void plan_scores(int rows, int V, int &waves, int &n_parts, int &part)
+// Waves to a row, and parts of it.  A wave reads CHUNK = 256 vectors at a time, a workgroup of 16 waves 16 times as many.
+// Measured (us; 1 / 4 / 8 / 16 waves), 16 alternatives: 1024 x 32000 bf16 36.9 / 25.8 / 22.6 / 24.2, 4096 x 32000 68 / 68 / 62 / 78, 8192 x 32000 125 /
+// 133 / 124 / 154, 256 x 8000 15.7 / 5.8 / 6.9 / 8.7, 256 x 131072 fp32 136 / 72 / 43 / 31, 4096 x 2500 fp32 14.6 / 17.7 / 28 / 54; none: 1024 x
+// 32000 bf16 14.8 / 14.9 / 15.1 / 16.0.  In parts, with another launch that joins them (1 / 4 / 8 / 16 of them): 1 x 131072 fp32 17.7 / 11.3 / 9.2 /
+// 9.7, 16 x 262144 fp32 39 / 25 / 21 / 18, 64 x 131072 fp32 24.5 / 16.3 / 16.6 / 16.5; a row of two pieces of 16 waves, 1 x 32000 fp32, 7.6 whole, 8.7.
+constexpr int FEW_ROWS = 256, STRETCH = 16384;   // (the shortest that a workgroup of 16 waves reads at a time)
+void plan_scores(int rows, int V, int n, int chunk, int &waves, int &n_parts, int &part)
 {
-    waves = rows >= 4096 || V <= 2048 ? 1 : rows >= 1024 || V <= 8192 ? 4 : 16;
+    const int chunks = (V + chunk - 1) / chunk;
+    if (chunks == 1 || rows >= 8192 || (chunks <= 3 && rows >= 2048) || (n == 0 && rows >= 1024)) waves = 1;
+    else waves = chunks <= 6 ? 4 : chunks <= 24 ? 8 : 16;
     n_parts = 1;
-    if (waves == 16 && rows < FEW_ROWS) {
-        n_parts = (V + STRETCH - 1) / STRETCH;
-        n_parts = n_parts < FEW_ROWS / rows ? n_parts : FEW_ROWS / rows;
+    const int pieces = (chunks + 15) / 16;
+    if (waves == 16 && pieces > 2 && rows < FEW_ROWS) {
+        n_parts = pieces < FEW_ROWS / rows ? pieces : FEW_ROWS / rows;
         n_parts = n_parts < MAX_PARTS ? n_parts : MAX_PARTS;
     }
     part = qr_round_up((int)(((int64_t)V + n_parts - 1) / n_parts), 8);
@@ -638,6 +648,7 @@ void launch_scores(const QrScoresArgs &a, int waves, hipStream_t st)
     const dim3 grid(a.n_parts, (unsigned)(n < 32768 ? n : 32768), (unsigned)((n + 32767) / 32768));
     if (waves == 1) scores_wave_kernel<T, TOP><<<grid, 256, 0, st>>>(a);
     else if (waves == 4) scores_group_kernel<T, 4, TOP><<<grid, 256, 0, st>>>(a);
+    else if (waves == 8) scores_group_kernel<T, 8, TOP><<<grid, 512, 0, st>>>(a);
     else scores_group_kernel<T, 16, TOP><<<grid, 1024, 0, st>>>(a);
     if (a.n_parts > 1) scores_join_kernel<T><<<a.rows, 64 * MAX_PARTS, 0, st>>>(a);
 }
@@ -666,7 +677,7 @@ extern "C" qrnnt_status qrnnt_token_scores(const void *logits, int32_t dtype, in
     a.logits = logits;  a.ld = ld;  a.token = token;  a.rows = rows;  a.V = V;  a.n = n_top;
     a.logp = logp_out;  a.entropy = entropy_out;  a.top_token = top_token_out;  a.top_logp = top_logp_out;
     int waves;
-    plan_scores(rows, V, waves, a.n_parts, a.part);
+    plan_scores(rows, V, n_top, dtype == QRNNT_F32 ? QrChunk<float>::LEN : QrChunk<__bf16>::LEN, waves, a.n_parts, a.part);
     a.heads = (QrScoresSum *)workspace;
     a.cands = (QrCand *)((char *)workspace + (size_t)rows * a.n_parts * sizeof(QrScoresSum));
     auto launch = [&](auto zero) {

@@ -310,6 +310,12 @@ def _here(first: torch.Tensor, *others):
         raise ValueError(f"expected a tensor on the current GPU, got one on {first.device}")
 
 
+def _here_stream(first: torch.Tensor, *others) -> int:
+    """_here, and the current stream's handle."""
+    _here(first, *others)
+    return torch._C._cuda_getCurrentRawStream(first.get_device())
+
+
 def _matrix(t: torch.Tensor, dtype, rows: int, cols: int):
     """(address, pitch) of a [rows, cols] matrix whose rows may lie apart."""
     if t.dtype is not dtype:
@@ -433,9 +439,10 @@ class Mx4Mat:
 
     def __init__(self, packed: torch.Tensor, rows: int, cols: int):
         self.packed, self.rows, self.cols = packed, rows, cols
+        self._c = CMx4(packed.data_ptr(), rows, cols)
 
     def c(self) -> CMx4:
-        return CMx4(self.packed.data_ptr(), self.rows, self.cols)
+        return self._c
 
 
 def mx4_pitch(cols: int) -> int:
@@ -451,40 +458,50 @@ def mx4_scale_pitch(cols: int) -> int:
 def _mx4(codes: torch.Tensor, scale: torch.Tensor, rows: int, cols: int):
     """(address and pitch of the codes, address and pitch of the scales) of [rows, cols] values."""
     width, n_scale = (cols + 31) // 32 * 16, (cols + 255) // 256 * 8
-    pq, ld_q = _matrix(codes, torch.uint8, rows, codes.shape[-1])
-    ps, ld_s = _matrix(scale, torch.uint8, rows, scale.shape[-1])
-    if codes.shape[1] < width or scale.shape[1] < n_scale:
-        raise ValueError(f"rows of {cols} columns take {width} bytes of codes and {n_scale} scales, got {codes.shape[1]} and {scale.shape[1]}")
-    return pq, width if rows <= 1 else ld_q, ps, n_scale if rows <= 1 else ld_s
+    wide, wide_s = codes.shape[-1], scale.shape[-1]
+    pq, ld_q = _matrix(codes, torch.uint8, rows, wide)
+    ps, ld_s = _matrix(scale, torch.uint8, rows, wide_s)
+    if wide < width or wide_s < n_scale:
+        raise ValueError(f"rows of {cols} columns take {width} bytes of codes and {n_scale} scales, got {wide} and {wide_s}")
+    return (pq, ld_q, ps, ld_s) if rows > 1 else (pq, width, ps, n_scale)
 
 
 def quantize_mx4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """[rows, cols] of float32, float16 or bfloat16 (rows may lie apart) -> uint8 codes [rows, mx4_pitch(cols)] (two columns to
     a byte) and uint8 scales [rows, mx4_scale_pitch(cols)]: 4-bit floats with a power of two for each block of 32 columns
     (qrnnt_quantize_mx4)."""
-    _here(x, codes, scale)
+    stream = _here_stream(x, codes, scale)
     dtype = x.dtype
     rows, cols = x.shape
     px, ld = _matrix(x, dtype, rows, cols)
+    given = codes is not None or scale is not None
+    ld_q, ld_s = (cols + 31) // 32 * 16, (cols + 255) // 256 * 8
     if codes is None:
-        codes = torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=x.device)
+        codes = torch.empty((rows, ld_q), dtype=torch.uint8, device=x.device)
     if scale is None:
-        scale = torch.empty((rows, (cols + 255) // 256 * 8), dtype=torch.uint8, device=x.device)
-    pq, ld_q, ps, ld_s = _mx4(codes, scale, rows, cols)
-    _call("qrnnt_quantize_mx4", px, _dtype(dtype), rows, cols, ld, pq, ld_q, ps, ld_s, _stream_handle())
+        scale = torch.empty((rows, ld_s), dtype=torch.uint8, device=x.device)
+    if given:
+        pq, ld_q, ps, ld_s = _mx4(codes, scale, rows, cols)
+    else:
+        pq, ps = codes.data_ptr(), scale.data_ptr()
+    _call("qrnnt_quantize_mx4", px, _dtype(dtype), rows, cols, ld, pq, ld_q, ps, ld_s, stream)
     return codes, scale
 
 
 def dequantize_mx4(codes: torch.Tensor, scale: torch.Tensor, cols: int, dtype: torch.dtype = torch.float32,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values [rows, cols] that codes and scales stand for (qrnnt_dequantize_mx4)."""
-    _here(codes, scale, out)
+    stream = _here_stream(codes, scale, out)
     rows = codes.shape[0]
     pq, ld_q, ps, ld_s = _mx4(codes, scale, rows, _int32(cols, "cols"))
     if out is None:
+        kind = _dtype(dtype)
         out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
-    px, ld = _matrix(out, out.dtype, rows, cols)
-    _call("qrnnt_dequantize_mx4", pq, ld_q, ps, ld_s, rows, cols, px, _dtype(out.dtype), ld, _stream_handle())
+        px, ld = out.data_ptr(), cols
+    else:
+        kind = _dtype(out.dtype)
+        px, ld = _matrix(out, out.dtype, rows, cols)
+    _call("qrnnt_dequantize_mx4", pq, ld_q, ps, ld_s, rows, cols, px, kind, ld, stream)
     return out
 
 
@@ -515,7 +532,7 @@ def linear_mx4(w: Mx4Mat, codes: torch.Tensor, scale: torch.Tensor, bias: Option
                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Linear layer of microscaled 4-bit floats: w from pack_mx4, codes and scales as quantize_mx4 returns them
     (qrnnt_linear_mx4).  out may be a matrix whose rows lie apart."""
-    _here(codes, scale, bias, workspace, w.packed, out)
+    stream = _here_stream(codes, scale, bias, workspace, w.packed, out)
     M = codes.shape[0]
     pa, ld_a, ps, ld_s = _mx4(codes, scale, M, w.cols)
     if out is None:
@@ -525,13 +542,13 @@ def linear_mx4(w: Mx4Mat, codes: torch.Tensor, scale: torch.Tensor, bias: Option
     else:
         kind = _dtype(out.dtype)
         py, ld_y = _matrix(out, out.dtype, M, w.rows)
-    cw = w.c()
+    cw = C.byref(w.c())
     if workspace is None:
-        need = load().qrnnt_linear_mx4_workspace(C.byref(cw), M)
+        need = load().qrnnt_linear_mx4_workspace(cw, M)
         workspace = torch.empty(need, dtype=torch.uint8, device=codes.device) if need else None
     n_ws = 0 if workspace is None else workspace.nbytes
-    _call("qrnnt_linear_mx4", C.byref(cw), _vector(bias, torch.float32, w.rows), pa, ld_a, ps, ld_s, M, py, kind, ld_y,
-          _addr(workspace) if n_ws else None, n_ws, _stream_handle())
+    _call("qrnnt_linear_mx4", cw, _vector(bias, torch.float32, w.rows), pa, ld_a, ps, ld_s, M, py, kind, ld_y,
+          _addr(workspace) if n_ws else None, n_ws, stream)
     return out
 
 
@@ -799,25 +816,32 @@ def token_scores(logits: torch.Tensor, token: Optional[torch.Tensor] = None, n_t
     """Log probability of token[r] (int32; negative: padding, 0) in row r of logits [rows, V] (float32, float16 or bfloat16; rows may
     lie apart), the row's entropy, its n_top best tokens and their log probabilities: (logp [rows] or None without token,
     entropy [rows] or None, tokens [rows, n_top], logp of those), the last two None without n_top (qrnnt_token_scores)."""
-    _here(logits, token, workspace)
+    stream = _here_stream(logits, token, workspace)
     rows, V = logits.shape
-    pl, ld = _matrix(logits, logits.dtype, rows, V)
-    kind = _dtype(logits.dtype)
+    dtype, dev = logits.dtype, logits.device
+    pl, ld = _matrix(logits, dtype, rows, V)
+    kind = _dtype(dtype)
     pt = _vector(token, torch.int32, rows)
+    if not 0 <= n_top <= 64:
+        _check(7 if n_top > 64 else 2, "qrnnt_token_scores")
     if workspace is None:
-        need = token_scores_workspace(rows, V, n_top)
+        need = load().qrnnt_token_scores_workspace(rows, V, n_top)
         if need == 0:
-            _check(7 if rows >= 0 and V > 0 and n_top >= 0 else 2, "qrnnt_token_scores_workspace")
-        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
-    elif n_top < 0 or n_top > 64:
-        _check(2 if n_top < 0 else 7, "qrnnt_token_scores")
-    make = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
-    logp = None if token is None else make(rows)
-    ent = make(rows) if entropy else None
-    tokens, values = (make(rows, n_top, dtype=torch.int32), make(rows, n_top)) if n_top else (None, None)
-    ptr = lambda t: None if t is None else t.data_ptr()
-    _call("qrnnt_token_scores", pl, kind, ld, pt, rows, V, n_top, ptr(logp), ptr(ent), ptr(tokens), ptr(values), _addr(workspace),
-          workspace.nbytes, _stream_handle())
+            _check(7 if V > 0 else 2, "qrnnt_token_scores_workspace")
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    logp = ent = tokens = values = p_logp = p_ent = p_tokens = p_values = None
+    if token is not None:
+        logp = torch.empty(rows, dtype=torch.float32, device=dev)
+        p_logp = logp.data_ptr()
+    if entropy:
+        ent = torch.empty(rows, dtype=torch.float32, device=dev)
+        p_ent = ent.data_ptr()
+    if n_top:
+        tokens = torch.empty((rows, n_top), dtype=torch.int32, device=dev)
+        values = torch.empty((rows, n_top), dtype=torch.float32, device=dev)
+        p_tokens, p_values = tokens.data_ptr(), values.data_ptr()
+    _call("qrnnt_token_scores", pl, kind, ld, pt, rows, V, n_top, p_logp, p_ent, p_tokens, p_values, _addr(workspace), workspace.nbytes,
+          stream)
     return logp, ent, tokens, values
 
 
