@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_mx4_few_kernel(const QrMx4L
     for (int i = 0; i < RT; ++i) {
         const int rt = rt0 + i < n_row_tiles ? rt0 + i : n_row_tiles - 1;
         w[i] = p.w + (size_t)rt * p.nkc * 128 + lane;
-        sw[i] = p.s_w + (size_t)rt * p.nkc * 128 + lane * 2;
+        sw[i] = p.s_w + (size_t)rt * p.nkc * 128 + col * 8 + grp * 2;
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -123,15 +123,18 @@ __global__ __launch_bounds__(64 * WAVES) void linear_mx4_few_kernel(const QrMx4L
 
 // Many tokens: the matrix units are what is kept busy.  A workgroup of WN x WM waves has BN = 16*MT*WN weight rows x
 // BM = 16*NT*WM tokens.  LDS holds the weights of 2D steps of 128 columns (1 KiB blocks as the packed form has them: operand order),
-// the activations of D chunks of 256 (1 KiB blocks of 8 tokens x 128 bytes, lane l of the loading wave fetching token l/8's
-// 16-byte piece (l%8) ^ (l/8): whole lines per load, operand reads spread over the banks) and both scales of D chunks.  All arrive by
+// the activations of D chunks of 256 (1 KiB blocks of 8 tokens x 128 bytes, whole lines per load; token t of 16 has its 16-byte piece q
+// at q ^ (4 (t/8) + (t/2)%2): the lanes 0-3, 12-15 and 20-27, whose 256 bytes are read at a time, and the others likewise, find them in
+// different banks) and both scales of D chunks.  All arrive by
 // direct loads to LDS up to three steps ahead, and a wave reads the next step's first operands before its last matrix instructions of
 // the present one.
 template <int MT, int NT, int WN, int WM, int D>
 struct QrMx4Tile {
     static constexpr int WAVES = WN * WM, THREADS = 64 * WAVES;
     static constexpr int BN = 16 * MT * WN, BM = 16 * NT * WM;
+    static constexpr int AHEAD = MT > 4 ? 1 : 2;   // weight operands that are read ahead of their row tile
     static constexpr int A_BLOCKS = MT * WN, B_BLOCKS = 2 * NT * WM;      // of 1 KiB: weights of a step, activations of a chunk
+    static constexpr int SQ = NT < 4 ? 1 : 4;   // token tiles whose scales are read at once
     static constexpr int SA_BLOCKS = MT * WN / 2, SB_BLOCKS = NT * WM / 2;   // of 256 bytes: scales of a chunk
     static constexpr int A_LOADS = A_BLOCKS / WAVES, B_LOADS = B_BLOCKS / WAVES, S_LOADS = (SA_BLOCKS + SB_BLOCKS) / WAVES;
     static constexpr int A_STAGE = A_BLOCKS * 1024, B_STAGE = B_BLOCKS * 1024, S_STAGE = (SA_BLOCKS + SB_BLOCKS) * 256;
@@ -140,6 +143,7 @@ struct QrMx4Tile {
     static constexpr int BIAS_BYTES = BN * 4, LDS = BIAS + 2 * BIAS_BYTES;
     static_assert(A_BLOCKS % WAVES == 0 && B_BLOCKS % WAVES == 0 && (SA_BLOCKS + SB_BLOCKS) % WAVES == 0, "every wave loads as much");
     static_assert(MT * WN % 2 == 0 && NT * WM % 2 == 0, "scales of two tiles to a load");
+    static_assert(MT % 4 == 0 && NT % SQ == 0, "scales of four tiles to a read");
     static_assert(D == 2 || D == 4, "ring of chunks");
     static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
 };
@@ -161,7 +165,6 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
     constexpr bool PART = std::is_same<T, v4f>::value;
     const int kc0 = PART ? (int)((int64_t)p.nkc * blockIdx.y / gridDim.y) : 0;
     const int nkc = PART ? (int)((int64_t)p.nkc * (blockIdx.y + 1) / gridDim.y) - kc0 : p.nkc;
-    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
     auto locate = [&](int at, int &rt0, int &m0) {
         const int xcd = at & 7, each = total >> 3, rest = total & 7;
         const int tile = xcd * each + (xcd < rest ? xcd : rest) + (at >> 3);
@@ -170,6 +173,8 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
         rt0 = (stripe * G + in_stripe % width) * (P::BN / 16);
         m0 = in_stripe / width * P::BM;
     };
+    static_assert(P::B_LOADS % 2 == 0, "a wave's blocks begin with tokens 0 to 7 of a tile");
+    auto piece = [&](int i) { return ((lane & 7) ^ ((i & 1) * 4 + (lane >> 4 & 1))) * 16; };
     const v4i *src_a[P::A_LOADS];
     const uint8_t *src_b[P::B_LOADS], *src_s[P::S_LOADS];
     auto load_a = [&](int i, int k) {
@@ -180,7 +185,7 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
         if (i < P::B_LOADS) {
             const int c = (kc0 + kc) * 128;   // pieces behind the row: its start instead (finite codes meet zero weights)
             const unsigned to = lds0 + P::B_AT + (kc & (D - 1)) * P::B_STAGE + (wave * P::B_LOADS + i) * 1024;
-            qr_load_lds16(src_b[i] + (c + piece < p.bytes ? c : -piece), __builtin_amdgcn_readfirstlane(to));
+            qr_load_lds16(src_b[i] + (c + piece(i) < p.bytes ? c : -piece(i)), __builtin_amdgcn_readfirstlane(to));
         } else {
             const int j = i - P::B_LOADS, at = wave * P::S_LOADS + j;
             const unsigned to = lds0 + P::S_AT + (kc & (D - 1)) * P::S_STAGE + at * 256;
@@ -217,17 +222,21 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
 #pragma unroll
         for (int i = 0; i < P::B_LOADS; ++i) {
             const int m = m0 + (wave * P::B_LOADS + i) * 8 + (lane >> 3);
-            src_b[i] = p.a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_a + piece;
+            src_b[i] = p.a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_a + piece(i);
         }
 #pragma unroll
         for (int j = 0; j < P::S_LOADS; ++j) {
             const int at = wave * P::S_LOADS + j;
-            if (at < P::SA_BLOCKS) {   // two row tiles
-                const int t = rt0 + 2 * at + (lane >> 5), rt = t < n_row_tiles ? t : n_row_tiles - 1;
-                src_s[j] = p.s_w + ((size_t)rt * p.nkc + kc0) * 128 + (lane & 31) * 4;
-            } else {                   // 32 tokens
-                const int m = m0 + (at - P::SA_BLOCKS) * 32 + (lane >> 1);
-                src_s[j] = p.s_a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_sa + kc0 * 8 + (lane & 1) * 4;
+            // in LDS: [four tiles][half of the chunk's scales][row of a tile][tile], four bytes each, so that a lane reads four tiles' at once
+            const bool w = at < P::SA_BLOCKS;
+            const int d = (w ? at : at - P::SA_BLOCKS) * 64 + lane, Q = w ? 4 : P::SQ;
+            const int tile = d / (32 * Q) * Q + d % Q, r = d / Q % 16, half = d / (16 * Q) % 2 * 4;
+            if (w) {
+                const int rt = rt0 + tile < n_row_tiles ? rt0 + tile : n_row_tiles - 1;
+                src_s[j] = p.s_w + ((size_t)rt * p.nkc + kc0) * 128 + r * 8 + half;
+            } else {
+                const int m = m0 + tile * 16 + r;
+                src_s[j] = p.s_a + (int64_t)(m < p.M ? m : p.M - 1) * p.ld_sa + kc0 * 8 + half;
             }
         }
 #pragma unroll
@@ -238,14 +247,17 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
     };
     const char *fa = lds + wn * MT * 1024 + lane * 16;
     const char *fb = lds + P::B_AT + (wm * NT * 2 + (col >> 3)) * 1024 + (col & 7) * 128;
-    const int half0 = ((2 * grp) ^ (col & 7)) * 16, half1 = ((2 * grp + 1) ^ (col & 7)) * 16;
-    const char *fsa = lds + P::S_AT + wn * MT * 128 + lane * 2;
-    const char *fsb = lds + P::S_AT + P::SA_BLOCKS * 256 + (wm * NT * 16 + col) * 8 + grp * 2;
+    const int turn_of = (col >> 3) * 4 + (col >> 1 & 1), half0 = ((2 * grp) ^ turn_of) * 16, half1 = ((2 * grp + 1) ^ turn_of) * 16;
+    const char *fsa = lds + P::S_AT + (wn * (MT / 4) * 32 + (grp >> 1) * 16 + col) * 16;
+    const char *fsb = lds + P::S_AT + P::SA_BLOCKS * 256 + (wm * (NT / P::SQ) * 32 + (grp >> 1) * 16 + col) * (4 * P::SQ);
+    const int mine = (grp & 1) * 16;   // a lane's two scales of four
 
-    constexpr int AHEAD = MT > 2 ? 2 : 1;   // weight operands that are read ahead
+    constexpr int AHEAD = P::AHEAD;
     v4f acc[MT][NT];
     v4i b[2][NT] = {}, w[2][MT] = {};
-    int sw[MT], sa[NT], sw_next[MT] = {}, sa_next[NT] = {};   // scales of the chunk
+    int sw[MT], sa[NT];   // scales of the chunk
+    v4i sw_next[MT / 4] = {}, sa_next[(NT + 3) / 4] = {};
+    static_assert(P::SQ == 4 || NT <= 4, "scales of token tiles in one vector");
     auto wait = [&](auto left) {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(left)::value) : "memory");
@@ -259,10 +271,16 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) w[h][j] = *(const v4i *)(fa + (k & (2 * D - 1)) * P::A_STAGE + j * 1024);
         if (h == 0) {
+            const int at = ((k >> 1) & (D - 1)) * P::S_STAGE;
+            if constexpr (P::SQ == 4) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sa_next[nt] = *(const uint16_t *)(fsb + ((k >> 1) & (D - 1)) * P::S_STAGE + nt * 128);
+                for (int q = 0; q < NT / 4; ++q) sa_next[q] = *(const v4i *)(fsb + at + q * 512);
+            } else {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) sw_next[i] = *(const uint16_t *)(fsa + ((k >> 1) & (D - 1)) * P::S_STAGE + i * 128);
+                for (int nt = 0; nt < NT; ++nt) sa_next[0][nt] = *(const int *)(fsb + at + nt * 128);
+            }
+#pragma unroll
+            for (int q = 0; q < MT / 4; ++q) sw_next[q] = *(const v4i *)(fsa + at + q * 512);
         }
     };
     using std::integral_constant;
@@ -273,9 +291,9 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
         constexpr int NB = decltype(lb)::value ? B : 0, N = NB + (decltype(la)::value ? A : 0), ROOM = MT - AHEAD;
         if (h == 0) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sa[nt] = sa_next[nt];
+            for (int nt = 0; nt < NT; ++nt) sa[nt] = (int)((unsigned)sa_next[nt / 4][nt % 4] >> mine);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) sw[i] = sw_next[i];
+            for (int i = 0; i < MT; ++i) sw[i] = (int)((unsigned)sw_next[i / 4][i % 4] >> mine);
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -289,10 +307,8 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
                 wait(integral_constant<int, LEFT >= 0 ? LEFT : 0>{});
                 first_reads(k + 1, integral_constant<int, 1 - h>{});
             }
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) acc[i][nt] = mfma_mx4<h>(w[h][i], b[h][nt], sw[i], sa[nt], acc[i][nt]);
-            __builtin_amdgcn_sched_barrier(0);
         }
     };
     constexpr integral_constant<int, 0> zero{};
@@ -512,7 +528,7 @@ void launch_tiles(const QrMx4Linear &p, int parts, hipStream_t st)
 {
     using P = QrMx4Tile<MT, NT, WN, WM, D>;
     const int tn = (p.rows + P::BN - 1) / P::BN, tm = (p.M + P::BM - 1) / P::BM;
-    const int places = P::WAVES == 8 ? 256 : 512;   // what 256 compute units hold
+    const int places = P::LDS > 80 * 1024 ? 256 : 512;   // what 256 compute units hold
     static std::atomic<bool> allowed[QR_MAX_DEVICES];   // per device: more than 64 KiB of LDS
     const int d = qr_current_device();
     if (!allowed[d].load(std::memory_order_relaxed) &&

@@ -16,6 +16,6 @@ static inline int qr_mx4_chunks(int cols) { return qr_mx4_scale_pitch(cols) / 8;
 // Packed weights: first the codes, for every [row tile of 16][chunk] two blocks of 1 KiB, each the operand of one matrix
 // instruction as it is: lane l's 16 bytes at 16*l of block h are block 8*chunk + 2*(l/16) + h of row 16*tile + l%16.  (A lane of
 // group g takes the blocks 2g and 2g + 1 in the two instructions, so that its two scales lie side by side; the activations
-// are read in the same order.)  Then the scales, 128 bytes for every [row tile][chunk]: bytes 2*l and 2*l + 1 for lane l.
+// are read in the same order.)  Then the scales, 128 bytes for every [row tile][chunk]: the chunk's 8 scales of 16 rows.
 static inline size_t qr_mx4_tiles(int rows, int cols) { return (size_t)((rows + 15) / 16) * qr_mx4_chunks(cols); }
 static inline size_t qr_mx4_packed_bytes(int rows, int cols) { return qr_mx4_tiles(rows, cols) * (2048 + 128); }

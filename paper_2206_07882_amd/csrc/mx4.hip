@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256) void pack_mx4_kernel(const QrMx4Pack a)
         unsigned two = 0u;
 #pragma unroll
         for (int j = 0; j < 2; ++j) two |= (row < a.rows && b + j < a.blocks ? (unsigned)a.scale[row * a.ld_s + b + j] : 127u) << (8 * j);
-        *(uint16_t *)(a.out + a.tiles * 2048 + tile * 128 + lane * 2) = (uint16_t)two;
+        *(uint16_t *)(a.out + a.tiles * 2048 + tile * 128 + (lane & 15) * 8 + (lane >> 4) * 2) = (uint16_t)two;
     }
 }
 

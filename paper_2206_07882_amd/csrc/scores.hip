@@ -290,7 +290,7 @@ struct QrScoresWave {
             count += (int)__popcll(m);
         }
         __builtin_amdgcn_wave_barrier();
-        if (count >= 2 * n + 32) {
+        if (count >= 3 * n + 48) {
             // what this wave has not read yet lies behind: to be among the best it has to be larger
             const unsigned k = keep_best<CAP>(list, count, n, n + n / 4, lane) + 1u;
             key = k > key ? k : key;
@@ -298,18 +298,19 @@ struct QrScoresWave {
     }
 };
 
-// The bound that groups of a wave's logits give.  Few ranks: a lane's are a group.
+// The bound that groups of a wave's logits give.  Few ranks: a lane's are a group.  (Up to twice as many as there are ranks may reach it:
+// the search is shorter, 1024 x 32000 bf16, 16 ranks, AA us with a quarter more at most, BB now.)
 template <class T>
 __device__ __forceinline__ unsigned first_bound(const QrScoresWave<T> &w, int n)
 {
-    if (n <= 16) {
+    if (n <= 24) {
         const unsigned g[1] = {qr_logit_key(w.largest)};
-        return qr_bound_of(g, qr_wave_reduce_u32<true>(g[0]), n, n + n / 4);
+        return qr_bound_of(g, qr_wave_reduce_u32<true>(g[0]), n, 2 * n);
     }
     unsigned g[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) g[v] = qr_logit_key(w.best[v]);
-    return qr_bound_of(g, qr_wave_reduce_u32<true>(qr_logit_key(w.largest)), n, n + n / 4);
+    return qr_bound_of(g, qr_wave_reduce_u32<true>(qr_logit_key(w.largest)), n, 2 * n);
 }
 
 // Sums of a row's part that are good for any logits: relative to its largest one.  WPR waves of a workgroup, `most` in LDS.
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
                 one[0] = g[i] > one[0] ? g[i] : one[0];
             }
             const unsigned top = qr_wave_reduce_u32<true>(one[0]);
-            const unsigned bound = a.n <= 16 ? qr_bound_of(one, top, a.n, a.n + a.n / 4) : qr_bound_of(g, top, a.n, a.n + a.n / 4);
+            const unsigned bound = a.n <= 24 ? qr_bound_of(one, top, a.n, 2 * a.n) : qr_bound_of(g, top, a.n, 2 * a.n);
             if (lane == 0) shared_key = bound;
         }
     };
@@ -588,16 +589,21 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
         values.write(a, row, token);
     }
     if (a.n == 0) return;
-    const unsigned four = qr_quad_max((unsigned)(mine >> 32));
-    if ((lane & 3) == 0) group_best[tid >> 2] = four;
-    __syncthreads();
-    unsigned g[4], most = 0u;
+    unsigned bound = 1u;
+    if (a.n_parts * a.n > 256) {   // (ranks of fewer are counted in less time than a bound takes)
+        const unsigned four = qr_quad_max((unsigned)(mine >> 32));
+        if ((lane & 3) == 0) group_best[tid >> 2] = four;
+        __syncthreads();
+        unsigned g[4], most = 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        g[i] = group_best[i * 64 + lane];
-        most = g[i] > most ? g[i] : most;
+        for (int i = 0; i < 4; ++i) {
+            g[i] = group_best[i * 64 + lane];
+            most = g[i] > most ? g[i] : most;
+        }
+        bound = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, 2 * a.n);
+    } else {
+        __syncthreads();
     }
-    const unsigned bound = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, a.n + a.n / 4);
     if (mine != 0ull && (unsigned)(mine >> 32) >= bound) all[atomicAdd(&n_all, 1)] = mine;
     __syncthreads();
     const int M = n_all;

@@ -312,8 +312,13 @@ def _here(first: torch.Tensor, *others):
 
 def _here_stream(first: torch.Tensor, *others) -> int:
     """_here, and the current stream's handle."""
-    _here(first, *others)
-    return torch._C._cuda_getCurrentRawStream(first.get_device())
+    device = first.get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError(f"expected a tensor on the current GPU, got one on {first.device}")
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"expected a tensor on the current GPU, got one on {t.device}")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _matrix(t: torch.Tensor, dtype, rows: int, cols: int):
@@ -477,9 +482,9 @@ def quantize_mx4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: O
     given = codes is not None or scale is not None
     ld_q, ld_s = (cols + 31) // 32 * 16, (cols + 255) // 256 * 8
     if codes is None:
-        codes = torch.empty((rows, ld_q), dtype=torch.uint8, device=x.device)
+        codes = torch.empty(rows, ld_q, dtype=torch.uint8, device=x.device)
     if scale is None:
-        scale = torch.empty((rows, ld_s), dtype=torch.uint8, device=x.device)
+        scale = torch.empty(rows, ld_s, dtype=torch.uint8, device=x.device)
     if given:
         pq, ld_q, ps, ld_s = _mx4(codes, scale, rows, cols)
     else:
@@ -496,7 +501,7 @@ def dequantize_mx4(codes: torch.Tensor, scale: torch.Tensor, cols: int, dtype: t
     pq, ld_q, ps, ld_s = _mx4(codes, scale, rows, _int32(cols, "cols"))
     if out is None:
         kind = _dtype(dtype)
-        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+        out = torch.empty(rows, cols, dtype=dtype, device=codes.device)
         px, ld = out.data_ptr(), cols
     else:
         kind = _dtype(out.dtype)
@@ -537,7 +542,7 @@ def linear_mx4(w: Mx4Mat, codes: torch.Tensor, scale: torch.Tensor, bias: Option
     pa, ld_a, ps, ld_s = _mx4(codes, scale, M, w.cols)
     if out is None:
         kind = _dtype(dtype)
-        out = torch.empty((M, w.rows), dtype=dtype, device=codes.device)
+        out = torch.empty(M, w.rows, dtype=dtype, device=codes.device)
         py, ld_y = out.data_ptr(), w.rows
     else:
         kind = _dtype(out.dtype)
@@ -837,8 +842,8 @@ def token_scores(logits: torch.Tensor, token: Optional[torch.Tensor] = None, n_t
         ent = torch.empty(rows, dtype=torch.float32, device=dev)
         p_ent = ent.data_ptr()
     if n_top:
-        tokens = torch.empty((rows, n_top), dtype=torch.int32, device=dev)
-        values = torch.empty((rows, n_top), dtype=torch.float32, device=dev)
+        tokens = torch.empty(rows, n_top, dtype=torch.int32, device=dev)
+        values = torch.empty(rows, n_top, dtype=torch.float32, device=dev)
         p_tokens, p_values = tokens.data_ptr(), values.data_ptr()
     _call("qrnnt_token_scores", pl, kind, ld, pt, rows, V, n_top, p_logp, p_ent, p_tokens, p_values, _addr(workspace), workspace.nbytes,
           stream)
