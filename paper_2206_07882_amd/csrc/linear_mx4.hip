@@ -325,6 +325,10 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
     locate(blockIdx.x, rt0, m0);
     int bias = P::BIAS;
     begin(rt0, m0, bias);
+    // Of several large tiles to a workgroup every second compute unit's begin later, by half the time that a tile's stores take: some store
+    // while others compute (16000 x 2560 x 1280 fp32 53 us, so 47; bf16 39 and 37; 8192 x 8192 x 512 bf16 35 and 32).
+    if (!PART && P::WAVES == 8 && total > (int)gridDim.x && (blockIdx.x >> 3 & 1))
+        for (int i = 0; i < 3 * (int)sizeof(T); ++i) __builtin_amdgcn_s_sleep(16);   // (of 1024 cycles)
     for (int at = blockIdx.x;;) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -456,26 +460,31 @@ struct QrMx4Plan {
     int n;
 };
 
-// What tiles take (us): a chunk of 256 columns while at most half of the places on the device are taken, and with all of them; what a
-// tile costs besides; what a launch does.  256 compute units hold one large tile each, or two of the others.
+// What tiles take (us), fitted to 5166 layers of 40 to 8192 columns, 48 to 32000 rows and 17 to 16384 tokens (80 % of the times within 8, 12
+// and 15 % of it; the kind and number of parts chosen by it are on average 0.4 % slower than the best): a chunk of 256 columns while
+// at most half of the places on the device are taken, and with all of them; what a tile costs besides, and for each byte of a
+// result; what a launch does.  256 compute units hold one large tile each, or two of the others.
 struct QrTileCost {
     int size, places;
-    float alone, full, fixed, start;
-    float time(int64_t tiles, int chunks) const
+    float alone, full, fixed, byte, start;
+    float time(int64_t tiles, int chunks, int bytes) const
     {
-        const int64_t rounds = tiles / places, rest = tiles % places;
-        return start + rounds * (chunks * full + fixed) + (rest == 0 ? 0.0f : chunks * (rest <= places / 2 ? alone : full) + fixed);
+        const int64_t rounds = tiles / places, rest = tiles % places, half = places / 2;
+        const float each = fixed + byte * bytes, last = alone + (rest > half ? (full - alone) * (rest - half) / half : 0.0f);
+        return start + rounds * (chunks * full + each) + (rest == 0 ? 0.0f : chunks * last + each);
     }
     int64_t tiles(int rows, int M) const { return (int64_t)((rows + size - 1) / size) * ((M + size - 1) / size); }
 };
-constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.26f, 0.43f, 1.1f, 1.9f}, {128, 512, 0.66f, 1.1f, 3.6f, 0.6f}, {256, 256, 1.03f, 1.4f, 9.6f, -1.4f}};
+constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.31f, 0.56f, 0.78f, 0.12f, 2.1f}, {128, 512, 0.70f, 1.40f, 1.0f, 0.53f, 1.7f}, {256, 256, 1.14f, 1.89f, 4.0f, 0.70f, 1.7f}};
 
 // A sum of few columns is not cut, nor one whose parts' sums, read and written, pass 512 tokens x 128 rows for each chunk of it: so
 // what a call may need is known without its plan.
 int most_parts(int nkc) { return nkc < 16 ? 1 : nkc < 32 ? nkc / 4 : 8; }
 int64_t most_sums(int nkc) { return (int64_t)nkc << 16; }
 
-QrMx4Piece plan_piece(int rows, int nkc, int M, float &least)
+// Measured at each choice (us, bf16; small / middle / large): 1000 x 1000 x 1000 (tokens x rows x columns) 4.4 / 6.8 / 11.7; 128 x 32000 x 1024 7.9 /
+// 6.6 / 10.0; 4000 x 1024 x 4096 20 / 15 / 24; 2000 x 5000 x 3000 40 / 28 / 25.  256 x 256 x 8192 on small tiles whole 13.2, in four parts 8.4.
+QrMx4Piece plan_piece(int rows, int nkc, int M, int bytes, float &least)
 {
     QrMx4Piece best = {SMALL, 1, M};
     least = INFINITY;
@@ -483,8 +492,8 @@ QrMx4Piece plan_piece(int rows, int nkc, int M, float &least)
         const QrTileCost &c = TILE_COST[kind];
         for (int parts = 1; parts <= (kind == SMALL ? most_parts(nkc) : 1); ++parts) {
             if (parts > 1 && (int64_t)parts * M * qr_round_up(rows, 4) > most_sums(nkc)) break;
-            const float join = parts == 1 ? 0.0f : 3.0f + (float)parts * M * rows * 8 / 4e6f;   // a launch, and the sums written and read at 4 TB/s
-            const float t = c.time(c.tiles(rows, M) * parts, (nkc + parts - 1) / parts) + join;
+            const float join = parts == 1 ? 0.0f : 1.0f + (float)parts * M * rows * 4e-6f;   // a launch, and the sums written and read
+            const float t = c.time(c.tiles(rows, M) * parts, (nkc + parts - 1) / parts, parts == 1 ? bytes : 4) + join;
             if (t < least) {
                 least = t;
                 best = {(QrMx4Kind)kind, parts, M};
@@ -494,17 +503,23 @@ QrMx4Piece plan_piece(int rows, int nkc, int M, float &least)
     return best;
 }
 
+// Few tokens: beyond 32 their codes are fetched as often as the weights and more, so long or many rows go to tiles.  Few against the best
+// tiles, in time: 17 to 32 tokens 0.5 to 0.9 (over 16384 rows and 4096 columns 1.04); 33 to 48 0.6 to 0.9 up to 4096 rows, 0.8 to 8192 (over 4096
+// columns 1.1), 0.9 to 16384 of up to 512 columns, 1.05 and more beyond; 49 to 64 0.7 to 0.9 up to 4096 rows, 0.8 to 8192 and 0.9 to 16384 of up to 512
+// columns, 1.0 and more beyond.
 bool few_tokens(int rows, int K, int M)
 {
-    return M <= 16 || (M <= 32 && (rows <= 8192 || K <= 2048)) || (M <= 64 && rows <= 4096 && K <= (M <= 48 ? 4096 : 2048));
+    if (M <= 32) return true;
+    if (M <= 48) return rows <= 4096 || (rows <= 8192 && K <= 4096) || (rows <= 16384 && K <= 512);
+    return M <= 64 && (rows <= 4096 || (rows <= 16384 && K <= 512));
 }
 
-QrMx4Plan plan_linear(int rows, int K, int M)
+QrMx4Plan plan_linear(int rows, int K, int M, int bytes)
 {
     if (few_tokens(rows, K, M)) return {{{FEW, 1, M}}, 1};
     const int nkc = qr_mx4_chunks(K);
     float least;
-    QrMx4Plan best = {{plan_piece(rows, nkc, M, least)}, 1};
+    QrMx4Plan best = {{plan_piece(rows, nkc, M, bytes, least)}, 1};
     // whole rounds of large tiles first, what would leave a round part empty in a launch of its own
     const QrTileCost &c = TILE_COST[LARGE];
     const int across = (rows + c.size - 1) / c.size;
@@ -513,8 +528,8 @@ QrMx4Plan plan_linear(int rows, int K, int M)
         const int64_t first = r * c.places / across * c.size;   // tokens of the whole rounds
         if (first < c.size || first >= M) continue;
         float rest;
-        const QrMx4Piece second = plan_piece(rows, nkc, M - (int)first, rest);
-        const float t = c.time(c.tiles(rows, (int)first), nkc) + rest + 3.5f;   // (the second launch waits for the first one's last stores)
+        const QrMx4Piece second = plan_piece(rows, nkc, M - (int)first, bytes, rest);
+        const float t = c.time(c.tiles(rows, (int)first), nkc, bytes) + rest + 2.0f;   // (the second launch waits for the first one's last stores)
         if (t < least) {
             least = t;
             best = {{{LARGE, 1, (int)first}, second}, 2};
@@ -621,7 +636,7 @@ extern "C" qrnnt_status qrnnt_linear_mx4(const qrnnt_mx4 *w, const float *bias, 
     p.nkc = qr_mx4_chunks(w->cols);  p.rows = w->rows;  p.bytes = qr_mx4_pitch(w->cols);
     p.a = a;  p.s_a = a_scale;  p.ld_a = ld_a;  p.ld_sa = ld_scale;  p.M = M;  p.y = y;  p.ld_y = ld_y;
     p.part = workspace;  p.ld_part = qr_round_up(w->rows, 4) / 4;
-    const QrMx4Plan plan = plan_linear(w->rows, w->cols, M);
+    const QrMx4Plan plan = plan_linear(w->rows, w->cols, M, (int)qr_dtype_size(y_dtype));
     QR_REQUIRE(plan.piece[0].kind == FEW || TILE_COST[plan.piece[0].kind].tiles(w->rows, M) < 1 << 23, QRNNT_ERR_UNSUPPORTED);   // (a grid has less than 2^32 threads)
     if (y_dtype == QRNNT_F32) launch_linear<float>(p, plan, (hipStream_t)stream);
     else if (y_dtype == QRNNT_F16) launch_linear<_Float16>(p, plan, (hipStream_t)stream);
