@@ -3,7 +3,7 @@
 //
 // With S = sum 2^(x L - r), U = sum 2^(x L - r)(x L - r), L = log2(e), for any r:  log P(x) = ln 2 (x L - r) - log S,
 // entropy = log S - ln 2 U / S.  A wave takes the largest logit of the first that it reads for r, a product, a sum, an exponential and
-// two more sums a logit then do; where a logit passes r by far (2^40) sums move to a larger one.  Lanes add up at the end of the row.
+// two more sums a logit then do; where a logit passes r by far (a sum of 2^12) sums move to a larger one.  Lanes add up at the end of the row, in fp32.
 // Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read again, with x - max
 // formed first.
 //
@@ -20,7 +20,7 @@
 namespace {
 
 constexpr int MAX_TOP = 64, CAP = 256, LIST = 1024;   // ranks; candidates in a wave's and in a workgroup's list
-constexpr int MAX_PARTS = 16;
+constexpr int MAX_PARTS = 16, FEW_RANKS = 24;
 constexpr float LOG2E = 1.4426950408889634f, FAR = -300.0f;   // 2^FAR is 0 in fp32
 constexpr float MOST = 0x1p100f;                              // r stays within
 constexpr double LN2 = 0.69314718055994530942;
@@ -131,6 +131,18 @@ typedef __attribute__((address_space(3))) QrCand *QrLdsList;   // (for functions
 __device__ __forceinline__ int lanes_below(unsigned long long m) { return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u)); }
 __device__ __forceinline__ float least_of(unsigned key) { return key > 0x00800000u ? qr_key_float(key) : -FLT_MAX; }   // (keys up to there are those of -inf and below)
 __device__ __forceinline__ float wave_max(float v) { return qr_key_float(qr_wave_reduce_u32<true>(qr_float_key(v))); }   // (v is not NaN)
+__device__ __forceinline__ float wave_add(float v)   // in all lanes: within rows of 16, then over the rows
+{
+#define QR_DPP_ADD(ctrl, rmask) v += __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, rmask, 0xf, false))
+    QR_DPP_ADD(0x111, 0xf);   // row_shr:1
+    QR_DPP_ADD(0x112, 0xf);   // row_shr:2
+    QR_DPP_ADD(0x114, 0xf);   // row_shr:4
+    QR_DPP_ADD(0x118, 0xf);   // row_shr:8
+    QR_DPP_ADD(0x142, 0xa);   // row_bcast:15 into rows 1 and 3
+    QR_DPP_ADD(0x143, 0xc);   // row_bcast:31 into rows 2 and 3
+#undef QR_DPP_ADD
+    return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
 __device__ __forceinline__ float limited(float r) { return fminf(fmaxf(r, -MOST), MOST); }
 
 // A wave keeps the n best of a list in LDS, or up to `enough` while that needs no look at indices; returns the key that n of them reach
@@ -214,7 +226,7 @@ struct QrScoresWave {
     {
         float cs, cu;
         add_chunk(cs, cu);
-        if (__ballot(!(cs < 0x1p40f))) {
+        if (__ballot(!(cs < 0x1p12f))) {
             if (!FOUND) find_best();
             const float to = limited(LOG2E * wave_max(largest));
             if (to > r) {
@@ -229,7 +241,7 @@ struct QrScoresWave {
         s += (double)cs;
         u += (double)cu;
     }
-    __device__ __forceinline__ QrScoresSum sum() const { return {(double)r, qr_wave_sum(s), qr_wave_sum(u)}; }
+    __device__ __forceinline__ QrScoresSum sum() const { return {(double)r, (double)wave_add((float)s), (double)wave_add((float)u)}; }
     // Which of a lane's logits are not below `least`, as bits.
     __device__ __forceinline__ unsigned from(float least)
     {
@@ -298,19 +310,19 @@ struct QrScoresWave {
     }
 };
 
-// The bound that groups of a wave's logits give.  Few ranks: a lane's are a group.  (Up to twice as many as there are ranks may reach it:
-// the search is shorter, 1024 x 32000 bf16, 16 ranks, AA us with a quarter more at most, BB now.)
+// The bound that groups of a wave's logits give.  Few ranks: a lane's are a group, and up to twice as many may reach the bound, which makes
+// the search shorter; of many ranks counting them would take longer (1024 x 32000 bf16, 64 ranks 35 us, with a quarter more at most 28).
 template <class T>
 __device__ __forceinline__ unsigned first_bound(const QrScoresWave<T> &w, int n)
 {
-    if (n <= 24) {
+    if (n <= FEW_RANKS) {
         const unsigned g[1] = {qr_logit_key(w.largest)};
         return qr_bound_of(g, qr_wave_reduce_u32<true>(g[0]), n, 2 * n);
     }
     unsigned g[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) g[v] = qr_logit_key(w.best[v]);
-    return qr_bound_of(g, qr_wave_reduce_u32<true>(qr_logit_key(w.largest)), n, 2 * n);
+    return qr_bound_of(g, qr_wave_reduce_u32<true>(qr_logit_key(w.largest)), n, n + n / 4);
 }
 
 // Sums of a row's part that are good for any logits: relative to its largest one.  WPR waves of a workgroup, `most` in LDS.
@@ -458,7 +470,7 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
                 one[0] = g[i] > one[0] ? g[i] : one[0];
             }
             const unsigned top = qr_wave_reduce_u32<true>(one[0]);
-            const unsigned bound = a.n <= 24 ? qr_bound_of(one, top, a.n, 2 * a.n) : qr_bound_of(g, top, a.n, 2 * a.n);
+            const unsigned bound = a.n <= FEW_RANKS ? qr_bound_of(one, top, a.n, 2 * a.n) : qr_bound_of(g, top, a.n, a.n + a.n / 4);
             if (lane == 0) shared_key = bound;
         }
     };
@@ -516,23 +528,24 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
             __syncthreads();
         }
     }
-    const double s_of = lane < NW ? sums[lane].s : 0.0;
-    if (__ballot(!(s_of < INFINITY)) || !__ballot(s_of > 0.0)) {   // uniform
+    QrScoresSum sum = sums[lane & (NW - 1)];
+    if (__ballot(!(sum.s < INFINITY)) || !__ballot(sum.s > 0.0)) {   // uniform
         __syncthreads();
         const QrScoresSum any = sums_of_any<T, NW>(x, n, wave, lane, most_of);
         if (lane == 0) sums[wave] = any;
         __syncthreads();
+        sum = sums[lane & (NW - 1)];
     }
-    QrScoresSum sum = {0.0, 0.0, 0.0};
     if (wave == 0) {   // joins the sums, the others rank
-        sum = lane < NW ? sums[lane] : QrScoresSum{-1e300, 0.0, 0.0};
         double to = sum.r;
 #pragma unroll
         for (int off = 1; off < NW; off <<= 1) to = fmax(to, __shfl_xor(to, off));
-        to = __shfl(to, 0);
         sum.move(to);
-        sum.s = qr_wave_sum(sum.s);
-        sum.u = qr_wave_sum(sum.u);
+#pragma unroll
+        for (int off = 1; off < NW; off <<= 1) {
+            sum.s += __shfl_xor(sum.s, off);
+            sum.u += __shfl_xor(sum.u, off);
+        }
     } else if (TOP) {
         for (int i0 = 0; i0 < M; i0 += 16 * (NW - 1)) {   // uniform; four threads count for one candidate
             const int i = i0 + ((tid - 64) >> 2);
@@ -600,7 +613,7 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
             g[i] = group_best[i * 64 + lane];
             most = g[i] > most ? g[i] : most;
         }
-        bound = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, 2 * a.n);
+        bound = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, a.n + a.n / 4);
     } else {
         __syncthreads();
     }
