@@ -235,7 +235,8 @@ qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const i
  * qrnnt_mx4_pitch(cols) = 16 ceil(cols/32)); its scales are bytes at a pitch of ld_scale (a multiple of 8, at least
  * qrnnt_mx4_scale_pitch(cols) = ceil(cols/32) rounded up to 8).  Codes start on 16-byte boundaries, scales on 8-byte ones.
  * Both pitches are 0 for a number of columns below 1 or above 2^30.  QRNNT_ERR_UNSUPPORTED: more than 2^31 - 1 rows or 2^30
- * columns to quantize, 2^28 rows or tokens or QRNNT_MX4_MAX_COLS columns of a linear layer, matrices of more than 2^60 elements. */
+ * columns to quantize, 2^28 rows or tokens, QRNNT_MX4_MAX_COLS columns or 2^36 weights of a linear layer, matrices of more than
+ * 2^60 elements. */
 #define QRNNT_MX4_MAX_COLS (1 << 20)
 int32_t qrnnt_mx4_pitch(int32_t cols);
 int32_t qrnnt_mx4_scale_pitch(int32_t cols);
@@ -269,7 +270,8 @@ typedef struct {
 } qrnnt_mx4;
 
 /* y[m,r] = sum_k value_w[r,k] * value_a[m,k] + bias[r], summed in fp32 and rounded once to y_dtype.  Products are exact; a matrix
- * instruction adds 128 of them to a sum at a time, which rounds by at most 2^-23 of the largest magnitude in it.  The order of the
+ * instruction adds 128 of them to a sum at a time, all cut at 2^-27 of the largest magnitude among them and rounded once: by less
+ * than 2^-19 of that largest one in all (not at all where they lie within 2^27 of each other and of the sum).  The order of the
  * sums depends on the sizes of the call, not on its data.  A row of a or w with a NaN scale gives NaN.
  * a, a_scale [device]: M rows as qrnnt_quantize_mx4 writes them.  The codes behind column cols and the bytes behind the row may hold
  * anything, the scales from ceil(cols/32) up to qrnnt_mx4_scale_pitch(cols) anything but 255.  bias [device] fp32 [rows] or

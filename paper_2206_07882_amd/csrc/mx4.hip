@@ -205,7 +205,8 @@ extern "C" qrnnt_status qrnnt_dequantize_mx4(const uint8_t *q, int32_t ld_q, con
 
 extern "C" size_t qrnnt_pack_mx4_bytes(int32_t rows, int32_t cols)
 {
-    return rows > 0 && cols > 0 && rows <= 1 << 28 && cols <= QRNNT_MX4_MAX_COLS ? qr_mx4_packed_bytes(rows, cols) : 0;
+    if (rows <= 0 || cols <= 0 || rows > 1 << 28 || cols > QRNNT_MX4_MAX_COLS) return 0;
+    return qr_mx4_tiles(rows, cols) <= 1 << 24 ? qr_mx4_packed_bytes(rows, cols) : 0;   // (a grid has less than 2^32 threads)
 }
 
 extern "C" qrnnt_status qrnnt_pack_mx4(const uint8_t *q, int32_t ld_q, const uint8_t *scale, int32_t ld_scale, int32_t rows,
@@ -217,7 +218,6 @@ extern "C" qrnnt_status qrnnt_pack_mx4(const uint8_t *q, int32_t ld_q, const uin
     QR_REQUIRE(ld_q >= qr_mx4_pitch(cols) && ld_q % 16 == 0 && ld_scale >= qr_mx4_blocks(cols), QRNNT_ERR_SHAPE);
     QR_REQUIRE(qr_aligned(q, 16) && qr_aligned(packed_out, 16), QRNNT_ERR_ALIGN);
     QrMx4Pack a = {q, scale, ld_q, ld_scale, rows, cols, qr_mx4_blocks(cols), qr_mx4_chunks(cols), (uint8_t *)packed_out, qr_mx4_tiles(rows, cols)};
-    QR_REQUIRE(a.tiles <= 1 << 24, QRNNT_ERR_UNSUPPORTED);   // (a grid has less than 2^32 threads)
     pack_mx4_kernel<<<(unsigned)((a.tiles * 128 + 255) / 256), 256, 0, (hipStream_t)stream>>>(a);
     return qr_launch_status();
 }

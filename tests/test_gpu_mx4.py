@@ -133,6 +133,7 @@ def run(q, M, N, K, dtype, seed, bias=True, low=126, high=128, **more):
 
 
 def assert_same(y, ref, b, dtype):
+    """Held to the last bit: magnitudes below 2^20 and multiples of 2^-4 lie within 2^27 of each other."""
     r = torch.from_numpy(ref.astype(np.float32))   # exact
     r = (r if b is None else r + b.cpu()).to(dtype)
     assert torch.equal(y.cpu(), r)
@@ -188,12 +189,10 @@ def test_codes_at_wide_pitches_with_anything_behind_them(gpu_lib, M, N, K):
 @pytest.mark.parametrize("M,N,K", [(8, 50, 640), (200, 150, 1000), (500, 600, 2000), (130, 64, 6000)])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_linear_with_scales_far_apart(gpu_lib, M, N, K, dtype):
-    """Every instruction rounds its sum by at most 2^-23 of the largest magnitude in it, which the sum of magnitudes bounds; a row has
-    2 ceil(K / 256) of them, up to 8 partial sums are joined, the bias is added: each at most half a step."""
+    """The sums are off by plain.sum_tolerance, the bias costs half a step of fp32 and the result half a step of its type."""
     y, ref, mag, b = run(gpu_lib, M, N, K, dtype, 9, low=117, high=130)
     want = ref + b.double().cpu().numpy()
-    steps = 2 * ((K + 255) // 256) + 8
-    bound = steps * 2.0 ** -23 * (mag + np.abs(want)) + (np.abs(want) * HALF_STEP[dtype] + float(torch.finfo(dtype).smallest_normal) * 2.0 ** -9) * (1 + 2.0 ** -10)
+    bound = plain.sum_tolerance(K, mag) + 2.0 ** -24 * np.abs(want) + (np.abs(want) * HALF_STEP[dtype] + float(torch.finfo(dtype).smallest_normal) * 2.0 ** -9) * (1 + 2.0 ** -10)
     got = y.double().cpu().numpy()
     if dtype == torch.float16:   # beyond its range
         far = np.abs(want) > 65000
@@ -249,3 +248,24 @@ def test_a_workspace_for_many_tokens_serves_fewer(gpu_lib):
         a, sa = codes_of(M, M, K)
         y = q.linear_mx4(mat, dev(plain.join(a)), dev(sa), workspace=ws)
         assert_same(y, exact(a, sa, K) @ exact(w, sw, K).T, None, torch.float32)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 20, 384), (70, 100, 384), (300, 300, 640)])
+def test_sums_of_one_large_and_many_small_products(gpu_lib, M, N, K):
+    """The first block's scale makes its products larger than the others by up to 2^44: what is cut off stays within the bound."""
+    q = gpu_lib
+    for d in (20, 27, 28, 31, 44):
+        code = np.full((M, (K + 31) // 32 * 32), 3, np.uint8)   # 1.5
+        code[:, 1:32] = 0
+        scale = np.full((M, (K + 255) // 256 * 8), 127, np.uint8)
+        scale[:, 0] = 127 + d // 2
+        w, sw = np.resize(code[:1], (N, code.shape[1])).copy(), np.resize(scale[:1], (N, scale.shape[1])).copy()
+        w[1::2, 32:] |= 8   # every second row's small products are negative
+        dev = lambda x: torch.from_numpy(x).to(DEV)
+        y = q.linear_mx4(q.pack_mx4(dev(plain.join(w)), dev(sw), K), dev(plain.join(code)), dev(scale)).double().cpu().numpy()
+        a, b = exact(code, scale, K), exact(w, sw, K)
+        want, largest = a @ b.T, (np.abs(a[:, 0])[:, None] * np.abs(b[:, 0])[None, :])
+        steps = 2 * ((K + 255) // 256)
+        assert (np.abs(y - want) <= steps * 2.0 ** -19 * (largest + np.abs(want))).all()
+        if d < 24:
+            assert np.array_equal(y, want.astype(np.float32))

@@ -60,9 +60,8 @@ def test_against_64_bits(gpu_lib, lists, length, H, V):
     w = plain.values(plain.split(r.w_codes.cpu().numpy()), r.w_scale.cpu().numpy()[:, :want_scale.shape[1]])
     a = plain.values(want, want_scale)
     y = a @ w.T + r.bias.double().cpu().numpy()
-    mag = np.abs(a) @ np.abs(w).T + np.abs(y)
-    steps = 2 * ((H + 255) // 256) + 8   # roundings of sums to fp32, as in the linear layer's own test
-    assert (np.abs(logits.double().numpy() - y) <= steps * 2.0 ** -23 * mag + np.abs(y) * HALF_STEP[r.dtype] * (1 + 2.0 ** -7)).all()
+    bound = plain.sum_tolerance(H, np.abs(a) @ np.abs(w).T) + 2.0 ** -24 * np.abs(y)   # (the bias)
+    assert (np.abs(logits.double().numpy() - y) <= bound + (np.abs(y) + bound) * HALF_STEP[r.dtype]).all()
     lp, ent, tok, val = plain.scores(logits.double().numpy(), r.token.cpu().numpy(), r.n)
     lse, bound = plain.scores_tolerance(V)
     assert (np.abs(logp.numpy() - lp) <= lse + np.abs(lp) * 2.0 ** -24).all()
