@@ -96,15 +96,21 @@ template <class T>
 struct QrChunk {
     static constexpr int V = QrVec<T>::N, LEN = 256 * V, PER = 4 * V;
     v4i raw[4];
+    // Whether any lane's vector v holds one of n logits (v = 0: as if it did).
+    static __device__ __forceinline__ bool holds(int v, int n) { return v == 0 || v * 64 * V < n; }
     __device__ __forceinline__ void load(const T *x, int n, int lane)
     {
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int c = (v * 64 + lane) * V;
+            typename QrVec<T>::type u;
+#pragma unroll
+            for (int i = 0; i < V; ++i) u[i] = (T)-INFINITY;
+            raw[v] = __builtin_bit_cast(v4i, u);
+            if (!holds(v, n)) continue;   // uniform
             if (c + V <= n) {
                 raw[v] = __builtin_bit_cast(v4i, *(const typename QrVec<T>::any *)(x + c));
-            } else {
-                typename QrVec<T>::type u;
+            } else if (c < n) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) u[i] = c + i < n ? x[c + i] : (T)-INFINITY;
                 raw[v] = __builtin_bit_cast(v4i, u);
@@ -198,11 +204,14 @@ struct QrScoresWave {
     float r = -MOST;
     double s = 0.0, u = 0.0;
 
-    __device__ __forceinline__ void find_best()
+    // n: logits from the chunk's start on
+    __device__ __forceinline__ void find_best(int n)
     {
         now.fresh();
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
+            best[v] = -INFINITY;
+            if (!QrChunk<T>::holds(v, n)) continue;   // uniform
             best[v] = now.at(v * V);
 #pragma unroll
             for (int i = 1; i < V; ++i) best[v] = fmaxf(best[v], now.at(v * V + i));
@@ -210,24 +219,28 @@ struct QrScoresWave {
         largest = fmaxf(-INFINITY, fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])));
     }
     __device__ __forceinline__ void start() { r = limited(LOG2E * wave_max(largest)); }
-    __device__ __forceinline__ void add_chunk(float &cs, float &cu)
+    __device__ __forceinline__ void add_chunk(int n, float &cs, float &cu)
     {
         cs = cu = 0.0f;
         now.fresh();
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const float d = fmaf(now.at(i), LOG2E, -r), e = __builtin_amdgcn_exp2f(d);
-            cs += e;
-            cu = fmaf(e, fmaxf(d, FAR), cu);
+        for (int v = 0; v < 4; ++v) {
+            if (!QrChunk<T>::holds(v, n)) continue;   // uniform
+#pragma unroll
+            for (int i = v * V; i < (v + 1) * V; ++i) {
+                const float d = fmaf(now.at(i), LOG2E, -r), e = __builtin_amdgcn_exp2f(d);
+                cs += e;
+                cu = fmaf(e, fmaxf(d, FAR), cu);
+            }
         }
     }
     template <bool FOUND>
-    __device__ __forceinline__ void add()
+    __device__ __forceinline__ void add(int n)
     {
         float cs, cu;
-        add_chunk(cs, cu);
+        add_chunk(n, cs, cu);
         if (__ballot(!(cs < 0x1p12f))) {
-            if (!FOUND) find_best();
+            if (!FOUND) find_best(n);
             const float to = limited(LOG2E * wave_max(largest));
             if (to > r) {
                 QrScoresSum moved = {(double)r, s, u};
@@ -235,7 +248,7 @@ struct QrScoresWave {
                 r = to;
                 s = moved.s;
                 u = moved.u;
-                add_chunk(cs, cu);
+                add_chunk(n, cs, cu);
             }
         }
         s += (double)cs;
@@ -378,9 +391,9 @@ __global__ __launch_bounds__(256, TOP ? 8 : 4) void scores_wave_kernel(const QrS
         const bool more = n - at > LEN;
         QrChunk<T> next;
         if (more) next.load(x + at + LEN, n - at - LEN, lane);
-        if (TOP || at == 0) w.find_best();
+        if (TOP || at == 0) w.find_best(n - at);
         if (at == 0) w.start();
-        w.template add<TOP>();
+        w.template add<TOP>(n - at);
         if (TOP) {
             if (at == 0) key = first_bound(w, a.n);
             w.hits_to(list, count, key, a.n, x + at, at, lane);
@@ -418,7 +431,7 @@ __device__ __attribute__((noinline)) QrCand best_of_any(const T *x, int len, int
     unsigned key = 0u;
     for (int at = wave * QrChunk<T>::LEN; at < len; at += NW * QrChunk<T>::LEN) {
         w.now.load(x + at, len - at, lane);
-        w.find_best();
+        w.find_best(len - at);
         w.hits_to(list, count, key, n, x + at, first + at, lane);
     }
     if (count > n) keep_best<CAP>(list, count, n, n, lane);
@@ -484,10 +497,10 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         const int mine = at + wave * LEN;
         QrChunk<T> next;
         if (more) next.load(x + mine + BLOCK, n - mine - BLOCK, lane);
-        if (TOP || at == 0) w.find_best();
+        if (TOP || at == 0) w.find_best(n - mine);
         if (at == 0) w.start();
         if (TOP && at == 0) find_bound(qr_logit_key(w.largest));   // (the other waves add up in the meantime)
-        w.template add<TOP>();
+        w.template add<TOP>(n - mine);
         if (TOP && !over) {
             __syncthreads();
             w.hits(least_of(shared_key), x + mine, lane, [&](float f, int i) { push(qr_cand(qr_float_key(f + 0.0f), first + mine + i)); });
@@ -636,13 +649,13 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
 // Waves to a row, and parts of it.  A wave reads CHUNK = 256 vectors at a time, a workgroup of 16 waves 16 times as many.
 // Measured (us; 1 / 4 / 8 / 16 waves), 16 alternatives: 1024 x 32000 bf16 36.9 / 25.8 / 22.6 / 24.2, 4096 x 32000 68 / 68 / 62 / 78, 8192 x 32000 125 /
 // 133 / 124 / 154, 256 x 8000 15.7 / 5.8 / 6.9 / 8.7, 256 x 131072 fp32 136 / 72 / 43 / 31, 4096 x 2500 fp32 14.6 / 17.7 / 28 / 54; none: 1024 x
-// 32000 bf16 14.8 / 14.9 / 15.1 / 16.0.  In parts, with another launch that joins them (1 / 4 / 8 / 16 of them): 1 x 131072 fp32 17.7 / 11.3 / 9.2 /
+// 32000 bf16 18.9 / 14.9 / 15.1 / 16.0, 4096 x 32000 43.1 / 43.4 / 42.2 / 49.2.  In parts, with another launch that joins them (1 / 4 / 8 / 16 of them): 1 x 131072 fp32 17.7 / 11.3 / 9.2 /
 // 9.7, 16 x 262144 fp32 39 / 25 / 21 / 18, 64 x 131072 fp32 24.5 / 16.3 / 16.6 / 16.5; a row of two pieces of 16 waves, 1 x 32000 fp32, 7.6 whole, 8.7.
 constexpr int FEW_ROWS = 256, STRETCH = 16384;   // (the shortest that a workgroup of 16 waves reads at a time)
 void plan_scores(int rows, int V, int n, int chunk, int &waves, int &n_parts, int &part)
 {
     const int chunks = (V + chunk - 1) / chunk;
-    if (chunks == 1 || rows >= 8192 || (chunks <= 3 && rows >= 2048) || (n == 0 && rows >= 1024)) waves = 1;
+    if (chunks == 1 || rows >= 8192 || (chunks <= 3 && rows >= 2048) || (n == 0 && rows >= 4096)) waves = 1;
     else waves = chunks <= 6 ? 4 : chunks <= 24 ? 8 : 16;
     n_parts = 1;
     const int pieces = (chunks + 15) / 16;

@@ -463,12 +463,26 @@ def mx4_scale_pitch(cols: int) -> int:
 def _mx4(codes: torch.Tensor, scale: torch.Tensor, rows: int, cols: int):
     """(address and pitch of the codes, address and pitch of the scales) of [rows, cols] values."""
     width, n_scale = (cols + 31) // 32 * 16, (cols + 255) // 256 * 8
-    wide, wide_s = codes.shape[-1], scale.shape[-1]
-    pq, ld_q = _matrix(codes, torch.uint8, rows, wide)
-    ps, ld_s = _matrix(scale, torch.uint8, rows, wide_s)
-    if wide < width or wide_s < n_scale:
-        raise ValueError(f"rows of {cols} columns take {width} bytes of codes and {n_scale} scales, got {wide} and {wide_s}")
-    return (pq, ld_q, ps, ld_s) if rows > 1 else (pq, width, ps, n_scale)
+    if codes.dtype is not torch.uint8 or scale.dtype is not torch.uint8:
+        raise TypeError(f"expected torch.uint8, got {codes.dtype} and {scale.dtype}")
+    n, wide = codes.shape
+    n_s, wide_s = scale.shape
+    if n != rows or n_s != rows or wide < width or wide_s < n_scale:
+        raise ValueError(f"{rows} rows of {cols} columns take {width} bytes of codes and {n_scale} scales each, got {tuple(codes.shape)} and {tuple(scale.shape)}")
+    if rows <= 1:   # (whatever pitch a single row's view has)
+        width, n_scale = max(width, 16), max(n_scale, 8)
+        if rows == 1 and (codes.stride(1) != 1 or scale.stride(1) != 1):
+            raise ValueError("the elements of a row must be contiguous")
+        return codes.data_ptr(), width, scale.data_ptr(), n_scale
+    ld_q, step = codes.stride()
+    ld_s, step_s = scale.stride()
+    if step != 1 or step_s != 1:
+        raise ValueError("the elements of a row must be contiguous")
+    if ld_q < wide or ld_s < wide_s:
+        raise ValueError("rows must not overlap")
+    if rows > _INT_MAX or ld_q > _INT_MAX or ld_s > _INT_MAX:   # (ctypes would drop the upper bits)
+        raise ValueError(f"a matrix of {rows} rows, pitches {ld_q} and {ld_s}, is too large")
+    return codes.data_ptr(), ld_q, scale.data_ptr(), ld_s
 
 
 def quantize_mx4(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):

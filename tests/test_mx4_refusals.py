@@ -129,3 +129,23 @@ def test_wrappers_refuse_tensors_that_are_not_on_the_gpu():
             call()
     with pytest.raises(ValueError):
         qrnnt.linear_mx4_workspace(m, 1 << 32)
+
+
+def test_wrappers_refuse_codes_of_other_shapes_and_types():
+    u8 = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    ok = qrnnt._mx4(u8(4, 32), u8(4, 8), 4, 40)
+    assert ok[1] == 32 and ok[3] == 8
+    assert qrnnt._mx4(u8(1, 32), u8(1, 8), 1, 40)[1::2] == (32, 8) and qrnnt._mx4(u8(0, 32), u8(0, 8), 0, 40)[1::2] == (32, 8)
+    assert qrnnt._mx4(u8(4, 64)[:, :32], u8(4, 24)[:, :8], 4, 40)[1::2] == (64, 24)
+    assert qrnnt._mx4(u8(2, 3, 64)[:1, 0], u8(3, 24)[1:2, :8], 1, 40)[1::2] == (32, 8)
+    for codes, scale in ((u8(4, 31), u8(4, 8)), (u8(4, 32), u8(4, 7)), (u8(3, 32), u8(4, 8)), (u8(4, 32), u8(5, 8)), (u8(4, 64)[:, ::2], u8(4, 8)),
+                         (u8(4, 32), u8(4, 16)[:, ::2]), (u8(32, 4).t(), u8(4, 8)), (u8(1, 32).expand(4, 32), u8(4, 8)), (u8(1, 64)[:, ::2], u8(1, 8))):
+        with pytest.raises(ValueError):
+            qrnnt._mx4(codes, scale, codes.shape[0] if codes.shape[0] == 1 else 4, 40)
+    for codes, scale in ((u8(4, 32).to(torch.int8), u8(4, 8)), (u8(4, 32), u8(4, 8).to(torch.int8))):
+        with pytest.raises(TypeError):
+            qrnnt._mx4(codes, scale, 4, 40)
+    far = lambda rows, cols, pitch: torch.empty_strided((rows, cols), (pitch, 1), dtype=torch.uint8, device="meta")
+    for codes, scale, rows in ((far(2, 32, 1 << 31), far(2, 8, 8), 2), (far(2, 32, 32), far(2, 8, 1 << 31), 2), (far(1 << 31, 32, 32), far(1 << 31, 8, 8), 1 << 31)):
+        with pytest.raises(ValueError):
+            qrnnt._mx4(codes, scale, rows, 40)
