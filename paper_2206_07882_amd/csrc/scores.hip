@@ -594,56 +594,71 @@ template <class T>
 __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrScoresArgs a)
 {
     __shared__ unsigned group_best[256];
-    __shared__ QrCand all[64 * MAX_PARTS];
+    __shared__ QrCand all[64 * MAX_PARTS], ranked[MAX_TOP];
     __shared__ int n_all;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = blockIdx.x;
     QrCand mine = tid < a.n_parts * a.n ? a.cands[row * a.n_parts * a.n + tid] : 0ull;
     QrScoresToken token;
-    token.load<T>(a, row);
-    // (the r of a part that holds no finite logit, 0, may be above the others': it counts only where there is something to it)
-    QrScoresSum sum = lane < a.n_parts ? a.heads[row * a.n_parts + lane] : QrScoresSum{0.0, 0.0, 0.0};
-    const bool some = sum.s != 0.0;
-    double to = some ? sum.r : -1e300;
-    for (int off = 1; off < MAX_PARTS; off <<= 1) to = fmax(to, __shfl_xor(to, off));
-    to = __shfl(to, 0);
-    if (some) sum.move(to);
-    sum = {to, qr_wave_sum(sum.s), qr_wave_sum(sum.u)};
-    const QrScoresRow values(sum);
-    if (tid == 0) {
-        n_all = 0;
-        values.write(a, row, token);
+    QrScoresSum sum = {0.0, 0.0, 0.0};
+    if (wave == 0) {
+        token.load<T>(a, row);
+        const int part = lane & (MAX_PARTS - 1);   // (every sixteen lanes do the same)
+        if (part < a.n_parts) sum = a.heads[row * a.n_parts + part];
     }
-    if (a.n == 0) return;
-    unsigned bound = 1u;
-    if (a.n_parts * a.n > 256) {   // (ranks of fewer are counted in less time than a bound takes)
-        const unsigned four = qr_quad_max((unsigned)(mine >> 32));
-        if ((lane & 3) == 0) group_best[tid >> 2] = four;
-        __syncthreads();
-        unsigned g[4], most = 0u;
+    if (a.n > 0) {
+        if (tid == 0) n_all = 0;
+        if (tid < MAX_TOP) ranked[tid] = 0ull;
+        unsigned bound = 1u;
+        if (a.n_parts * a.n > 256) {   // (ranks of fewer are counted in less time than a bound takes)
+            const unsigned four = qr_quad_max((unsigned)(mine >> 32));
+            if ((lane & 3) == 0) group_best[tid >> 2] = four;
+            __syncthreads();
+            unsigned g[4], most = 0u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            g[i] = group_best[i * 64 + lane];
-            most = g[i] > most ? g[i] : most;
+            for (int i = 0; i < 4; ++i) {
+                g[i] = group_best[i * 64 + lane];
+                most = g[i] > most ? g[i] : most;
+            }
+            bound = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, a.n + a.n / 4);
+        } else {
+            __syncthreads();
         }
-        bound = qr_bound_of(g, qr_wave_reduce_u32<true>(most), a.n, a.n + a.n / 4);
-    } else {
+        if (mine != 0ull && (unsigned)(mine >> 32) >= bound) all[atomicAdd(&n_all, 1)] = mine;
         __syncthreads();
     }
-    if (mine != 0ull && (unsigned)(mine >> 32) >= bound) all[atomicAdd(&n_all, 1)] = mine;
-    __syncthreads();
-    const int M = n_all;
-    for (int i0 = 0; i0 < M; i0 += 16 * MAX_PARTS) {   // uniform
-        const int i = i0 + (tid >> 2);
-        const QrCand c = all[i < M ? i : 0];
-        int rank = 0;
+    if (wave == 0) {   // joins the sums, the others rank
+        // (the r of a part that holds no finite logit, 0, may be above the others': it counts only where there is something to it)
+        const bool some = sum.s != 0.0;
+        double to = some ? sum.r : -1e300;
+#pragma unroll
+        for (int off = 1; off < MAX_PARTS; off <<= 1) to = fmax(to, __shfl_xor(to, off));
+        if (some) sum.move(to);
+        sum.r = to;
+#pragma unroll
+        for (int off = 1; off < MAX_PARTS; off <<= 1) {
+            sum.s += __shfl_xor(sum.s, off);
+            sum.u += __shfl_xor(sum.u, off);
+        }
+    } else if (a.n > 0) {
+        const int M = n_all;
+        for (int i0 = 0; i0 < M; i0 += 16 * (MAX_PARTS - 1)) {   // uniform; four threads count for one candidate
+            const int i = i0 + ((tid - 64) >> 2);
+            const QrCand c = all[i < M ? i : 0];
+            int rank = 0;
 #pragma unroll 8
-        for (int j = tid & 3; j < M; j += 4) rank += all[j] > c ? 1 : 0;
-        rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
-        rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
-        if ((tid & 3) == 0 && i < M && rank < a.n) values.write_rank(a, row, rank, c);
+            for (int j = tid & 3; j < M; j += 4) rank += all[j] > c ? 1 : 0;
+            rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
+            rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
+            if ((tid & 3) == 0 && i < M && rank < a.n) ranked[rank] = c;
+        }
     }
-    if (tid >= M && tid < a.n) values.write_rank(a, row, tid, 0ull);
+    const QrScoresRow values(sum);
+    if (tid == 0) values.write(a, row, token);
+    if (a.n > 0) {
+        __syncthreads();
+        if (tid < a.n) values.write_rank(a, row, tid, ranked[tid]);
+    }
 }
 
 // Waves to a row, and parts of it.  A wave reads CHUNK = 256 vectors at a time, a workgroup of 16 waves 16 times as many.
