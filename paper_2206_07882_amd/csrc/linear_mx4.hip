@@ -197,7 +197,8 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
             qr_load_lds4(src_s[j] + (size_t)kc * (at < P::SA_BLOCKS ? 128 : 8), __builtin_amdgcn_readfirstlane(to));
         }
     };
-    constexpr int A = P::A_LOADS, B = P::B_LOADS + P::S_LOADS, GROUP = B + 2 * A;   // loads of a wave: weights of a step, the rest of a chunk, all of it
+    // loads of a wave: weights of a step, the rest of a chunk, all of it
+    constexpr int A = P::A_LOADS, B = P::B_LOADS + P::S_LOADS, GROUP = B + 2 * A;
     static_assert((D - 1) * GROUP < 64, "the counter of loads has 6 bits");
     // Order of all loads: A(0), then for every chunk c: B(c), A(2c + 1), A(2c + 2).  Chunks up to D - 2 are on their way before the
     // loop; the two steps of chunk c start B(c + D - 1) and A(2(c + D) - 1), then A(2(c + D)).
@@ -480,7 +481,8 @@ struct QrTileCost {
     }
     int64_t tiles(int rows, int M) const { return (int64_t)((rows + size - 1) / size) * ((M + size - 1) / size); }
 };
-constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.31f, 0.56f, 0.78f, 0.12f, 2.1f}, {128, 512, 0.70f, 1.40f, 1.0f, 0.53f, 1.7f}, {256, 256, 1.14f, 1.89f, 4.0f, 0.70f, 1.7f}};
+constexpr QrTileCost TILE_COST[] = {{}, {64, 512, 0.31f, 0.56f, 0.78f, 0.12f, 2.1f}, {128, 512, 0.70f, 1.40f, 1.0f, 0.53f, 1.7f},
+                                    {256, 256, 1.14f, 1.89f, 4.0f, 0.70f, 1.7f}};
 
 // A sum of few columns is not cut, nor one whose parts' sums, read and written, pass 512 tokens x 128 rows for each chunk of it: so
 // what a call may need is known without its plan.
@@ -631,8 +633,8 @@ extern "C" qrnnt_status qrnnt_linear_mx4(const qrnnt_mx4 *w, const float *bias, 
     if (M == 0) return QRNNT_OK;
     QR_REQUIRE(a != nullptr && a_scale != nullptr && y != nullptr, QRNNT_ERR_NULL);
     const size_t need = qrnnt_linear_mx4_workspace(w, M);
-    QR_REQUIRE(qr_aligned(w->packed, 16) && qr_aligned(a, 16) && qr_aligned(a_scale, 8) && qr_aligned(y, qr_dtype_size(y_dtype)) && qr_aligned(bias, 4),
-               QRNNT_ERR_ALIGN);
+    QR_REQUIRE(qr_aligned(w->packed, 16) && qr_aligned(a, 16) && qr_aligned(a_scale, 8) && qr_aligned(y, qr_dtype_size(y_dtype)) &&
+                   qr_aligned(bias, 4), QRNNT_ERR_ALIGN);
     QR_REQUIRE(need == 0 || workspace != nullptr, QRNNT_ERR_NULL);
     QR_REQUIRE(need == 0 || qr_aligned(workspace, 256), QRNNT_ERR_ALIGN);
     QR_REQUIRE(workspace_bytes >= need, QRNNT_ERR_WORKSPACE);
@@ -642,7 +644,8 @@ extern "C" qrnnt_status qrnnt_linear_mx4(const qrnnt_mx4 *w, const float *bias, 
     p.a = a;  p.s_a = a_scale;  p.ld_a = ld_a;  p.ld_sa = ld_scale;  p.M = M;  p.y = y;  p.ld_y = ld_y;
     p.part = workspace;  p.ld_part = qr_round_up(w->rows, 4) / 4;
     const QrMx4Plan plan = plan_linear(w->rows, w->cols, M, (int)qr_dtype_size(y_dtype));
-    QR_REQUIRE(plan.piece[0].kind == FEW || TILE_COST[plan.piece[0].kind].tiles(w->rows, M) < 1 << 23, QRNNT_ERR_UNSUPPORTED);   // (a grid has less than 2^32 threads)
+    // (a grid has less than 2^32 threads)
+    QR_REQUIRE(plan.piece[0].kind == FEW || TILE_COST[plan.piece[0].kind].tiles(w->rows, M) < 1 << 23, QRNNT_ERR_UNSUPPORTED);
     if (y_dtype == QRNNT_F32) launch_linear<float>(p, plan, (hipStream_t)stream);
     else if (y_dtype == QRNNT_F16) launch_linear<_Float16>(p, plan, (hipStream_t)stream);
     else launch_linear<__bf16>(p, plan, (hipStream_t)stream);

@@ -3,8 +3,8 @@
 //
 // With S = sum 2^(x L - r), U = sum 2^(x L - r)(x L - r), L = log2(e), for any r:  log P(x) = ln 2 (x L - r) - log S,
 // entropy = log S - ln 2 U / S.  A wave takes the largest logit of the first that it reads for r, a product, a sum, an exponential and
-// two more sums a logit then do; where a logit passes r by far (a sum of 2^12) sums move to a larger one.  Lanes add up at the end of the row, in fp32.
-// Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read again, with x - max
+// two more sums a logit then do; where a logit passes r by far (a sum of 2^12) sums move to a larger one.  Lanes add up at the end of
+// the row, in fp32.  Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read again, with x - max
 // formed first.
 //
 // The best alternatives: the n-th largest of groups of the logits that are read first bounds the n-th best from below.  What reaches the
@@ -134,8 +134,12 @@ struct QrChunk {
 
 typedef __attribute__((address_space(3))) QrCand *QrLdsList;   // (for functions that are not inlined)
 
-__device__ __forceinline__ int lanes_below(unsigned long long m) { return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u)); }
-__device__ __forceinline__ float least_of(unsigned key) { return key > 0x00800000u ? qr_key_float(key) : -FLT_MAX; }   // (keys up to there are those of -inf and below)
+__device__ __forceinline__ int lanes_below(unsigned long long m)
+{
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u));
+}
+// (keys up to there are those of -inf and below)
+__device__ __forceinline__ float least_of(unsigned key) { return key > 0x00800000u ? qr_key_float(key) : -FLT_MAX; }
 __device__ __forceinline__ float wave_max(float v) { return qr_key_float(qr_wave_reduce_u32<true>(qr_float_key(v))); }   // (v is not NaN)
 __device__ __forceinline__ float wave_add(float v)   // in all lanes: within rows of 16, then over the rows
 {
@@ -439,6 +443,9 @@ __device__ __attribute__((noinline)) QrCand best_of_any(const T *x, int len, int
 }
 
 // A workgroup of NW waves to a row or a part of one.  Grid: x = part of a row, y (and z) = row.
+// Bound by a chain, not by memory: load, largest logit, bound, sums, list, ranks, one workgroup behind the other at each place on the
+// device (1024 x 32000 bf16, 65.5 MB, 16 alternatives 23 us; without alternatives 15, 4.4 TB/s).  What the waves do on the chain is
+// shared out: one searches the bound while the others add up, one joins the sums while the others rank.
 template <class T, int NW, bool TOP>
 __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScoresArgs a)
 {
@@ -589,7 +596,8 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
     }
 }
 
-// Rows that were cut: joins the parts' sums and lists.  Grid: one workgroup a row; a candidate to a thread.
+// Rows that were cut: joins the parts' sums and lists.  Grid: one workgroup a row; a candidate to a thread.  Bound by latency: 3.9 us of the
+// 15 of 64 x 131072 fp32 with 20 alternatives (4.7 before one wave joined the sums while the others rank).
 template <class T>
 __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrScoresArgs a)
 {
@@ -662,10 +670,11 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
 }
 
 // Waves to a row, and parts of it.  A wave reads CHUNK = 256 vectors at a time, a workgroup of 16 waves 16 times as many.
-// Measured (us; 1 / 4 / 8 / 16 waves), 16 alternatives: 1024 x 32000 bf16 36.9 / 25.8 / 22.6 / 24.2, 4096 x 32000 68 / 68 / 62 / 78, 8192 x 32000 125 /
-// 133 / 124 / 154, 256 x 8000 15.7 / 5.8 / 6.9 / 8.7, 256 x 131072 fp32 136 / 72 / 43 / 31, 4096 x 2500 fp32 14.6 / 17.7 / 28 / 54; none: 1024 x
-// 32000 bf16 18.9 / 14.9 / 15.1 / 16.0, 4096 x 32000 43.1 / 43.4 / 42.2 / 49.2.  In parts, with another launch that joins them (1 / 4 / 8 / 16 of them): 1 x 131072 fp32 17.7 / 11.3 / 9.2 /
-// 9.7, 16 x 262144 fp32 39 / 25 / 21 / 18, 64 x 131072 fp32 24.5 / 16.3 / 16.6 / 16.5; a row of two pieces of 16 waves, 1 x 32000 fp32, 7.6 whole, 8.7.
+// Measured (us; 1 / 4 / 8 / 16 waves), 16 alternatives: 1024 x 32000 bf16 36.9 / 25.8 / 22.6 / 24.2, 4096 x 32000 68 / 68 / 62 / 78, 8192 x
+// 32000 125 / 133 / 124 / 154, 256 x 8000 15.7 / 5.8 / 6.9 / 8.7, 256 x 131072 fp32 136 / 72 / 43 / 31, 4096 x 2500 fp32 14.6 / 17.7 / 28 /
+// 54; none: 1024 x 32000 bf16 18.9 / 14.9 / 15.1 / 16.0, 4096 x 32000 43.1 / 43.4 / 42.2 / 49.2.  In parts, with another launch that
+// joins them (1 / 4 / 8 / 16 of them): 1 x 131072 fp32 17.7 / 11.3 / 9.2 / 9.7, 16 x 262144 fp32 39 / 25 / 21 / 18, 64 x 131072 fp32 24.5 /
+// 16.3 / 16.6 / 16.5; a row of two pieces of 16 waves, 1 x 32000 fp32, 7.6 whole, 8.7 in two.
 constexpr int FEW_ROWS = 256, STRETCH = 16384;   // (the shortest that a workgroup of 16 waves reads at a time)
 void plan_scores(int rows, int V, int n, int chunk, int &waves, int &n_parts, int &part)
 {
