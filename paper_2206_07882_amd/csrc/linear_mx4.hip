@@ -573,7 +573,7 @@ void launch_few(const QrMx4Linear &p, hipStream_t st)
 }
 
 template <class T>
-void launch_piece(const QrMx4Linear &p, const QrMx4Piece &piece, hipStream_t st)
+void launch_piece(const QrMx4Linear &p, const QrMx4Piece &piece, bool past, hipStream_t st)
 {
     switch (piece.kind) {
     case FEW:
@@ -598,7 +598,7 @@ void launch_piece(const QrMx4Linear &p, const QrMx4Piece &piece, hipStream_t st)
         return;
     case MIDDLE: launch_tiles<T, 4, 4, 2, 2, 2>(p, 1, st); return;
     case LARGE:
-        if ((int64_t)p.M * p.rows * (int)sizeof(T) > LAST_CACHE) launch_tiles<T, 8, 4, 2, 4, 2, true>(p, 1, st);
+        if (past) launch_tiles<T, 8, 4, 2, 4, 2, true>(p, 1, st);
         else launch_tiles<T, 8, 4, 2, 4, 2>(p, 1, st);
         return;
     }
@@ -607,9 +607,10 @@ void launch_piece(const QrMx4Linear &p, const QrMx4Piece &piece, hipStream_t st)
 template <class T>
 void launch_linear(QrMx4Linear p, const QrMx4Plan &plan, hipStream_t st)
 {
+    const bool past = (int64_t)p.M * p.rows * (int)sizeof(T) > LAST_CACHE;
     for (int i = 0; i < plan.n; ++i) {
         p.M = plan.piece[i].M;
-        launch_piece<T>(p, plan.piece[i], st);
+        launch_piece<T>(p, plan.piece[i], past, st);
         p.a += (int64_t)p.M * p.ld_a;
         p.s_a += (int64_t)p.M * p.ld_sa;
         p.y = (T *)p.y + p.M * p.ld_y;

@@ -151,6 +151,18 @@ def test_linear(gpu_lib, M, N, K, dtype):
     assert_same(y, ref, b, dtype)
 
 
+@pytest.mark.parametrize("M,dtype", [(15001, torch.float32), (29001, torch.bfloat16)])
+def test_results_that_no_cache_holds(gpu_lib, M, dtype):
+    """Larger ones are stored in another way; all sums are exact, so the bits are those of calls for a part of the tokens."""
+    q, N, K = gpu_lib, 4096, 700
+    (a, sa), (w, sw) = codes_of(4, M, K), codes_of(5, N, K)
+    dev = lambda x: torch.from_numpy(x).to(DEV)
+    mat, a, sa = q.pack_mx4(dev(plain.join(w)), dev(sw), K), dev(plain.join(a)), dev(sa)
+    y = q.linear_mx4(mat, a, sa, dtype=dtype)
+    for m in range(0, M, 3000):
+        assert torch.equal(y[m:m + 3000], q.linear_mx4(mat, a[m:m + 3000], sa[m:m + 3000], dtype=dtype))
+
+
 @pytest.mark.parametrize("M,N,K", [(3, 40, 300), (70, 200, 300), (300, 300, 600), (1000, 1000, 260)])
 def test_linear_without_bias_into_rows_that_lie_apart(gpu_lib, M, N, K):
     for lead, pitch, dtype in ((0, N + 5, torch.float32), (1, N + 16, torch.bfloat16), (4, N + 128 - N % 128, torch.float16), (0, N, torch.bfloat16)):
