@@ -25,6 +25,22 @@ constexpr float LOG2E = 1.4426950408889634f, FAR = -300.0f;   // 2^FAR is 0 in f
 constexpr float MOST = 0x1p100f;                              // r stays within
 constexpr double LN2 = 0.69314718055994530942;
 
+// ln s of a positive number to 2^-32: s = 2^e m with m in [2/3, 4/3), ln m = 2 (z + z^3 / 3 + z^5 / 5 + ...) with z = (m - 1) / (m + 1), at most
+// 1/5 in magnitude; behind z^11 / 11 less than 2^-32 is left out.  (log(), exact to the last bit, takes
+// four times the instructions, a quarter of a short row's: 16384 x 64 fp32 without alternatives 8.1 us with it, 6.6 without.)
+__device__ __forceinline__ double log_of_sum(double s)
+{
+    double m = __builtin_amdgcn_frexp_mant(s);   // [1/2, 1)
+    int e = __builtin_amdgcn_frexp_exp(s);
+    const bool low = m < 2.0 / 3.0;
+    m = low ? 2.0 * m : m;
+    e = low ? e - 1 : e;
+    const double b = m + 1.0, r0 = (double)__builtin_amdgcn_rcpf((float)b), r = fma(fma(-b, r0, 1.0), r0, r0);   // (off by 2^-44)
+    const double z = (m - 1.0) * r, q = z * z;
+    const double p = fma(fma(fma(fma(fma(q, 1.0 / 11, 1.0 / 9), q, 1.0 / 7), q, 1.0 / 5), q, 1.0 / 3), q, 1.0);
+    return fma((double)e, LN2, 2.0 * z * p);
+}
+
 // A part's sums.
 struct QrScoresSum {
     double r, s, u;
@@ -69,12 +85,13 @@ struct QrScoresToken {
 struct QrScoresRow {
     double r, log_s, entropy;
     bool none, bad;   // no token can be; a logit is NaN or +inf
+    QrScoresRow() = default;
     __device__ __forceinline__ explicit QrScoresRow(const QrScoresSum &a)
     {
         r = a.r;
         none = a.s == 0.0;
         bad = !(a.s == a.s);
-        log_s = log(a.s);
+        log_s = log_of_sum(a.s);
         entropy = none ? 0.0 : log_s - LN2 * (a.u / a.s);
     }
     __device__ __forceinline__ float logp(float logit) const { return none ? -INFINITY : (float)(LN2 * ((double)logit * (double)LOG2E - r) - log_s); }
@@ -100,6 +117,11 @@ struct QrChunk {
     static __device__ __forceinline__ bool holds(int v, int n) { return v == 0 || v * 64 * V < n; }
     __device__ __forceinline__ void load(const T *x, int n, int lane)
     {
+        if (n >= LEN) {   // uniform
+#pragma unroll
+            for (int v = 0; v < 4; ++v) raw[v] = __builtin_bit_cast(v4i, *(const typename QrVec<T>::any *)(x + (v * 64 + lane) * V));
+            return;
+        }
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int c = (v * 64 + lane) * V;
@@ -413,14 +435,19 @@ __global__ __launch_bounds__(256, TOP ? 8 : 4) void scores_wave_kernel(const QrS
         if (count > 128) keep_best<CAP>(list, count, a.n, a.n, lane);
         const QrCand c0 = lane < count ? list[lane] : 0ull, c1 = lane + 64 < count ? list[lane + 64] : 0ull;
         int r0 = 0, r1 = 0;
+        if (count <= 64) {   // uniform
 #pragma unroll 4
-        for (int j = 0; j < count; ++j) {
-            const QrCand o = list[j];
-            r0 += o > c0 ? 1 : 0;
-            r1 += o > c1 ? 1 : 0;
+            for (int j = 0; j < count; ++j) r0 += list[j] > c0 ? 1 : 0;
+        } else {
+#pragma unroll 4
+            for (int j = 0; j < count; ++j) {
+                const QrCand o = list[j];
+                r0 += o > c0 ? 1 : 0;
+                r1 += o > c1 ? 1 : 0;
+            }
+            if (c1 != 0ull && r1 < a.n) values.write_rank(a, row, r1, c1);
         }
         if (c0 != 0ull && r0 < a.n) values.write_rank(a, row, r0, c0);
-        if (c1 != 0ull && r1 < a.n) values.write_rank(a, row, r1, c1);
         if (lane >= count && lane < a.n) values.write_rank(a, row, lane, 0ull);
     }
 }
@@ -556,6 +583,7 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         __syncthreads();
         sum = sums[lane & (NW - 1)];
     }
+    QrScoresRow values;
     if (wave == 0) {   // joins the sums, the others rank
         double to = sum.r;
 #pragma unroll
@@ -565,6 +593,10 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         for (int off = 1; off < NW; off <<= 1) {
             sum.s += __shfl_xor(sum.s, off);
             sum.u += __shfl_xor(sum.u, off);
+        }
+        if (a.n_parts == 1) {
+            values = QrScoresRow(sum);
+            if (lane == 0) values.write(a, row, token);
         }
     } else if (TOP) {
         for (int i0 = 0; i0 < M; i0 += 16 * (NW - 1)) {   // uniform; four threads count for one candidate
@@ -587,12 +619,9 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         }
         return;
     }
-    if (!TOP && wave > 0) return;
-    const QrScoresRow values(sum);
-    if (tid == 0) values.write(a, row, token);
     if (TOP) {
         __syncthreads();
-        if (tid < a.n) values.write_rank(a, row, tid, ranked[tid]);
+        if (tid < a.n) values.write_rank(a, row, tid, ranked[tid]);   // (wave 0)
     }
 }
 
@@ -635,6 +664,7 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
         if (mine != 0ull && (unsigned)(mine >> 32) >= bound) all[atomicAdd(&n_all, 1)] = mine;
         __syncthreads();
     }
+    QrScoresRow values;
     if (wave == 0) {   // joins the sums, the others rank
         // (the r of a part that holds no finite logit, 0, may be above the others': it counts only where there is something to it)
         const bool some = sum.s != 0.0;
@@ -648,6 +678,8 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
             sum.s += __shfl_xor(sum.s, off);
             sum.u += __shfl_xor(sum.u, off);
         }
+        values = QrScoresRow(sum);
+        if (lane == 0) values.write(a, row, token);
     } else if (a.n > 0) {
         const int M = n_all;
         for (int i0 = 0; i0 < M; i0 += 16 * (MAX_PARTS - 1)) {   // uniform; four threads count for one candidate
@@ -661,11 +693,9 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
             if ((tid & 3) == 0 && i < M && rank < a.n) ranked[rank] = c;
         }
     }
-    const QrScoresRow values(sum);
-    if (tid == 0) values.write(a, row, token);
     if (a.n > 0) {
         __syncthreads();
-        if (tid < a.n) values.write_rank(a, row, tid, ranked[tid]);
+        if (tid < a.n) values.write_rank(a, row, tid, ranked[tid]);   // (wave 0)
     }
 }
 
