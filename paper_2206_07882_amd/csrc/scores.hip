@@ -19,7 +19,8 @@
 
 namespace {
 
-constexpr int MAX_TOP = 64, CAP = 256, LIST = 1024;   // ranks; candidates in a wave's and in a workgroup's list
+constexpr int MAX_TOP = 64, CAP = 256;        // ranks; candidates in a wave's list
+constexpr int LIST = 1024, VECS = 512;       // candidates and vectors in a workgroup's lists
 constexpr int MAX_PARTS = 16, FEW_RANKS = 24;
 constexpr float LOG2E = 1.4426950408889634f, FAR = -300.0f;   // 2^FAR is 0 in fp32
 constexpr float MOST = 0x1p100f;                              // r stays within
@@ -318,7 +319,31 @@ struct QrScoresWave {
             take(f, i);
         }
     }
-    // The same into a wave's list, which never overflows: where it is full its n best are kept.  first: index of the chunk's first logit.
+    // Vectors that hold a logit from `least` on into a workgroup's list, while it has room.  at: index of the chunk's first logit.
+    __device__ __forceinline__ void vectors_to(v4i *vecs, int *index, int *n_vecs, int room, float least, int at, int lane) const
+    {
+        if (!__ballot(largest >= least)) return;
+        unsigned long long m[4];
+        int some = 0;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            m[v] = __ballot(best[v] >= least);
+            some += (int)__popcll(m[v]);
+        }
+        int to = 0;
+        if (lane == 0) to = atomicAdd(n_vecs, some);
+        to = __builtin_amdgcn_readfirstlane(to);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int mine = to + lanes_below(m[v]);
+            if (best[v] >= least && mine < room) {
+                vecs[mine] = now.raw[v];
+                index[mine] = at + (v * 64 + lane) * V;
+            }
+            to += (int)__popcll(m[v]);
+        }
+    }
+    // Logits from the key on into a wave's list, which never overflows: where it is full its n best are kept.  first: index of the chunk's first logit.
     template <class List>
     __device__ __forceinline__ void hits_to(List list, int &count, unsigned &key, int n, const T *x, int first, int lane)
     {
@@ -476,13 +501,22 @@ __device__ __attribute__((noinline)) QrCand best_of_any(const T *x, int len, int
 template <class T, int NW, bool TOP>
 __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScoresArgs a)
 {
-    constexpr int LEN = QrChunk<T>::LEN, BLOCK = NW * LEN;
-    __shared__ QrCand lists[TOP ? NW : 1][TOP ? CAP : 1];   // (of waves by themselves, where the list overflows)
+    constexpr int LEN = QrChunk<T>::LEN, BLOCK = NW * LEN, V = QrVec<T>::N;
+    // Of 16-bit logits whole vectors go to a list first, which the workgroup looks through at the end: to look for a logit in a vector of
+    // eight takes a wave 28 instructions, as many as to add it up (16 alternatives, 1024 x 32000 21.4 us so, 20.2 with vectors; 4096 x 32000
+    // 62 and 58; of fp32, vectors of four, 4096 x 8000 25 and 29, 64 x 131072 13.0 and 13.5).
+    constexpr bool VECTORS = sizeof(T) == 2;
+    constexpr int ROOM = VECTORS ? VECS : LIST, EACH = (ROOM + 64 * NW - 1) / (64 * NW);   // of the first list; of it to a thread
+    constexpr int POOL = !VECTORS || NW * CAP * 8 > VECS * 20 ? NW * CAP * 8 : VECS * 20;
+    __shared__ __attribute__((aligned(16))) char pool[TOP ? POOL : 16];   // vectors and where they begin; or the lists of waves by themselves
     __shared__ QrCand list[TOP ? LIST : 1], ranked[TOP ? MAX_TOP : 1];
+    v4i *vecs = (v4i *)pool;
+    int *index = (int *)(pool + VECS * 16);
     __shared__ unsigned group_best[256], shared_key;
     __shared__ QrScoresSum sums[NW];
     __shared__ float most_of[NW];
-    __shared__ int n_list;
+    __shared__ int n_list, n_vecs;
+    int &n_first = VECTORS ? n_vecs : n_list;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
     if (row >= a.rows) return;   // uniform
@@ -493,7 +527,7 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
     QrScoresToken token;
     if (a.n_parts == 1 && wave == 0) token.load<T>(a, row);
     if (TOP) {
-        if (tid == 0) n_list = 0;
+        if (tid == 0) n_list = n_vecs = 0;
         if (tid < MAX_TOP) ranked[tid] = 0ull;
     }
     // every thread has a key: a bound from below of the n-th best, by the best keys of groups of threads.  The work is wave 0's, the
@@ -537,26 +571,49 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         w.template add<TOP>(n - mine);
         if (TOP && !over) {
             __syncthreads();
-            w.hits(least_of(shared_key), x + mine, lane, [&](float f, int i) { push(qr_cand(qr_float_key(f + 0.0f), first + mine + i)); });
+            if (VECTORS) w.vectors_to(vecs, index, &n_first, ROOM, least_of(shared_key), mine, lane);
+            else w.hits(least_of(shared_key), x + mine, lane, [&](float f, int i) { push(qr_cand(qr_float_key(f + 0.0f), first + mine + i)); });
             if (more) {
                 __syncthreads();
-                const int count = n_list;
-                over = count > LIST;
-                if (count > LIST / 2 && !over) {   // uniform: what the list holds raises the bound and goes where it is below
-                    constexpr int EACH = LIST / (64 * NW);
+                const int count = n_first;
+                over = count > ROOM;
+                if (count > ROOM / 2 && !over) {   // uniform: what the list holds raises the bound and goes where it is below
+                    QrChunk<T> held;   // (its first vectors)
+                    int where[EACH];
                     QrCand c[EACH];
-                    unsigned k = 0u;
+                    unsigned key[EACH], k = 0u;
 #pragma unroll
                     for (int i = 0; i < EACH; ++i) {
-                        c[i] = tid + i * 64 * NW < count ? list[tid + i * 64 * NW] : 0ull;
-                        k = (unsigned)(c[i] >> 32) > k ? (unsigned)(c[i] >> 32) : k;
+                        key[i] = 0u;
+                        const int from = tid + i * 64 * NW;
+                        if (from >= count) continue;
+                        if constexpr (VECTORS) {
+                            held.raw[i] = vecs[from];
+                            where[i] = index[from];
+                            float f = held.at(i * V);
+#pragma unroll
+                            for (int j = 1; j < V; ++j) f = fmaxf(f, held.at(i * V + j));
+                            key[i] = qr_logit_key(f);
+                        } else {
+                            c[i] = list[from];
+                            key[i] = (unsigned)(c[i] >> 32);
+                        }
+                        k = key[i] > k ? key[i] : k;
                     }
                     find_bound(k);
-                    if (tid == 0) n_list = 0;
+                    if (tid == 0) n_first = 0;
                     __syncthreads();
 #pragma unroll
-                    for (int i = 0; i < EACH; ++i)
-                        if (c[i] != 0ull && (unsigned)(c[i] >> 32) >= shared_key) push(c[i]);
+                    for (int i = 0; i < EACH; ++i) {
+                        if (key[i] == 0u || key[i] < shared_key) continue;
+                        if constexpr (VECTORS) {
+                            const int to = atomicAdd(&n_first, 1);
+                            vecs[to] = held.raw[i];
+                            index[to] = where[i];
+                        } else {
+                            push(c[i]);
+                        }
+                    }
                 }
             }
         }
@@ -568,9 +625,21 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
     __syncthreads();
     int M = 0;
     if (TOP) {
-        M = n_list;
-        if (M > LIST) {   // uniform
-            list[tid] = best_of_any<T, NW>(x, n, first, a.n, wave, lane, (QrLdsList)lists[wave]);
+        M = n_first;
+        over = M > ROOM;
+        if (VECTORS && !over) {
+            const float least = least_of(shared_key);
+            for (int i = tid; i < M * V; i += 64 * NW) {
+                const float f = (float)((const T *)pool)[i];
+                if (f >= least) push(qr_cand(qr_float_key(f + 0.0f), first + index[i / V] + i % V));
+            }
+            __syncthreads();
+            M = n_list;
+            over = M > LIST;
+        }
+        if (over) {   // uniform
+            __syncthreads();
+            list[tid] = best_of_any<T, NW>(x, n, first, a.n, wave, lane, (QrLdsList)pool + wave * CAP);
             M = 64 * NW;
             __syncthreads();
         }
