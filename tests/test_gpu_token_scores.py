@@ -85,6 +85,23 @@ def test_rising_and_falling_rows(gpu_lib, rows, V, dtype):
         check(gpu_lib, x.contiguous(), some_tokens(3, rows, V), 3)
 
 
+@pytest.mark.parametrize("rows,V", [(3, 9001), (2, 24500), (3, 48999), (70, 140001)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_large_logits_among_small_ones(gpu_lib, rows, V, dtype):
+    """As many as fill the lists of candidates by half, nearly, and over; different or equal, in what is read first or later."""
+    base = logits(V, rows, V, dtype, 0.1)
+    for many in (250, 300, 513, 700, 1000) if rows < 70 else (300, 700):
+        for start in (0, 17000, V - 16 * many) if rows < 70 else (40000,):
+            if start < 0 or start + 16 * many > V:
+                continue
+            x = base.clone()
+            at = start + 16 * torch.arange(many, device=DEV)
+            x[:, at] = 5.0 + torch.arange(many, device=DEV).to(dtype) / 64
+            x[0, at] = 5.0
+            for n in (64, 5) if rows < 70 else (64,):
+                check(gpu_lib, x, None, n)
+
+
 @pytest.mark.parametrize("V", [50, 2500, 9001, 33000, 100000])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_masks(gpu_lib, V, dtype):
