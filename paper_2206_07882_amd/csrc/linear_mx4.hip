@@ -129,11 +129,11 @@ __global__ __launch_bounds__(64 * WAVES) void linear_mx4_few_kernel(const QrMx4L
 // different banks) and both scales of D chunks.  All arrive by
 // direct loads to LDS up to three steps ahead, and a wave reads the next step's first operands before its last matrix instructions of
 // the present one.
-// Bound, large tiles, by the clock that the power leaves the matrix units: 8192^3 bf16 236 us, 4.7 PFLOP/s, where the instructions
+// Bound, large tiles, by the clock that the power leaves the matrix units: 8192^3 bf16 240 us, 4.6 PFLOP/s, where the instructions
 // alone, from registers, reach 7.0 with random operands and 9.7 with zeros (this kernel with zeros: 190 us).  They are busy 57 % of the
 // cycles, at 1.85 GHz; operands of a whole step read a step ahead gave no more (256 us), nor wave tiles of 128 x 128 with one
-// wave to a SIMD (287).  Many rows and tokens of few columns by the stores (16000 x 2560 x 1280 fp32, 164 MB, 44 us;
-// the stores alone take 24): waits that count the last tile's stores in, so that two steps of the next run before these are through,
+// wave to a SIMD (287).  Many rows and tokens of few columns by the stores (16000 x 2560 x 1280 fp32, 164 MB, 45 us;
+// such stores alone take 31): waits that count the last tile's stores in, so that two steps of the next run before these are through,
 // gave nothing (47 us; 8192^3 7 % slower).
 template <int MT, int NT, int WN, int WM, int D>
 struct QrMx4Tile {
@@ -156,7 +156,7 @@ struct QrMx4Tile {
 };
 
 // T: type of y; v4f: the sums themselves go to p.part (a share of a product that is cut along its columns, blockIdx.y).
-template <class T, int MT, int NT, int WN, int WM, int D, bool PAST>
+template <class T, int MT, int NT, int WN, int WM, int D>
 __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Linear p, int tiles_n, int tiles_m)
 {
     using P = QrMx4Tile<MT, NT, WN, WM, D>;
@@ -165,8 +165,8 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
     const int col = lane & 15, grp = lane >> 4;
     const int wn = wave % WN, wm = wave / WN;
     // Workgroups go to the 8 XCDs in turn; each XCD gets a run of tiles, G blocks of rows side by side, so that what runs on it at a
-    // time shares its L2 and writes long pieces of rows (G = 4, 8, 16: 8192^3 234, 232, 243 us; 8192 x 8192 x 2048 75, 72, 72; 16000 x 2560 x
-    // 1280 fp32 45.7, 44.1, 43.3; 16384 x 8192 x 256 fp32 116, 96, 88; 2048 x 32000 x 1536 bf16 56.2, 58.6, 59.9)
+    // time shares its L2 and writes long pieces of rows (G = 4, 8, 16: 8192^3 240, 240, 241 us; 8192 x 8192 x 2048 75, 73, 77; 16000 x 2560 x
+    // 1280 fp32 46.4, 45.2, 45.3; 8192 x 8192 x 256 fp32 60, 51, 48; 4096 x 16384 x 1024 bf16 55, 46, 46; 2048 x 32000 x 1280 bf16 51, 53, 54)
     constexpr int G = 8;
     const int total = tiles_n * tiles_m, n_row_tiles = (p.rows + 15) >> 4;
     const unsigned lds0 = (unsigned)(size_t)lds;
@@ -385,8 +385,10 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
             typedef T vec_e __attribute__((ext_vector_type(E)));
             typedef T vec_4 __attribute__((ext_vector_type(4)));
             // Rows of whole lines are not kept in the L2 (whose lines the operands are in, and which a launch ends with writing back):
-            // stores go through it into the cache behind it, or past both.  Where rows begin inside a line, two stores share it, which only
-            // the L2 can join.  Small results stay in the caches behind it all the same.
+            // large tiles store past it and the cache behind it, the others through it.  (Through, large tiles are as fast or slower where
+            // results do not fall on those of the last call: us, past and through, 16000 x 2560 x 1280 fp32 44 / 51, 2048 x 32000 x 2048 fp32
+            // 85 / 92, 8192 x 8192 x 1280 bf16 53 / 54.  Into one buffer again and again, which the cache holds, it would be 46 / 44.)  Where rows begin inside a
+            // line, two stores share it, which only the L2 can join.  Small results stay in the caches behind it all the same.
             const uintptr_t odd = (uintptr_t)p.y | ((uintptr_t)p.ld_y * sizeof(T));
             const bool pieces = (odd & 127) == 0 || ((odd & 15) == 0 && p.M * p.ld_y * (int64_t)sizeof(T) <= 16 << 20);
             v4f bs[MT];
@@ -405,7 +407,7 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_mx4_kernel(const QrMx4Lin
                     if (tm0 + t < p.M) {
                         if (r0 + r + E <= p.rows) {
                             if (!pieces) *(typename QrVec<T>::any *)y = out[i];
-                            else if (PAST) qr_store_past((float *)y, __builtin_bit_cast(v4f, out[i]));
+                            else if (MT * WN >= 16) qr_store_past((float *)y, __builtin_bit_cast(v4f, out[i]));
                             else qr_store_through((float *)y, __builtin_bit_cast(v4f, out[i]));
                         } else {
 #pragma unroll
@@ -548,11 +550,7 @@ QrMx4Plan plan_linear(int rows, int K, int M, int bytes)
     return best;
 }
 
-// What does not fit into the cache in front of the memory (256 MiB) is stored past it by large tiles (us, through and past: 8192 x 8192 x 2048
-// bf16, 134 MB, 72 / 75, 16000 x 2560 x 1280 fp32, 164 MB, 44 / 46, 12544 x 4608 x 640 fp32, 231 MB, 45 / 54; 13312 x 4608 x 1280 fp32, 245 MB,
-// 68 / 62, 16384 x 4608 x 640 fp32, 302 MB, 82 / 65).
-constexpr int64_t LAST_CACHE = (int64_t)224 << 20;
-template <class T, int MT, int NT, int WN, int WM, int D, bool PAST = false>
+template <class T, int MT, int NT, int WN, int WM, int D>
 void launch_tiles(const QrMx4Linear &p, int parts, hipStream_t st)
 {
     using P = QrMx4Tile<MT, NT, WN, WM, D>;
@@ -561,9 +559,9 @@ void launch_tiles(const QrMx4Linear &p, int parts, hipStream_t st)
     static std::atomic<bool> allowed[QR_MAX_DEVICES];   // per device: more than 64 KiB of LDS
     const int d = qr_current_device();
     if (!allowed[d].load(std::memory_order_relaxed) &&
-        hipFuncSetAttribute((const void *)linear_mx4_kernel<T, MT, NT, WN, WM, D, PAST>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS) == hipSuccess)
+        hipFuncSetAttribute((const void *)linear_mx4_kernel<T, MT, NT, WN, WM, D>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS) == hipSuccess)
         allowed[d].store(true, std::memory_order_relaxed);   // (where it failed the launch says so, and the next call asks again)
-    linear_mx4_kernel<T, MT, NT, WN, WM, D, PAST><<<dim3((unsigned)(tn * tm < places ? tn * tm : places), parts), P::THREADS, P::LDS, st>>>(p, tn, tm);
+    linear_mx4_kernel<T, MT, NT, WN, WM, D><<<dim3((unsigned)(tn * tm < places ? tn * tm : places), parts), P::THREADS, P::LDS, st>>>(p, tn, tm);
 }
 
 template <class T, int RT, int NT, int WAVES>
@@ -573,7 +571,7 @@ void launch_few(const QrMx4Linear &p, hipStream_t st)
 }
 
 template <class T>
-void launch_piece(const QrMx4Linear &p, const QrMx4Piece &piece, bool past, hipStream_t st)
+void launch_piece(const QrMx4Linear &p, const QrMx4Piece &piece, hipStream_t st)
 {
     switch (piece.kind) {
     case FEW:
@@ -597,20 +595,16 @@ void launch_piece(const QrMx4Linear &p, const QrMx4Piece &piece, bool past, hipS
         }
         return;
     case MIDDLE: launch_tiles<T, 4, 4, 2, 2, 2>(p, 1, st); return;
-    case LARGE:
-        if (past) launch_tiles<T, 8, 4, 2, 4, 2, true>(p, 1, st);
-        else launch_tiles<T, 8, 4, 2, 4, 2>(p, 1, st);
-        return;
+    case LARGE: launch_tiles<T, 8, 4, 2, 4, 2>(p, 1, st); return;
     }
 }
 
 template <class T>
 void launch_linear(QrMx4Linear p, const QrMx4Plan &plan, hipStream_t st)
 {
-    const bool past = (int64_t)p.M * p.rows * (int)sizeof(T) > LAST_CACHE;
     for (int i = 0; i < plan.n; ++i) {
         p.M = plan.piece[i].M;
-        launch_piece<T>(p, plan.piece[i], past, st);
+        launch_piece<T>(p, plan.piece[i], st);
         p.a += (int64_t)p.M * p.ld_a;
         p.s_a += (int64_t)p.M * p.ld_sa;
         p.y = (T *)p.y + p.M * p.ld_y;

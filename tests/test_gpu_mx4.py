@@ -153,7 +153,7 @@ def test_linear(gpu_lib, M, N, K, dtype):
 
 @pytest.mark.parametrize("M,dtype", [(15001, torch.float32), (29001, torch.bfloat16)])
 def test_results_that_no_cache_holds(gpu_lib, M, dtype):
-    """Larger ones are stored in another way; all sums are exact, so the bits are those of calls for a part of the tokens."""
+    """All sums are exact, so the bits are those of calls for a part of the tokens."""
     q, N, K = gpu_lib, 4096, 700
     (a, sa), (w, sw) = codes_of(4, M, K), codes_of(5, N, K)
     dev = lambda x: torch.from_numpy(x).to(DEV)
