@@ -4,8 +4,8 @@
 // With S = sum 2^(x L - r), U = sum 2^(x L - r)(x L - r), L = log2(e), for any r:  log P(x) = ln 2 (x L - r) - log S,
 // entropy = log S - ln 2 U / S.  A wave takes the largest logit of the first that it reads for r, a product, a sum, an exponential and
 // two more sums a logit then do; where a logit passes r by far (a sum of 2^12) sums move to a larger one.  Lanes add up at the end of
-// the row, in fp32.  Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read again, with x - max
-// formed first.
+// the row, in fp32.  Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read
+// again, with x - max formed first.
 //
 // The best alternatives: the n-th largest of groups of the logits that are read first bounds the n-th best from below.  What reaches the
 // bound goes to a list in LDS, of which the n best are kept where it fills, and their smallest becomes the bound; at the end a
@@ -420,7 +420,8 @@ __device__ __attribute__((noinline)) QrScoresSum sums_of_any(const T *x, int n, 
 }
 
 // A wave to a row: many rows, or short ones.  Grid: y (and z) = four rows.
-// Bound by memory where rows are long (16384 x 32000 bf16, 1.05 GB: 190 us, 5.5 TB/s; with eight waves to a SIMD instead of four 198).
+// Bound by what its instructions take, and by memory (16384 x 32000 bf16, 1.05 GB, 16 alternatives: 225 us, 4.7 TB/s).  Without
+// alternatives four waves to a SIMD (the same rows 190 us, with eight and their fewer registers 198).
 template <class T, bool TOP>
 __global__ __launch_bounds__(256, TOP ? 8 : 4) void scores_wave_kernel(const QrScoresArgs a)
 {
@@ -496,8 +497,9 @@ __device__ __attribute__((noinline)) QrCand best_of_any(const T *x, int len, int
 
 // A workgroup of NW waves to a row or a part of one.  Grid: x = part of a row, y (and z) = row.
 // Bound by a chain, not by memory: load, largest logit, bound, sums, list, ranks, one workgroup behind the other at each place on the
-// device (1024 x 32000 bf16, 65.5 MB, 16 alternatives 23 us; without alternatives 15, 4.4 TB/s).  What the waves do on the chain is
-// shared out: one searches the bound while the others add up, one joins the sums while the others rank.
+// device (1024 x 32000 bf16, 65.5 MB, 16 alternatives 20 us, of which vector units are busy 12; without alternatives 13.6, 4.8 TB/s).
+// What the waves do on the chain is shared out: one searches the bound while the others add up, one joins the sums while the others
+// rank.  Many long rows without alternatives are bound by memory (16384 x 32000 bf16, 1.05 GB, 175 us, 6.0 TB/s).
 template <class T, int NW, bool TOP>
 __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScoresArgs a)
 {
@@ -769,17 +771,18 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
 }
 
 // Waves to a row, and parts of it.  A wave reads CHUNK = 256 vectors at a time, a workgroup of 16 waves 16 times as many.
-// Measured (us; 1 / 4 / 8 / 16 waves), 16 alternatives: 1024 x 32000 bf16 36.9 / 25.8 / 22.6 / 24.2, 4096 x 32000 68 / 68 / 62 / 78, 8192 x
-// 32000 125 / 133 / 124 / 154, 256 x 8000 15.7 / 5.8 / 6.9 / 8.7, 256 x 131072 fp32 136 / 72 / 43 / 31, 4096 x 2500 fp32 14.6 / 17.7 / 28 /
-// 54; none: 1024 x 32000 bf16 18.9 / 14.9 / 15.1 / 16.0, 4096 x 32000 43.1 / 43.4 / 42.2 / 49.2.  In parts, with another launch that
-// joins them (1 / 4 / 8 / 16 of them): 1 x 131072 fp32 17.7 / 11.3 / 9.2 / 9.7, 16 x 262144 fp32 39 / 25 / 21 / 18, 64 x 131072 fp32 24.5 /
-// 16.3 / 16.6 / 16.5; a row of two pieces of 16 waves, 1 x 32000 fp32, 7.6 whole, 8.7 in two.
+// Measured (us; 1 / 4 / 8 / 16 waves), bf16, without alternatives: 4096 rows x 5000 10.0 / 10.8 / 14.8 / 24, 16384 x 8000 43 / 40 / 56 / 96, 16384 x
+// 16000 102 / 97 / 90 / 122, 16384 x 32000 189 / 184 / 176 / 175, 4096 x 32000 45 / 43 / 41 / 40; with 5: 4096 x 5000 16.9 / 18.6 / 24 / 41, 16384 x
+// 32000 219 / 247 / 230 / 261; with 16: 256 x 8000 12.5 / 5.9 / 5.5 / 6.2, 2048 x 5000 12.9 / 11.0 / 14.2 / 23, 4096 x 32000 66 / 64 / 53 / 67, 16384 x
+// 8000 72 / 66 / 93 / 162, 16384 x 16000 127 / 133 / 123 / 200, 16384 x 32000 225 / 253 / 230 / 271; 256 x 131072 fp32 135 / 71 / 45 / 34.  In parts,
+// with another launch that joins them (1 / 4 / 8 / 16 of them), fp32, 20 alternatives: 1 x 131072 20.0 / 10.4 / 8.5 / 8.6, 16 x 262144 40 / 19 / 12.7 /
+// 10.7, 64 x 131072 34 / 13.2 / 12.7 / 17.1, 128 x 131072 36 / 22 / 20 / 27 (two 25); two pieces, 1 x 32000 with 5, 7.0 whole, 6.8 in four.
 constexpr int FEW_ROWS = 256, STRETCH = 16384;   // (the shortest that a workgroup of 16 waves reads at a time)
 void plan_scores(int rows, int V, int n, int chunk, int &waves, int &n_parts, int &part)
 {
     const int chunks = (V + chunk - 1) / chunk;
-    if (chunks == 1 || rows >= 8192 || (chunks <= 3 && rows >= 2048) || (n == 0 && rows >= 4096)) waves = 1;
-    else waves = chunks <= 6 ? 4 : chunks <= 24 ? 8 : 16;
+    if (chunks == 1 || (chunks <= 3 && rows >= 2048 && n < 16) || (chunks > 8 && rows >= 8192 && n > 0)) waves = 1;
+    else waves = chunks <= 6 ? 4 : chunks <= (n > 0 ? 24 : 15) ? 8 : 16;
     n_parts = 1;
     const int pieces = (chunks + 15) / 16;
     if (waves == 16 && pieces > 2 && rows < FEW_ROWS) {

@@ -78,9 +78,10 @@ def scores(logits, token, n_top):
 
 
 def scores_tolerance(V, dtype=torch.float32):
-    """What lse and the entropy may be off by.  exp(x - m) with m at most 4 below the largest: x - m, its product with log2(e) and
-    that constant are each rounded (2.5 * 2^-24 of |x - m|, on average at most ln V + 4), an exponential has a step of its own (2^-23), 32 of them
-    are added in fp32 (31 * 2^-24), three joins cost an exponential each: in all less than (25 + 2 ln V) 2^-23 of the sum.  The entropy
-    has the mean of x - m, at most ln V + 8 in magnitude, with twice that, and lse."""
+    """What lse and the entropy may be off by, in steps of 2^-24.  x log2(e) - r, with r at most 12 binary digits (8.4 natural units)
+    below the largest, is rounded once, and so is the constant: 1.25 of |x - r|, on average over the probabilities at most ln V + 8.4
+    (the mean of lse - x is the entropy).  An exponential has a step of its own (2), 32 of them are added in fp32 (31; 7 for V <= 512),
+    then the lanes of a wave (1 + 6), and three joins cost an exponential each (6): less than 50 + 4 ln V in all.  The entropy has the
+    mean of x - m, at most ln V + 8 in magnitude, with twice that, and lse."""
     lse = (25 + 2 * np.log(V)) * 2.0 ** -23
     return lse, 2 * (9 + np.log(V)) * lse
