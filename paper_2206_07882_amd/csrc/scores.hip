@@ -231,14 +231,15 @@ struct QrScoresWave {
     float r = -MOST;
     double s = 0.0, u = 0.0;
 
-    // n: logits from the chunk's start on
+    // n: logits from the chunk's start on; VECS: of its vectors
+    template <int VECS = 4>
     __device__ __forceinline__ void find_best(int n)
     {
         now.fresh();
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             best[v] = -INFINITY;
-            if (!QrChunk<T>::holds(v, n)) continue;   // uniform
+            if (v >= VECS || !QrChunk<T>::holds(v, n)) continue;   // uniform
             best[v] = now.at(v * V);
 #pragma unroll
             for (int i = 1; i < V; ++i) best[v] = fmaxf(best[v], now.at(v * V + i));
@@ -443,7 +444,8 @@ __global__ __launch_bounds__(256, TOP ? 8 : 4) void scores_wave_kernel(const QrS
         const bool more = n - at > LEN;
         QrChunk<T> next;
         if (more) next.load(x + at + LEN, n - at - LEN, lane);
-        if (TOP || at == 0) w.find_best(n - at);
+        if (TOP) w.find_best(n - at);
+        else if (at == 0) w.template find_best<1>(n);   // (enough to begin with)
         if (at == 0) w.start();
         w.template add<TOP>(n - at);
         if (TOP) {
@@ -567,7 +569,8 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         const int mine = at + wave * LEN;
         QrChunk<T> next;
         if (more) next.load(x + mine + BLOCK, n - mine - BLOCK, lane);
-        if (TOP || at == 0) w.find_best(n - mine);
+        if (TOP) w.find_best(n - mine);
+        else if (at == 0) w.template find_best<1>(n - mine);   // (enough to begin with)
         if (at == 0) w.start();
         if (TOP && at == 0) find_bound(qr_logit_key(w.largest));   // (the other waves add up in the meantime)
         w.template add<TOP>(n - mine);
