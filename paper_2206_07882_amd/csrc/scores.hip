@@ -501,7 +501,7 @@ __device__ __attribute__((noinline)) QrCand best_of_any(const T *x, int len, int
 // Bound by a chain, not by memory: load, largest logit, bound, sums, list, ranks, one workgroup behind the other at each place on the
 // device (1024 x 32000 bf16, 65.5 MB, 16 alternatives 20 us, of which vector units are busy 12; without alternatives 13.6, 4.8 TB/s).
 // What the waves do on the chain is shared out: one searches the bound while the others add up, one joins the sums while the others
-// rank.  Many long rows without alternatives are bound by memory (16384 x 32000 bf16, 1.05 GB, 175 us, 6.0 TB/s).
+// rank.  Many long rows without alternatives are bound by memory (16384 x 32000 bf16, 1.05 GB, 168 us, 6.2 TB/s).
 template <class T, int NW, bool TOP>
 __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScoresArgs a)
 {
@@ -774,8 +774,8 @@ __global__ __launch_bounds__(64 * MAX_PARTS) void scores_join_kernel(const QrSco
 }
 
 // Waves to a row, and parts of it.  A wave reads CHUNK = 256 vectors at a time, a workgroup of 16 waves 16 times as many.
-// Measured (us; 1 / 4 / 8 / 16 waves), bf16, without alternatives: 4096 rows x 5000 10.0 / 10.8 / 14.8 / 24, 16384 x 8000 43 / 40 / 56 / 96, 16384 x
-// 16000 102 / 97 / 90 / 122, 16384 x 32000 189 / 184 / 176 / 175, 4096 x 32000 45 / 43 / 41 / 40; with 5: 4096 x 5000 16.9 / 18.6 / 24 / 41, 16384 x
+// Measured (us; 1 / 4 / 8 / 16 waves), bf16, without alternatives: 4096 rows x 5000 10.3 / 10.7 / 14.6 / 23, 16384 x 8000 42 / 40 / 53 / 91, 16384 x
+// 16000 101 / 97 / 87 / 116, 16384 x 32000 187 / 182 / 175 / 168, 4096 x 32000 41 / 42 / 42 / 39; with 5: 4096 x 5000 16.9 / 18.6 / 24 / 41, 16384 x
 // 32000 219 / 247 / 230 / 261; with 16: 256 x 8000 12.5 / 5.9 / 5.5 / 6.2, 2048 x 5000 12.9 / 11.0 / 14.2 / 23, 4096 x 32000 66 / 64 / 53 / 67, 16384 x
 // 8000 72 / 66 / 93 / 162, 16384 x 16000 127 / 133 / 123 / 200, 16384 x 32000 225 / 253 / 230 / 271; 256 x 131072 fp32 135 / 71 / 45 / 34.  In parts,
 // with another launch that joins them (1 / 4 / 8 / 16 of them), fp32, 20 alternatives: 1 x 131072 20.0 / 10.4 / 8.5 / 8.6, 16 x 262144 40 / 19 / 12.7 /
