@@ -246,7 +246,8 @@ struct QrScoresWave {
         }
         largest = fmaxf(-INFINITY, fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3])));
     }
-    __device__ __forceinline__ void start() { r = limited(LOG2E * wave_max(largest)); }
+    // from the first vectors, so that r is the same whether the others' largest are known or not
+    __device__ __forceinline__ void start() { r = limited(LOG2E * wave_max(fmaxf(-INFINITY, best[0]))); }
     __device__ __forceinline__ void add_chunk(int n, float &cs, float &cu)
     {
         cs = cu = 0.0f;
