@@ -53,7 +53,9 @@ struct QrScoresSum {
         s *= c;
         r = to;
     }
-    __device__ __forceinline__ bool good() const { return s > 0.0 && s < INFINITY; }
+    // (both: where d is some 120, e d passes fp32 before e does)
+    __device__ __forceinline__ bool finite() const { return s < INFINITY && fabs(u) < INFINITY; }
+    __device__ __forceinline__ bool good() const { return s > 0.0 && finite(); }
 };
 
 struct QrScoresArgs {
@@ -651,7 +653,7 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         }
     }
     QrScoresSum sum = sums[lane & (NW - 1)];
-    if (__ballot(!(sum.s < INFINITY)) || !__ballot(sum.s > 0.0)) {   // uniform
+    if (__ballot(!sum.finite()) || !__ballot(sum.s > 0.0)) {   // uniform
         __syncthreads();
         const QrScoresSum any = sums_of_any<T, NW>(x, n, wave, lane, most_of);
         if (lane == 0) sums[wave] = any;

@@ -1,0 +1,41 @@
+"""Token scores of rows that hold very large finite logits, either sign, beside ordinary ones: as masks, as single logits, throughout.
+Against 64 bits, within the tolerances of ordinary rows."""
+import pytest
+import torch
+
+from tests.test_gpu_token_scores import DEV, check, logits, some_tokens
+
+pytestmark = pytest.mark.gpu
+# chunks of 256 vectors to a row, and rows: a wave to a row of one chunk and of three, four waves twice, eight, eight or sixteen, sixteen, five parts
+WAYS = [(0.7, 0), (2.5, 2048), (2.5, 0), (5.3, 0), (7.9, 0), (18.3, 0), (30.1, 0), (70.2, 0)]
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def length(chunks, dtype):
+    return int(chunks * (1024 if dtype == torch.float32 else 2048))
+
+
+def check_rows(q, x, rows, seed):
+    """The rows of x by themselves (in two calls where they are too many to be cut into parts), or among `rows` in all."""
+    if rows > x.shape[0]:
+        x = x.repeat((rows + x.shape[0] - 1) // x.shape[0], 1)
+    for piece in x.split(60) if x.shape[1] > 50000 and not rows else [x]:
+        t = some_tokens(seed, piece.shape[0], piece.shape[1])
+        t[::2] = piece[::2].float().argmax(dim=1).int()
+        for n in (0, 3, 40):
+            check(q, piece, t, n)
+
+
+@pytest.mark.parametrize("chunks,rows", WAYS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_masks_of_large_magnitude(gpu_lib, chunks, rows, dtype):
+    """One constant in the tail or the head of a row, as masks are added: exponentials against it may be large and their products with
+    exponents larger."""
+    V = length(chunks, dtype)
+    values = [-1e4, -1e7, -11629081.0, -11629160.0, -1e9, -3080770304.0, -1e10, -1e11, -1e38]
+    values += (-3e9 * (20 / 3) ** torch.rand(15, generator=torch.Generator().manual_seed(1))).tolist()
+    x = logits(V, 2 * len(values), V, dtype)
+    for i, v in enumerate(values):
+        x[2 * i, (1, 300, V // 3, V // 8)[i % 4]:] = v
+        x[2 * i + 1, :(1, 300, V // 2, V - 2)[i % 4]] = v
+    check_rows(gpu_lib, x, rows, 3)
