@@ -1,8 +1,8 @@
 // Scores of given tokens, from logits: log probability of a row's token, entropy of the row, its best alternatives, in one pass
 // over the logits.
 //
-// With S = sum 2^(x L - r), U = sum 2^(x L - r)(x L - r), L = log2(e), for any r:  log P(x) = ln 2 (x L - r) - log S,
-// entropy = log S - ln 2 U / S.  A wave takes the largest logit of the first that it reads for r, a product, a sum, an exponential and
+// With S = sum 2^(x L - r), U = sum 2^(x L - r)(x L - r), L = log2(e), for any r:  log P(x) = (x L - r) / L - log S,
+// entropy = log S - U / (L S).  A wave takes the largest logit of the first that it reads for r, a product, a sum, an exponential and
 // two more sums a logit then do; where a logit passes r by far (a sum of 2^12) sums move to a larger one.  Lanes add up at the end of
 // the row, in fp32.  Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read
 // again, with x - max formed first.
@@ -25,6 +25,7 @@ constexpr int MAX_PARTS = 16, FEW_RANKS = 24;
 constexpr float LOG2E = 1.4426950408889634f, FAR = -300.0f;   // 2^FAR is 0 in fp32
 constexpr float MOST = 0x1p100f;                              // r stays within
 constexpr double LN2 = 0.69314718055994530942;
+constexpr double UNIT = 1.0 / (double)LOG2E;                  // of x L - r, with the L that the sums take (2^-26 from log2(e), of which 1e9 would show)
 
 // ln s of a positive number to 2^-32: s = 2^e m with m in [2/3, 4/3), ln m = 2 (z + z^3 / 3 + z^5 / 5 + ...) with z = (m - 1) / (m + 1), at most
 // 1/5 in magnitude; behind z^11 / 11 less than 2^-32 is left out.  (log(), exact to the last bit, takes
@@ -95,9 +96,9 @@ struct QrScoresRow {
         none = a.s == 0.0;
         bad = !(a.s == a.s);
         log_s = log_of_sum(a.s);
-        entropy = none ? 0.0 : log_s - LN2 * (a.u / a.s);
+        entropy = none ? 0.0 : log_s - UNIT * (a.u / a.s);
     }
-    __device__ __forceinline__ float logp(float logit) const { return none ? -INFINITY : (float)(LN2 * ((double)logit * (double)LOG2E - r) - log_s); }
+    __device__ __forceinline__ float logp(float logit) const { return none ? -INFINITY : (float)(UNIT * ((double)logit * (double)LOG2E - r) - log_s); }
     __device__ __forceinline__ void write(const QrScoresArgs &a, int64_t row, const QrScoresToken &t) const
     {
         if (a.logp) a.logp[row] = t.t < 0 ? 0.0f : t.t >= a.V ? NAN : logp(t.x);

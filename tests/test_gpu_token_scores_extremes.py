@@ -39,3 +39,16 @@ def test_masks_of_large_magnitude(gpu_lib, chunks, rows, dtype):
         x[2 * i, (1, 300, V // 3, V // 8)[i % 4]:] = v
         x[2 * i + 1, :(1, 300, V // 2, V - 2)[i % 4]] = v
     check_rows(gpu_lib, x, rows, 3)
+
+
+@pytest.mark.parametrize("V", [50, 3000, 9001, 100000])
+def test_tokens_far_below_the_others(gpu_lib, V):
+    """A masked token's log probability is its own logit but for the row's lse, rounded once."""
+    rows = 200
+    x = logits(V, rows, V, torch.float32)
+    t = some_tokens(V, rows, V)
+    g = torch.Generator().manual_seed(6)
+    low = -torch.exp2(torch.randint(10, 127, (rows,), generator=g)) * (1 + 0.2 * torch.rand(rows, generator=g))
+    x[torch.arange(rows, device=DEV), t.long()] = low.to(DEV)
+    check(gpu_lib, x, t, 0)
+    check(gpu_lib, x[:, :40].contiguous(), t % 40, 40)
