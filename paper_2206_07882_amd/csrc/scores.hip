@@ -4,8 +4,8 @@
 // With S = sum 2^(x L - r), U = sum 2^(x L - r)(x L - r), L = log2(e), for any r:  log P(x) = (x L - r) / L - log S,
 // entropy = log S - U / (L S).  A wave takes the largest logit of the first that it reads for r, a product, a sum, an exponential and
 // two more sums a logit then do; where a logit passes r by far (a sum of 2^12) sums move to a larger one.  Lanes add up at the end of
-// the row, in fp32.  Rows that fp32 cannot hold this way (logits beyond 2^99, infinities, NaN, nothing but -inf) show in S and are read
-// again, with x - max formed first.
+// the row, in fp32.  What fp32 cannot hold this way (a largest logit beyond 1.1e7 in magnitude, where x L is no longer
+// known to 1, infinities, NaN, nothing but -inf) shows in S and U and is read again, with x - max formed first.
 //
 // The best alternatives: the n-th largest of groups of the logits that are read first bounds the n-th best from below.  What reaches the
 // bound goes to a list in LDS, of which the n best are kept where it fills, and their smallest becomes the bound; at the end a
@@ -23,7 +23,7 @@ constexpr int MAX_TOP = 64, CAP = 256;        // ranks; candidates in a wave's l
 constexpr int LIST = 1024, VECS = 512;       // candidates and vectors in a workgroup's lists
 constexpr int MAX_PARTS = 16, FEW_RANKS = 24;
 constexpr float LOG2E = 1.4426950408889634f, FAR = -300.0f;   // 2^FAR is 0 in fp32
-constexpr float MOST = 0x1p100f;                              // r stays within
+constexpr float MOST = 0x1p24f;                               // r stays within, so that it is less than 1 from the x L that it was rounded from
 constexpr double LN2 = 0.69314718055994530942;
 constexpr double UNIT = 1.0 / (double)LOG2E;                  // of x L - r, with the L that the sums take (2^-26 from log2(e), of which 1e9 would show)
 
@@ -56,7 +56,8 @@ struct QrScoresSum {
     }
     // (both: where d is some 120, e d passes fp32 before e does)
     __device__ __forceinline__ bool finite() const { return s < INFINITY && fabs(u) < INFINITY; }
-    __device__ __forceinline__ bool good() const { return s > 0.0 && finite(); }
+    // Whether a logit lies at r: always, but where all are -inf or beyond MOST.
+    __device__ __forceinline__ bool some() const { return s >= 0.5; }
 };
 
 struct QrScoresArgs {
@@ -395,6 +396,9 @@ __device__ __forceinline__ unsigned first_bound(const QrScoresWave<T> &w, int n)
 }
 
 // Sums of a row's part that are good for any logits: relative to its largest one.  WPR waves of a workgroup, `most` in LDS.
+// (A part that holds nothing but masks of -1e9 comes here: 64 x 131072 fp32, the last of four parts masked so, 16.8 us, with masks of -1e4
+// 7.5.  Differences formed first in the pass itself, for logits beyond MOST, leave no registers to the others: 1024 x 32000 bf16 with 16
+// alternatives 22.5 us instead of 20.0; this function by whole vectors 16384 x 32000 without any 224 instead of 169.)
 template <class T, int WPR>
 __device__ __attribute__((noinline)) QrScoresSum sums_of_any(const T *x, int n, int wave, int lane, float *most)
 {
@@ -460,7 +464,7 @@ __global__ __launch_bounds__(256, TOP ? 8 : 4) void scores_wave_kernel(const QrS
         w.now = next;
     }
     QrScoresSum sum = w.sum();
-    if (!sum.good()) sum = sums_of_any<T, 1>(x, n, 0, lane, nullptr);
+    if (!sum.some() || !sum.finite()) sum = sums_of_any<T, 1>(x, n, 0, lane, nullptr);
     const QrScoresRow values(sum);
     if (lane == 0) values.write(a, row, token);
     if (TOP) {
@@ -654,7 +658,8 @@ __global__ __launch_bounds__(64 * NW, 8) void scores_group_kernel(const QrScores
         }
     }
     QrScoresSum sum = sums[lane & (NW - 1)];
-    if (__ballot(!sum.finite()) || !__ballot(sum.s > 0.0)) {   // uniform
+    // (a wave whose r is above -MOST has one of its logits there; where all r are -MOST one such wave will do)
+    if (__ballot(!sum.finite()) || !__ballot(sum.some())) {   // uniform
         __syncthreads();
         const QrScoresSum any = sums_of_any<T, NW>(x, n, wave, lane, most_of);
         if (lane == 0) sums[wave] = any;

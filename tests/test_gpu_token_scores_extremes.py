@@ -41,6 +41,38 @@ def test_masks_of_large_magnitude(gpu_lib, chunks, rows, dtype):
     check_rows(gpu_lib, x, rows, 3)
 
 
+@pytest.mark.parametrize("chunks,rows", WAYS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_very_large_logit(gpu_lib, chunks, rows, dtype):
+    """In what is read first, and later."""
+    V = length(chunks, dtype)
+    g = torch.Generator().manual_seed(2)
+    values = [1.1e7, 11629079.0, 11629081.0, 11629165.0, 1.2e7, 2e9, 5e9, 1e10, 1e11, 1e15, 1e20, 1e30, 3e38]
+    values += (1e9 * 20 ** torch.rand(24, generator=g)).tolist() + (1e10 * 2 ** torch.rand(11, generator=g)).tolist()
+    x = logits(V, 2 * len(values), V, dtype)
+    for i, v in enumerate(values):
+        x[2 * i, (5, min(300, V - 1), V // 2 + 3, V - 1)[i % 4]] = v
+        x[2 * i + 1, torch.randint(0, V, (1,), generator=g).item()] = v
+    check_rows(gpu_lib, x, rows, 4)
+
+
+@pytest.mark.parametrize("chunks,rows", WAYS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_without_an_ordinary_logit(gpu_lib, chunks, rows, dtype):
+    """One far above the others, all of them large; one and nothing else; all equal; ordinary differences around a large logit."""
+    V = length(chunks, dtype)
+    base = logits(V, 1, V, torch.float32)[0]
+    made = []
+    for at in (5, V // 2 + 3, V - 1):
+        for high, low in ((-1e10, -2e10), (-1e7, -1e9), (1e10, 0.99e10), (2e9, -2e9), (-1e9, float("-inf")), (1.4e10, float("-inf")), (-1e9, -3e38)):
+            r = torch.full((V,), low, device=DEV)
+            r[at] = high
+            made.append(r)
+    for c in [11629079.0 + 4 * i for i in range(25)] + [-11629079.0 - 16 * i for i in range(12)] + [1e10, -1e10, 1e30, -1e30]:
+        made += [torch.full((V,), c, device=DEV), torch.full((V,), c, device=DEV) + torch.round(base)]
+    check_rows(gpu_lib, torch.stack(made).to(dtype), rows, 5)
+
+
 @pytest.mark.parametrize("V", [50, 3000, 9001, 100000])
 def test_tokens_far_below_the_others(gpu_lib, V):
     """A masked token's log probability is its own logit but for the row's lse, rounded once."""
