@@ -235,8 +235,8 @@ qrnnt_status qrnnt_linear_tokens(const qrnnt_qmat *w, const float *bias, const i
  * qrnnt_mx4_pitch(cols) = 16 ceil(cols/32)); its scales are bytes at a pitch of ld_scale (a multiple of 8, at least
  * qrnnt_mx4_scale_pitch(cols) = ceil(cols/32) rounded up to 8).  Codes start on 16-byte boundaries, scales on 8-byte ones.
  * Both pitches are 0 for a number of columns below 1 or above 2^30.  QRNNT_ERR_UNSUPPORTED: more than 2^31 - 1 rows or 2^30
- * columns to quantize, 2^28 rows or tokens, QRNNT_MX4_MAX_COLS columns or 2^36 weights of a linear layer, matrices of more than
- * 2^60 elements. */
+ * columns to quantize, 2^28 rows or tokens, QRNNT_MX4_MAX_COLS columns or 2^36 weights of a linear layer, 2^23 and more tiles of its
+ * result (64 x 64, 128 x 128 or 256 x 256, as the call takes them; no call of up to 64 tokens has so many), matrices of more than 2^60 elements. */
 #define QRNNT_MX4_MAX_COLS (1 << 20)
 int32_t qrnnt_mx4_pitch(int32_t cols);
 int32_t qrnnt_mx4_scale_pitch(int32_t cols);

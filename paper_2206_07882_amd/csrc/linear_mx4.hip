@@ -649,7 +649,7 @@ extern "C" qrnnt_status qrnnt_linear_mx4(const qrnnt_mx4 *w, const float *bias, 
     p.a = a;  p.s_a = a_scale;  p.ld_a = ld_a;  p.ld_sa = ld_scale;  p.M = M;  p.y = y;  p.ld_y = ld_y;
     p.part = workspace;  p.ld_part = qr_round_up(w->rows, 4) / 4;
     const QrMx4Plan plan = plan_linear(w->rows, w->cols, M, (int)qr_dtype_size(y_dtype));
-    // (a grid has less than 2^32 threads)
+    // (numbers of tiles, and of tiles of a stripe, stay far from the end of 32 bits)
     QR_REQUIRE(plan.piece[0].kind == FEW || TILE_COST[plan.piece[0].kind].tiles(w->rows, M) < 1 << 23, QRNNT_ERR_UNSUPPORTED);
     if (y_dtype == QRNNT_F32) launch_linear<float>(p, plan, (hipStream_t)stream);
     else if (y_dtype == QRNNT_F16) launch_linear<_Float16>(p, plan, (hipStream_t)stream);
