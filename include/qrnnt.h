@@ -493,6 +493,7 @@ qrnnt_status qrnnt_beam_select(const float *score, const void *logits, int32_t d
  * tokens.  token[r] < 0 (padding) gives logp 0, whatever the row holds; token[r] >= V gives NaN.
  * The order is exact.  Exponentials are summed in fp32 32 at a time, then in fp64, and over 64 lanes in fp32: lse is off by at most
  * (25 + 2 ln V) 2^-23, the entropy by at most 2 (9 + ln V)(25 + 2 ln V) 2^-23; on top of that each result is rounded to fp32.
+ * How the sums are split goes by type, rows, V and n_top: calls that differ in these may differ within that.
  * logits [device] [rows, V] of `dtype`, row pitch ld elements, rows at any element.  token [device] int32 [rows], or NULL where
  * logp_out is NULL.  Any of logp_out, entropy_out [device] fp32 [rows] may be NULL; top_token_out int32 and top_logp_out fp32
  * [device] may be NULL where n_top is 0.  n_top <= 64, rows <= 2^25, V <= 2^30.  No output may overlap an input.  workspace [device]:
