@@ -90,3 +90,19 @@ def test_sums_that_pass_fp32_are_not_finite(gpu_lib, M, N, K):
     assert int(over.sum()) == M + 1 and np.array_equal(np.isfinite(y), ~over)
     want, mag = va @ vw.T, np.abs(va) @ np.abs(vw).T
     assert (np.abs(y - want)[~over] <= (plain.sum_tolerance(K, mag) + 2.0 ** -24 * np.abs(want))[~over]).all()
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_what_is_not_finite_when_quantized_makes_its_row_nan(gpu_lib, M, N, K, dtype):
+    """The quantizer writes such a block as zeros with a NaN scale; its products are NaN, whatever they meet, zeros too."""
+    q = gpu_lib
+    g = torch.Generator().manual_seed(M)
+    x, w = torch.randn((M, K), generator=g), torch.randn((N, K), generator=g)
+    w[:, :64] = 0.0
+    want = q.linear_mx4(q.pack_mx4(*q.quantize_mx4(w.to(DEV)), K), *q.quantize_mx4(x.to(DEV)), dtype=dtype)
+    x[2, 40], x[M - 1, K - 1], w[N - 1, 3] = float("nan"), float("inf"), -float("inf")
+    y = q.linear_mx4(q.pack_mx4(*q.quantize_mx4(w.to(DEV)), K), *q.quantize_mx4(x.to(DEV)), dtype=dtype)
+    assert bool(y[2].isnan().all()) and bool(y[M - 1].isnan().all()) and bool(y[:, N - 1].isnan().all())
+    rows = [m for m in range(M) if m not in (2, M - 1)]
+    assert torch.equal(y[rows, :N - 1], want[rows, :N - 1])
